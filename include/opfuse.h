@@ -691,6 +691,117 @@ size_t of_mse_workspace_size(int64_t M, int64_t D);
 of_status of_mse_fwd_bwd(const float* y, const float* t, int64_t M, int64_t D, int64_t ld,
                          float* loss, float* dy, void* ws, size_t ws_bytes, void* stream);
 
+/* ---------------------------------------------- rotary positions, attention */
+
+/*
+ * Attention of the Transformer blocks (support operators: the paper trains a Transformer, Appendix C,
+ * and defines none of them).  Tensors are [T, H, D]: row t (a token), head h, element d is at
+ * t * ld + h * hs + d, so a row can hold its heads one after the other (hs = D), the heads can lie
+ * behind each other (ld = D, hs = T * D), and Q, K and V can be parts of one packed QKV row.  A
+ * stride of 0 means that of a contiguous [T, H, D] tensor (ld = H * D, hs = D).  Row strides are at
+ * most 2^22 elements; rows may not overlap.  dtype OF_F32 or OF_BF16 is the type in memory
+ * (uint16 bit patterns for bf16) and of the matrix-core operands; every sum, row statistic and angle
+ * is fp32 or wider.  bf16 pointers must be 2-byte aligned; 128-bit paths are used when pointers are
+ * 16-byte aligned and strides (attention: and D) are multiples of 16 bytes.
+ */
+
+/* How the rotary frequencies w_i = base^(-2i/rot), i < rot/2, are changed for longer contexts. */
+typedef enum of_rope_scaling {
+  OF_ROPE_NONE = 0,
+  OF_ROPE_LINEAR = 1,  /* w_i / factor (positions are compressed) */
+  OF_ROPE_BASE = 2,    /* base * factor^(rot / (rot - 2)) for base: the slowest pair turns 1 / factor as fast */
+  OF_ROPE_BANDS = 3    /* by the turns n_i = orig_len * w_i / (2 pi) of the trained length: w_i from
+                          high_turns on, w_i / factor up to low_turns, linear in n_i between them */
+} of_rope_scaling;
+
+typedef struct of_rotary_desc {
+  int64_t T;            /* rows */
+  int64_t seq_len;      /* pos == NULL: row t is at position pos0 + t % seq_len; 0 means T */
+  int64_t pos0;
+  int32_t H, D;         /* heads turned (e.g. the query and key heads of a packed row), head width */
+  int32_t rot;          /* leading elements of a head that are turned: even, <= D, <= 512 */
+  int32_t interleaved;  /* pairs: 0: (i, i + rot/2); 1: (2i, 2i + 1) */
+  int32_t dtype;        /* of_dtype of both tensors */
+  int32_t scaling;      /* of_rope_scaling */
+  int64_t ldx, hsx;     /* layout of x and dx */
+  int64_t ldy, hsy;     /* layout of y and dy */
+  double base;          /* e.g. 10000 */
+  double factor, orig_len, low_turns, high_turns;   /* of the scaling; others ignored */
+  float mscale;         /* factor of the turned elements; 0 means 1 */
+} of_rotary_desc;
+
+/*
+ * Rotary positions.  Pair (u, v) of row t at position p, with a = p * w_i (float64):
+ *   (u, v) -> mscale * (u cos a - v sin a,  u sin a + v cos a);
+ * elements from rot on are copied.  pos: int64 [T] (device), or NULL (see seq_len).  y may be x
+ * (in place, one layout: elements from rot on stay as they are) and must not overlap it otherwise.
+ */
+of_status of_rotary_fwd(const of_rotary_desc* d, const void* x, const int64_t* pos, void* y, void* stream);
+
+/* Its gradient, dx = transpose(dy): the same turn backwards.  dy has the y layout, dx the x layout;
+ * dx may be dy (one layout) and must not overlap it otherwise. */
+of_status of_rotary_bwd(const of_rotary_desc* d, const void* dy, const int64_t* pos, void* dx, void* stream);
+
+/*
+ * Softmax attention over nseq sequences.  Sequence s has queries (rows of q, o) and keys (rows of
+ * k, v):
+ *   q_off == NULL: the Tq rows are nseq slots of Tq / nseq rows; else slot s is rows
+ *     [q_off[s], q_off[s + 1]) (int32 [nseq + 1], device, not decreasing);
+ *   q_len == NULL: the slot is the sequence; else its first q_len[s] rows are (int32 [nseq], device),
+ *   and k_off, k_len the same for keys.
+ * The offsets and lengths are read by the kernels; values that would leave [0, T) are cut to it.
+ * Rows of no sequence (behind a length or the last offset) are never read or written.
+ *
+ * Query i of a sequence of nq queries and nk keys is at position p = i + nk - nq (the last query sees
+ * the last key: a generation step has nq = 1) and sees key j if
+ *   causal: j <= p;   window > 0: j > p - window, and j < p + window without causal.
+ * With z_ij = scale * q_i . k_j over the keys it sees (query heads h of a group of Hq / Hkv share key head
+ * h / (Hq / Hkv)):
+ *   lse_i = log sum_j exp(z_ij),  o_i = sum_j exp(z_ij - lse_i) v_j;
+ * a query that sees no key has o = 0, lse = -infinity and gives and gets no gradient.  What a query does
+ * not see is left out by its place, not by its value: K and V of other sequences and of rows of none
+ * may hold anything; a NaN or an infinity in a row of a sequence may reach every row of that sequence.
+ */
+typedef struct of_attn_desc {
+  int64_t Tq, Tk;        /* rows of q, o and of k, v */
+  int64_t nseq;          /* sequences */
+  int32_t Hq, Hkv;       /* query heads, key (and value) heads: Hq a multiple of Hkv */
+  int32_t D;             /* head width, 1 .. 256 */
+  int32_t dtype;         /* of_dtype of q, k, v, o */
+  int32_t grad_dtype;    /* backward: of_dtype of dout, dq, dk, dv (OF_BF16 only with dtype OF_BF16; fp32
+                            gradients of bf16 operands: dout is rounded to bf16 as an operand) */
+  int32_t causal;        /* 0 or 1 */
+  int64_t window;        /* 0: none */
+  int64_t ldq, hsq;      /* layout of q and dq */
+  int64_t ldk, hsk;      /* layout of k and dk */
+  int64_t ldv, hsv;      /* layout of v and dv */
+  int64_t ldo, hso;      /* layout of o and dout */
+  float scale;           /* 0 means 1 / sqrt(D) */
+  const int32_t *q_off, *k_off, *q_len, *k_len;
+} of_attn_desc;
+
+typedef enum of_attn_op { OF_ATTN_FWD = 0, OF_ATTN_BWD = 1 } of_attn_op;
+
+/* Bytes of workspace `op` needs for `d` (0 if none; 0 and OF_EINVAL or OF_EUNSUPPORTED in
+ * of_last_error() for an invalid descriptor).  16-byte aligned; its content does not matter. */
+size_t of_attn_workspace_size(const of_attn_desc* d, int32_t op);
+
+/* Forward.  lse: fp32 [Hq, Tq], kept for the backward, or NULL.  o must not overlap an input. */
+of_status of_attn_fwd(const of_attn_desc* d, const void* q, const void* k, const void* v, void* o, float* lse,
+                      void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Backward.  With P = exp(z - lse) computed again, dP_ij = dout_i . v_j and delta_i = dout_i . o_i:
+ *   dv_j = sum_i P_ij dout_i,  dS_ij = P_ij (dP_ij - delta_i),
+ *   dq_i = scale sum_j dS_ij k_j,  dk_j = scale sum_i dS_ij q_i
+ * (dk and dv sum over the query heads of the group).  o and lse are the forward's.  Deterministic: no
+ * atomics.  Keys that no query sees get zeros.  dq, dk and dv must not overlap an input or each other
+ * (they may be parts of one packed row).
+ */
+of_status of_attn_bwd(const of_attn_desc* d, const void* q, const void* k, const void* v, const void* o,
+                      const float* lse, const void* dout, void* dq, void* dk, void* dv, void* ws,
+                      size_t ws_bytes, void* stream);
+
 /* ---------------------------------------------------------- measurement */
 
 /*

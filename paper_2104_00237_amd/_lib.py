@@ -71,6 +71,30 @@ class OfConvDesc(ctypes.Structure):
                 ("stride", c_int32)]   # 0 or 1: stride 1; 2: depthwise stride 2
 
 
+OF_ROPE_NONE, OF_ROPE_LINEAR, OF_ROPE_BASE, OF_ROPE_BANDS = 0, 1, 2, 3
+ROPE_SCALINGS = {"none": OF_ROPE_NONE, "linear": OF_ROPE_LINEAR, "base": OF_ROPE_BASE,
+                 "bands": OF_ROPE_BANDS}
+OF_ATTN_FWD, OF_ATTN_BWD = 0, 1
+
+
+class OfRotaryDesc(ctypes.Structure):
+    _fields_ = [("T", c_int64), ("seq_len", c_int64), ("pos0", c_int64), ("H", c_int32),
+                ("D", c_int32), ("rot", c_int32), ("interleaved", c_int32), ("dtype", c_int32),
+                ("scaling", c_int32), ("ldx", c_int64), ("hsx", c_int64), ("ldy", c_int64),
+                ("hsy", c_int64), ("base", ctypes.c_double), ("factor", ctypes.c_double),
+                ("orig_len", ctypes.c_double), ("low_turns", ctypes.c_double),
+                ("high_turns", ctypes.c_double), ("mscale", c_float)]
+
+
+class OfAttnDesc(ctypes.Structure):
+    _fields_ = [("Tq", c_int64), ("Tk", c_int64), ("nseq", c_int64), ("Hq", c_int32),
+                ("Hkv", c_int32), ("D", c_int32), ("dtype", c_int32), ("grad_dtype", c_int32),
+                ("causal", c_int32), ("window", c_int64), ("ldq", c_int64), ("hsq", c_int64),
+                ("ldk", c_int64), ("hsk", c_int64), ("ldv", c_int64), ("hsv", c_int64),
+                ("ldo", c_int64), ("hso", c_int64), ("scale", c_float), ("q_off", c_void_p),
+                ("k_off", c_void_p), ("q_len", c_void_p), ("k_len", c_void_p)]
+
+
 class OpfuseError(RuntimeError):
     def __init__(self, status, fn, msg):
         super().__init__(f"{fn}: {STATUS_NAMES.get(status, status)}: {msg}")
@@ -156,6 +180,12 @@ _SIGS = {
                                    c_int64, c_int64, c_void_p, c_void_p, c_void_p, c_void_p]),
     "of_reduce_rows": (c_int32, [c_void_p, c_int64, c_int64, c_int64, c_void_p, c_void_p]),
     "of_add": (c_int32, [c_void_p, c_void_p, c_int64, c_void_p, c_void_p]),
+    "of_rotary_fwd": (c_int32, [P(OfRotaryDesc), c_void_p, c_void_p, c_void_p, c_void_p]),
+    "of_rotary_bwd": (c_int32, [P(OfRotaryDesc), c_void_p, c_void_p, c_void_p, c_void_p]),
+    "of_attn_workspace_size": (c_size_t, [P(OfAttnDesc), c_int32]),
+    "of_attn_fwd": (c_int32, [P(OfAttnDesc), c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
+                              c_void_p, c_size_t, c_void_p]),
+    "of_attn_bwd": (c_int32, [P(OfAttnDesc)] + [c_void_p] * 10 + [c_size_t, c_void_p]),
     "of_xent_fwd_bwd": (c_int32, [c_void_p, c_void_p, c_int64, c_int64, c_int64, c_void_p,
                                   c_void_p, c_void_p]),
     "of_mse_workspace_size": (c_size_t, [c_int64, c_int64]),
@@ -221,6 +251,10 @@ def of_dwconv_workspace_size(desc):
     return load().of_dwconv_workspace_size(ctypes.byref(desc))
 
 
+def of_attn_workspace_size(desc, op):
+    return load().of_attn_workspace_size(ctypes.byref(desc), op)
+
+
 def of_layernorm_partial_rows(M):
     return load().of_layernorm_partial_rows(M)
 
@@ -233,7 +267,8 @@ for _n in ("of_linear_fwd", "of_linear_fwd_carry", "of_linear_fwd_res", "of_conv
            "of_maxpool2x2_fwd", "of_maxpool2x2_bwd", "of_avgpool_fwd", "of_avgpool_bwd",
            "of_layernorm_fwd", "of_layernorm_fwd_bf16", "of_layernorm_bwd",
            "of_reduce_rows", "of_add", "of_dwconv_fwd", "of_dwconv_bwd_data",
-           "of_dwconv_bwd_weight", "of_dwconv_wgrad_fused"):
+           "of_dwconv_bwd_weight", "of_dwconv_wgrad_fused", "of_rotary_fwd", "of_rotary_bwd",
+           "of_attn_fwd", "of_attn_bwd"):
     globals()[_n] = _wrap(_n)
 del _n
 

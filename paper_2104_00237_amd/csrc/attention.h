@@ -1,0 +1,209 @@
+// Device helpers shared by the attention kernels: which rows a workgroup works on, LDS tiles and
+// their fragments, loads and stores of head rows.
+//
+// All products run on 32x32 MFMA tiles whose *columns* (lane % 32) are the rows a wavefront owns
+// (queries in the forward and for dQ, keys for dK and dV) and whose rows (registers) are the rows
+// that stream by.  A register k of lane half h = lane / 32 holds streamed row 8 (k/4) + 4 h + k % 4:
+//   - row statistics of an owned row are sums over one lane's registers and its other half's;
+//   - exp(S) is already the B operand of the next product, whose contraction runs over the streamed
+//     rows: the order of a contraction is free, so the A operand (the streamed tile, transposed) is
+//     read in the registers' order and the probabilities never go through LDS.
+#pragma once
+
+#include "attention_seq.h"
+#include "gemm_common.h"
+
+namespace opfuse {
+
+typedef __bf16 abf16x8_t __attribute__((ext_vector_type(8)));
+typedef __bf16 abf16x2_t __attribute__((ext_vector_type(2)));
+typedef float afloat2_t __attribute__((ext_vector_type(2)));
+typedef float afloatx4_t __attribute__((ext_vector_type(4)));
+typedef float acc16_t __attribute__((ext_vector_type(16)));
+typedef short ashort4_t __attribute__((ext_vector_type(4)));
+typedef short ashort8_t __attribute__((ext_vector_type(8)));
+typedef uint32_t au32x4_t __attribute__((ext_vector_type(4)));
+
+constexpr float kLog2e = 1.44269504088896340736f;
+constexpr float kLn2 = 0.69314718055994530942f;
+
+// ------------------------------------------------------------------- tiles
+// A tile in LDS: rows of DP elements (DP * sizeof(T) bytes, 16-byte slots), slot s of row x at slot
+// s ^ swz(x).  Rows are read as fragments (16 bytes of 32 rows at one slot: 16 consecutive rows take
+// all 64 banks) and transposed (four consecutive rows of one 64-byte block, again all banks), so the
+// two low bits of x go to the block bits of the slot and the next two below them.
+template <int SLOTS>
+__device__ __forceinline__ int swz(int x) {
+  if constexpr (SLOTS == 8) return (((x >> 1) & 1) << 2) | ((x >> 2) & 3);   // two rows take the banks
+  return ((x & 3) << 2) | ((x >> 2) & 3);
+}
+
+template <typename T>
+struct Mma;
+
+template <>
+struct Mma<uint16_t> {   // bf16 operands, v_mfma_f32_32x32x16_bf16
+  static constexpr int E = 8;     // elements of a 16-byte slot
+  static constexpr int TR = 16;   // streamed rows of one transposed fragment
+  typedef abf16x8_t frag;
+  static __device__ __forceinline__ acc16_t mma(frag a, frag b, acc16_t c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+  }
+  static __device__ __forceinline__ frag zero() { return __builtin_bit_cast(frag, au32x4_t{0, 0, 0, 0}); }
+  // probabilities u: registers 8u .. 8u + 7, rounded to nearest even (an MFMA operand)
+  static __device__ __forceinline__ frag pack(const acc16_t& s, int u) {
+    au32x4_t r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const afloat2_t v = {s[8 * u + 2 * i], s[8 * u + 2 * i + 1]};
+      r[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(v, abf16x2_t));
+    }
+    return __builtin_bit_cast(frag, r);
+  }
+  // rows r0 .. r0 + 15 of columns x0 .. x0 + 31, transposed: lane: column x0 + lane % 32, rows
+  // 4 h + j and 8 + 4 h + j
+  template <int SLOTS>
+  static __device__ __forceinline__ frag tr(const char* t, int r0, int x0, int lane) {
+    const int r = r0 + (lane >> 5) * 4 + ((lane & 15) >> 2);
+    const int x = x0 + (lane & 16) + (lane & 3) * 4;
+    typedef __attribute__((address_space(3))) ashort4_t* lp;
+    const char* a = t + r * (SLOTS * 16) + (((x >> 3) ^ swz<SLOTS>(r)) << 4) + (x & 4) * 2;
+    const char* b = t + (r + 8) * (SLOTS * 16) + (((x >> 3) ^ swz<SLOTS>(r + 8)) << 4) + (x & 4) * 2;
+    const ashort4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)a);
+    const ashort4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lp)b);
+    return __builtin_bit_cast(frag, (ashort8_t)__builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+  }
+  static __device__ __forceinline__ uint16_t from(float f) { return f32_to_bf16(f); }
+  static __device__ __forceinline__ float to(uint16_t u) { return __uint_as_float((uint32_t)u << 16); }
+};
+
+template <>
+struct Mma<float> {   // fp32 operands, v_mfma_f32_32x32x2_f32: four of them make one fragment's step
+  static constexpr int E = 4;
+  static constexpr int TR = 8;
+  typedef afloatx4_t frag;
+  static __device__ __forceinline__ acc16_t mma(frag a, frag b, acc16_t c) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[j], b[j], c, 0, 0, 0);
+    return c;
+  }
+  static __device__ __forceinline__ frag zero() { return frag{0.f, 0.f, 0.f, 0.f}; }
+  static __device__ __forceinline__ frag pack(const acc16_t& s, int u) {
+    return frag{s[4 * u], s[4 * u + 1], s[4 * u + 2], s[4 * u + 3]};
+  }
+  template <int SLOTS>
+  static __device__ __forceinline__ frag tr(const char* t, int r0, int x0, int lane) {
+    const int x = x0 + (lane & 31);
+    frag f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int r = r0 + (lane >> 5) * 4 + j;
+      f[j] = *reinterpret_cast<const float*>(t + r * (SLOTS * 16) + (((x >> 2) ^ swz<SLOTS>(r)) << 4) + (x & 3) * 4);
+    }
+    return f;
+  }
+  static __device__ __forceinline__ float from(float f) { return f; }
+  static __device__ __forceinline__ float to(float f) { return f; }
+};
+
+// 16 bytes of row x0 + lane % 32 for contraction step s (slot 2 s + h)
+template <typename T, int SLOTS>
+__device__ __forceinline__ typename Mma<T>::frag row_frag(const char* t, int x0, int s, int lane) {
+  const int x = x0 + (lane & 31);
+  return *reinterpret_cast<const typename Mma<T>::frag*>(t + x * (SLOTS * 16) + (((2 * s + (lane >> 5)) ^ swz<SLOTS>(x)) << 4));
+}
+
+// Rows row0 .. row0 + n - 1 (n <= ROWS) of one head into a tile; the rest of the tile is zero, and so
+// are columns from D on.  NT threads.  VEC: 16-byte loads (pointer and strides are multiples of 16
+// bytes and D of a slot), else element by element.
+template <typename T, int SLOTS, int ROWS, int NT, bool VEC>
+__device__ __forceinline__ void load_tile(char* tile, const HeadRows& x, int64_t row0, int head, int n, int D, int tid) {
+  constexpr int E = Mma<T>::E, ES = sizeof(T);
+  n = max(n, 0);
+  const rsrc_t rs = make_rsrc((const T*)x.p + (n ? row0 * x.ld + head * x.hs : 0), n ? (int)(((n - 1) * x.ld + D) * ES) : 0);
+  constexpr int PER = ROWS * SLOTS / NT;
+  static_assert(PER * NT == ROWS * SLOTS, "whole slots per thread");
+  au32x4_t v[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int id = tid + i * NT, r = id / SLOTS, s = id % SLOTS;
+    const uint32_t at = (uint32_t)(r * x.ld * ES) + s * 16;
+    if constexpr (VEC) {
+      v[i] = __builtin_bit_cast(au32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rs, r < n && s * E < D ? at : kOOB, 0, 0));
+    } else if constexpr (ES == 4) {
+#pragma unroll
+      for (int e = 0; e < E; ++e)
+        v[i][e] = __builtin_amdgcn_raw_buffer_load_b32(rs, r < n && s * E + e < D ? at + 4 * e : kOOB, 0, 0);
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; e += 2) {
+        const uint32_t lo = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rs, r < n && s * E + e < D ? at + 2 * e : kOOB, 0, 0);
+        const uint32_t hi = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rs, r < n && s * E + e + 1 < D ? at + 2 * e + 2 : kOOB, 0, 0);
+        v[i][e / 2] = lo | hi << 16;
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int id = tid + i * NT, r = id / SLOTS, s = id % SLOTS;
+    *reinterpret_cast<au32x4_t*>(tile + r * (SLOTS * 16) + ((s ^ swz<SLOTS>(r)) << 4)) = v[i];
+  }
+}
+
+// The lane's own row as B fragments: 16 bytes at slot 2 s + h for every step s.
+template <typename T, int NS, bool VEC>
+__device__ __forceinline__ void load_own(typename Mma<T>::frag (&f)[NS], const T* row, bool has, int D, int lane) {
+  constexpr int E = Mma<T>::E;
+#pragma unroll
+  for (int s = 0; s < NS; ++s) {
+    const int d = (2 * s + (lane >> 5)) * E;
+    f[s] = Mma<T>::zero();
+    if constexpr (VEC) {
+      if (has && d < D) f[s] = *reinterpret_cast<const typename Mma<T>::frag*>(row + d);
+    } else {
+      T t[E];
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        t[e] = 0;
+        if (has && d + e < D) t[e] = row[d + e];
+      }
+      f[s] = __builtin_bit_cast(typename Mma<T>::frag, t);
+    }
+  }
+}
+
+// Accumulators [d, own row] times f, stored to the lane's row.
+template <typename T, int NB>
+__device__ __forceinline__ void store_own(T* row, const acc16_t (&acc)[NB], float f, int D, bool vec, int lane) {
+#pragma unroll
+  for (int b = 0; b < NB; ++b)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int d = b * 32 + g * 8 + (lane >> 5) * 4;
+      float4 v = make_float4(acc[b][4 * g] * f, acc[b][4 * g + 1] * f, acc[b][4 * g + 2] * f, acc[b][4 * g + 3] * f);
+      if (vec && d + 3 < D) {
+        if constexpr (sizeof(T) == 4) st4((float*)row + d, v);
+        else st_bf16x4((uint16_t*)row + d, v);
+      } else {
+        const float e[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (d + j < D) row[d + j] = Mma<T>::from(e[j]);
+      }
+    }
+}
+
+template <int N>
+__device__ __forceinline__ void zero_acc(acc16_t (&a)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int k = 0; k < 16; ++k) a[i][k] = 0.f;
+}
+
+// The other lane half's value of the same column.
+__device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+
+}  // namespace opfuse

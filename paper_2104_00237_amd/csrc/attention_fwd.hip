@@ -1,0 +1,202 @@
+// Softmax attention, forward: O = softmax(scale Q K^T + mask) V and lse = log sum exp, one pass over
+// the keys with a running maximum and sum (the probabilities never reach memory).
+
+#include "attention.h"
+
+namespace opfuse {
+
+namespace {
+constexpr int NW = 4;               // wavefronts of a workgroup
+constexpr int BM = 32 * NW;         // rows: (query, head of the group) pairs, 32 a wavefront
+}  // namespace
+
+// Rows r of a key head's group: query r / G, head r % G, so that the query heads that share a key
+// head share its tiles.  BN: keys of a tile.
+template <typename T, int DP, int BN, bool VEC>
+__global__ __launch_bounds__(256) void attn_fwd_kernel(AttnArgs a) {
+  constexpr int ES = sizeof(T), SLOTS = DP * ES / 16, NS = SLOTS / 2, NB = DP / 32, NK = BN / 32;
+  typedef typename Mma<T>::frag frag;
+  __shared__ __attribute__((aligned(1024))) char sk[BN * SLOTS * 16], sv[BN * SLOTS * 16];
+  const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  int64_t w = blockIdx.x;
+  const int hk = (int)(w % a.Hkv);
+  w /= a.Hkv;
+  const int split = (int)(w % a.nsplit);
+  w /= a.nsplit;
+  int s;
+  int64_t tile;
+  find_tile(a.q_off, a.Tq, a.nseq, a.G, BM, w, s, tile);
+  const SeqRows q = seq_rows(a.q_off, a.q_len, a.Tq, a.nseq, s);
+  const SeqRows kv = seq_rows(a.k_off, a.k_len, a.Tk, a.nseq, s);
+  const int64_t R = (int64_t)q.len * a.G;
+  const int64_t tiles = (R + BM - 1) / BM;
+  if (tile < 0 || tile >= tiles) return;
+  tile = tiles - 1 - tile;                  // with a causal mask the longest rows come first
+  const int shift = kv.len - q.len;
+  const int r0 = (int)(tile * BM), r1 = (int)min(R, (int64_t)r0 + BM);
+  const int r = r0 + wave * 32 + (lane & 31);
+  const bool has = r < R;
+  const int i = fdiv(has ? r : r0, a.dG), h = hk * a.G + ((has ? r : r0) - i * a.G);
+  int lo, hi, klo, khi, lo1, hi0;
+  keys_of(a.causal, a.window, i, shift, kv.len, lo, hi);
+  // keys of the tile's rows: [klo, khi); seen by every row: [lo1, hi0)
+  keys_of(a.causal, a.window, fdiv(r0, a.dG), shift, kv.len, klo, hi0);
+  keys_of(a.causal, a.window, fdiv(r1 - 1, a.dG), shift, kv.len, lo1, khi);
+  klo = klo / BN;                           // in tiles from here on
+  const int nt = max((khi + BN - 1) / BN - klo, 0);
+  const int per = (nt + a.nsplit - 1) / a.nsplit;
+  const int t0 = klo + min(split * per, nt), t1 = klo + min(split * per + per, nt);
+  const unsigned span = has ? max(hi - lo, 0) : 0;
+
+  frag fq[NS];
+  load_own<T, NS, VEC>(fq, (const T*)a.q.p + (q.beg + i) * a.q.ld + (int64_t)h * a.q.hs, has, a.D, lane);
+  acc16_t acc[NB];
+  zero_acc(acc);
+  float m = -INFINITY, l = 0.f;
+
+  for (int t = t0; t < t1; ++t) {
+    const int j0 = t * BN;
+    __syncthreads();
+    load_tile<T, SLOTS, BN, 256, VEC>(sk, a.k, kv.beg + j0, hk, min(BN, kv.len - j0), a.D, tid);
+    load_tile<T, SLOTS, BN, 256, VEC>(sv, a.v, kv.beg + j0, hk, min(BN, kv.len - j0), a.D, tid);
+    __syncthreads();
+    acc16_t z[NK];
+    zero_acc(z);
+#pragma unroll
+    for (int n = 0; n < NK; ++n)
+#pragma unroll
+      for (int u = 0; u < NS; ++u) z[n] = Mma<T>::mma(row_frag<T, SLOTS>(sk, n * 32, u, lane), fq[u], z[n]);
+    if (j0 < lo1 || j0 + BN > hi0 || r1 - r0 < BM) {   // some row does not see some key
+#pragma unroll
+      for (int n = 0; n < NK; ++n)
+#pragma unroll
+        for (int k = 0; k < 16; ++k) {
+          const int j = j0 + n * 32 + (k >> 2) * 8 + half * 4 + (k & 3);
+          if ((unsigned)(j - lo) >= span) z[n][k] = -INFINITY;
+        }
+    }
+    float top = z[0][0];
+#pragma unroll
+    for (int n = 0; n < NK; ++n)
+#pragma unroll
+      for (int k = 0; k < 16; ++k) top = fmaxf(top, z[n][k]);
+    top = fmaxf(top, other_half(top)) * a.c;
+    const float mn = fmaxf(m, top);
+    const float ms = mn == -INFINITY ? 0.f : mn;      // no key so far: exp2(-inf - 0) = 0
+    const float f = exp2_fast(m - ms);
+    m = mn;
+    float sum = 0.f;
+#pragma unroll
+    for (int n = 0; n < NK; ++n)
+#pragma unroll
+      for (int k = 0; k < 16; ++k) {
+        z[n][k] = exp2_fast(__fmaf_rn(z[n][k], a.c, -ms));
+        sum += z[n][k];
+      }
+    l = l * f + sum;
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int k = 0; k < 16; ++k) acc[b][k] *= f;
+#pragma unroll
+    for (int n = 0; n < NK; ++n)
+#pragma unroll
+      for (int u = 0; u < 32 / Mma<T>::TR; ++u) {
+        const frag p = Mma<T>::pack(z[n], u);
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+          acc[b] = Mma<T>::mma(Mma<T>::template tr<SLOTS>(sv, n * 32 + u * Mma<T>::TR, b * 32, lane), p, acc[b]);
+      }
+  }
+  l += other_half(l);
+  if (!has) return;
+  const int64_t stat = (int64_t)h * a.Tq + q.beg + i;
+  if (a.nsplit > 1) {      // this split's sums; attn_join_kernel puts them together
+    const int64_t rows = (int64_t)a.Hq * a.Tq;
+    float* part = a.part + (split * rows + stat) * a.D;
+    store_own(part, acc, 1.f, a.D, a.D % 4 == 0, lane);
+    if (half == 0) {
+      float* st = a.part + a.nsplit * rows * a.D + (split * rows + stat) * 2;
+      st[0] = m;
+      st[1] = l;
+    }
+    return;
+  }
+  store_own((T*)a.o.p + (q.beg + i) * a.o.ld + (int64_t)h * a.o.hs, acc, l > 0.f ? 1.f / l : l == 0.f ? 0.f : l, a.D, a.ovec, lane);
+  if (a.lse && half == 0) a.lse[stat] = l == 0.f ? -INFINITY : __fmaf_rn(m, kLn2, logf(l));
+}
+
+// Joins the splits of a row: O = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s.  A wavefront a row.
+template <typename T>
+__global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int64_t w = blockIdx.x;
+  int s;
+  int64_t tile;
+  find_tile(a.q_off, a.Tq, a.nseq, a.Hq, 4, w, s, tile);
+  const SeqRows q = seq_rows(a.q_off, a.q_len, a.Tq, a.nseq, s);
+  const int64_t r = tile * 4 + (threadIdx.x >> 6);
+  if (tile < 0 || r >= (int64_t)q.len * a.Hq) return;
+  const int64_t i = r / a.Hq;
+  const int h = (int)(r - i * a.Hq);
+  const int64_t rows = (int64_t)a.Hq * a.Tq, stat = h * a.Tq + q.beg + i;
+  const float* st = a.part + a.nsplit * rows * a.D + stat * 2;
+  float m = -INFINITY, l = 0.f;
+  for (int k = 0; k < a.nsplit; ++k) m = fmaxf(m, st[k * rows * 2]);
+  const float ms = m == -INFINITY ? 0.f : m;
+  for (int k = 0; k < a.nsplit; ++k) l += exp2_fast(st[k * rows * 2] - ms) * st[k * rows * 2 + 1];
+  const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
+  T* o = (T*)a.o.p + (q.beg + i) * a.o.ld + (int64_t)h * a.o.hs;
+  for (int d = lane; d < a.D; d += 64) {
+    float x = 0.f;
+    for (int k = 0; k < a.nsplit; ++k)
+      x += exp2_fast(st[k * rows * 2] - ms) * a.part[(k * rows + stat) * a.D + d];
+    o[d] = Mma<T>::from(x * inv);
+  }
+  if (a.lse && lane == 0) a.lse[stat] = l == 0.f ? -INFINITY : __fmaf_rn(m, kLn2, logf(l));
+}
+
+namespace {
+// Splits of the keys: enough workgroups to fill the chip twice, at least 256 keys (of an average
+// sequence) in each.
+int splits(const AttnArgs& a) {
+  const int64_t wgs = attn_tiles(a.Tq, a.nseq, a.q_off != nullptr, a.G, BM) * a.Hkv;
+  const int64_t keys = a.Tk / a.nseq;
+  int64_t n = 1;
+  if (wgs < 256) n = std::min<int64_t>((512 + wgs - 1) / wgs, std::max<int64_t>(1, keys / 256));
+  return (int)std::min<int64_t>(n, 64);
+}
+
+template <typename T, int DP, int BN>
+hipError_t launch(const AttnArgs& a, bool vec, hipStream_t stream) {
+  const int64_t n = attn_tiles(a.Tq, a.nseq, a.q_off != nullptr, a.G, BM) * a.Hkv * a.nsplit;
+  if (vec) hipLaunchKernelGGL((attn_fwd_kernel<T, DP, BN, true>), dim3((unsigned)n), dim3(256), 0, stream, a);
+  else hipLaunchKernelGGL((attn_fwd_kernel<T, DP, BN, false>), dim3((unsigned)n), dim3(256), 0, stream, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.nsplit == 1) return e;
+  const int64_t nj = attn_tiles(a.Tq, a.nseq, a.q_off != nullptr, a.Hq, 4);
+  hipLaunchKernelGGL((attn_join_kernel<T>), dim3((unsigned)nj), dim3(256), 0, stream, a);
+  return hipGetLastError();
+}
+}  // namespace
+
+size_t attn_fwd_ws_bytes(const AttnArgs& a) {
+  const int n = splits(a);
+  return n == 1 ? 0 : (size_t)n * a.Hq * a.Tq * (a.D + 2) * 4;
+}
+
+hipError_t attn_fwd_launch(AttnArgs a, bool bf16, bool vec, void* ws, hipStream_t stream) {
+  a.nsplit = splits(a);
+  a.part = (float*)ws;
+  if (bf16) {
+    if (a.D <= 64) return launch<uint16_t, 64, 64>(a, vec, stream);
+    if (a.D <= 128) return launch<uint16_t, 128, 64>(a, vec, stream);
+    return launch<uint16_t, 256, 64>(a, vec, stream);
+  }
+  if (a.D <= 64) return launch<float, 64, 64>(a, vec, stream);
+  if (a.D <= 128) return launch<float, 128, 64>(a, vec, stream);
+  return launch<float, 256, 32>(a, vec, stream);
+}
+
+}  // namespace opfuse

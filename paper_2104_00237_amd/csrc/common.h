@@ -442,4 +442,43 @@ size_t mse_ws_bytes(int64_t M, int64_t D);
 hipError_t launch_mse(const float* y, const float* t, int64_t M, int64_t D, int64_t ld,
                       float* loss, float* dy, void* ws, hipStream_t stream);
 
+
+// ------------------------------------------------------- rotary, attention
+constexpr int kRotMax = 512;       // turned elements of a head
+struct RotaryArgs {
+  const void* x;
+  void* y;
+  const int64_t* pos;              // NULL: pos0 + t % seq_len
+  int64_t T, seq_len, pos0, ldx, hsx, ldy, hsy;
+  int H, D, rot, interleaved, copy, rows;
+  float mscale, sign;              // factors of the cosines and the sines
+  double w[kRotMax / 2];           // turns per position of each pair
+};
+hipError_t rotary_launch(RotaryArgs a, bool bf16, hipStream_t stream);
+// A [T, H, D] tensor: element (t, h, d) is p[t * ld + h * hs + d].
+struct HeadRows {
+  void* p;
+  int64_t ld, hs;
+};
+
+struct AttnArgs {
+  HeadRows q, k, v, o, dout, dq, dk, dv;
+  float* lse;              // [Hq, Tq]
+  float* delta;            // [Hq, Tq], backward
+  float* part;             // partial sums of a split call
+  const int32_t *q_off, *k_off, *q_len, *k_len;
+  int64_t Tq, Tk;
+  int nseq, Hq, Hkv, G, D;
+  int causal, window;      // window 0: none
+  float scale, c;          // c = scale * log2(e)
+  FastDiv dG;
+  int nsplit;
+  int ovec;                // stores of 4 elements are aligned
+};
+// vec: 16-byte loads of Q, K, V (and dO) are aligned.
+size_t attn_fwd_ws_bytes(const AttnArgs& a);
+size_t attn_bwd_ws_bytes(const AttnArgs& a, bool bf16, bool grad_bf16);
+hipError_t attn_fwd_launch(AttnArgs a, bool bf16, bool vec, void* ws, hipStream_t stream);
+hipError_t attn_bwd_launch(AttnArgs a, bool bf16, bool grad_bf16, bool vec, void* ws, hipStream_t stream);
+
 }  // namespace opfuse

@@ -1145,4 +1145,225 @@ of_status of_mse_fwd_bwd(const float* y, const float* t, int64_t M, int64_t D, i
                     "of_mse_fwd_bwd launch");
 }
 
+namespace {
+// Layout of a [T, H, D] tensor: strides resolved, and no two elements at one place.
+of_status check_heads(const char* name, int64_t T, int64_t H, int64_t D, int64_t* ld, int64_t* hs) {
+  if (*hs == 0) *hs = D;
+  if (*ld == 0) *ld = H * D;
+  REQUIRE(*ld >= D && *hs >= D, OF_EINVAL, "%s: row stride %lld and head stride %lld must be 0 or >= D", name,
+          (long long)*ld, (long long)*hs);
+  REQUIRE(*ld <= (1LL << 22) && *hs <= (1LL << 40), OF_EUNSUPPORTED,
+          "%s: row stride must be <= 2^22 and head stride <= 2^40", name);
+  REQUIRE(*ld >= (H - 1) * *hs + D || *hs >= (T - 1) * *ld + D, OF_EINVAL,
+          "%s: rows overlap (row stride %lld, head stride %lld)", name, (long long)*ld, (long long)*hs);
+  return OF_OK;
+}
+
+bool aligned_to(const void* p, size_t n) { return ((uintptr_t)p) % n == 0; }
+
+of_status check_rotary(const of_rotary_desc* d, const void* x, const int64_t* pos, const void* y, bool inverse,
+                       RotaryArgs* a) {
+  REQUIRE(d != nullptr, OF_EINVAL, "desc is NULL");
+  REQUIRE(x && y, OF_EINVAL, "input and output are required");
+  REQUIRE(d->T >= 1 && d->H >= 1 && d->D >= 1, OF_EINVAL, "T, H and D must be >= 1");
+  REQUIRE(d->rot >= 2 && d->rot % 2 == 0 && d->rot <= d->D, OF_EINVAL, "rot %d must be even, >= 2 and <= D",
+          (int)d->rot);
+  REQUIRE(d->rot <= kRotMax, OF_EUNSUPPORTED, "rot must be <= %d", kRotMax);
+  REQUIRE(d->T < (1LL << 31) && (int64_t)d->H * d->D <= (1LL << 22), OF_EUNSUPPORTED,
+          "T must be < 2^31 and H * D <= 2^22");
+  REQUIRE(d->interleaved == 0 || d->interleaved == 1, OF_EINVAL, "interleaved must be 0 or 1");
+  REQUIRE(d->dtype == OF_F32 || d->dtype == OF_BF16, OF_EINVAL, "dtype %d is not an of_dtype", (int)d->dtype);
+  REQUIRE(d->seq_len >= 0 && d->pos0 >= 0, OF_EINVAL, "seq_len and pos0 must be >= 0");
+  REQUIRE(std::isfinite(d->base) && d->base > 1.0, OF_EINVAL, "base must be finite and > 1");
+  REQUIRE(d->scaling >= OF_ROPE_NONE && d->scaling <= OF_ROPE_BANDS, OF_EINVAL,
+          "scaling %d is not an of_rope_scaling", (int)d->scaling);
+  REQUIRE(d->scaling == OF_ROPE_NONE || (std::isfinite(d->factor) && d->factor > 0.0), OF_EINVAL,
+          "factor must be finite and > 0");
+  REQUIRE(d->scaling != OF_ROPE_BANDS || (std::isfinite(d->orig_len) && d->orig_len > 0.0 &&
+                                          std::isfinite(d->high_turns) && d->low_turns >= 0.0 &&
+                                          d->low_turns < d->high_turns),
+          OF_EINVAL, "OF_ROPE_BANDS needs orig_len > 0 and 0 <= low_turns < high_turns");
+  REQUIRE(std::isfinite(d->mscale) && d->mscale >= 0.f, OF_EINVAL, "mscale must be finite and >= 0");
+  const size_t es = d->dtype == OF_BF16 ? 2 : 4;
+  REQUIRE(aligned_to(x, es) && aligned_to(y, es), OF_EALIGN, "input and output must be %d-byte aligned", (int)es);
+  REQUIRE(aligned_to(pos, 8), OF_EALIGN, "pos must be 8-byte aligned");
+  // the forward reads the x layout and writes the y layout, the backward the other way round
+  a->ldx = inverse ? d->ldy : d->ldx;
+  a->hsx = inverse ? d->hsy : d->hsx;
+  a->ldy = inverse ? d->ldx : d->ldy;
+  a->hsy = inverse ? d->hsx : d->hsy;
+  of_status st = check_heads(inverse ? "dy" : "x", d->T, d->H, d->D, &a->ldx, &a->hsx);
+  if (st != OF_OK) return st;
+  if ((st = check_heads(inverse ? "dx" : "y", d->T, d->H, d->D, &a->ldy, &a->hsy)) != OF_OK) return st;
+  REQUIRE(x != y || (a->ldx == a->ldy && a->hsx == a->hsy), OF_EINVAL, "in place needs one layout for both sides");
+  a->x = x;
+  a->y = const_cast<void*>(y);
+  a->pos = pos;
+  a->T = d->T;
+  a->seq_len = d->seq_len ? d->seq_len : d->T;
+  a->pos0 = d->pos0;
+  a->H = d->H;
+  a->D = d->D;
+  a->rot = d->rot;
+  a->interleaved = d->interleaved;
+  a->copy = x != y;
+  a->mscale = d->mscale ? d->mscale : 1.f;
+  a->sign = inverse ? -a->mscale : a->mscale;
+  double base = d->base;
+  if (d->scaling == OF_ROPE_BASE && d->rot > 2) base *= std::pow(d->factor, d->rot / (d->rot - 2.0));
+  constexpr double kTurn = 6.283185307179586476925;
+  for (int i = 0; i < d->rot / 2; ++i) {
+    double w = std::pow(base, -2.0 * i / d->rot);
+    if (d->scaling == OF_ROPE_LINEAR) w /= d->factor;
+    if (d->scaling == OF_ROPE_BANDS) {
+      const double keep =
+          std::min(1.0, std::max(0.0, (d->orig_len * w / kTurn - d->low_turns) / (d->high_turns - d->low_turns)));
+      w = keep * w + (1.0 - keep) * w / d->factor;
+    }
+    a->w[i] = w / kTurn;
+  }
+  return OF_OK;
+}
+
+of_status rotary_entry(const of_rotary_desc* d, const void* x, const int64_t* pos, void* y, bool inverse,
+                       void* stream) {
+  RotaryArgs a;
+  memset(&a, 0, sizeof(a));
+  const of_status st = check_rotary(d, x, pos, y, inverse, &a);
+  if (st != OF_OK) return st;
+  return hip_status(rotary_launch(a, d->dtype == OF_BF16, (hipStream_t)stream),
+                    inverse ? "of_rotary_bwd launch" : "of_rotary_fwd launch");
+}
+
+// Checks a descriptor and fills everything but the pointers.
+of_status check_attn(const of_attn_desc* d, bool bwd, AttnArgs* a) {
+  REQUIRE(d != nullptr, OF_EINVAL, "desc is NULL");
+  REQUIRE(d->Tq >= 1 && d->Tk >= 1 && d->nseq >= 1, OF_EINVAL, "Tq, Tk and nseq must be >= 1");
+  REQUIRE(d->Hq >= 1 && d->Hkv >= 1 && d->D >= 1, OF_EINVAL, "Hq, Hkv and D must be >= 1");
+  REQUIRE(d->Hq % d->Hkv == 0, OF_EINVAL, "Hq (%d) must be a multiple of Hkv (%d)", (int)d->Hq, (int)d->Hkv);
+  REQUIRE(d->D <= 256, OF_EUNSUPPORTED, "D (%d) must be <= 256", (int)d->D);
+  REQUIRE(d->dtype == OF_F32 || d->dtype == OF_BF16, OF_EINVAL, "dtype %d is not an of_dtype", (int)d->dtype);
+  REQUIRE(d->grad_dtype == OF_F32 || d->grad_dtype == OF_BF16, OF_EINVAL, "grad_dtype %d is not an of_dtype",
+          (int)d->grad_dtype);
+  REQUIRE(!bwd || d->grad_dtype == OF_F32 || d->dtype == OF_BF16, OF_EUNSUPPORTED,
+          "bf16 gradients need bf16 operands");
+  REQUIRE(d->causal == 0 || d->causal == 1, OF_EINVAL, "causal must be 0 or 1");
+  REQUIRE(d->window >= 0, OF_EINVAL, "window must be >= 0 (0: none)");
+  REQUIRE(std::isfinite(d->scale) && d->scale >= 0.f, OF_EINVAL, "scale must be finite and >= 0 (0: 1 / sqrt(D))");
+  REQUIRE(d->Tq < (1LL << 31) && d->Tk < (1LL << 31) && d->Tq <= ((1LL << 31) - 1) / d->Hq, OF_EUNSUPPORTED,
+          "Tq * Hq and Tk must be < 2^31");
+  REQUIRE(d->nseq <= (1LL << 27) / d->Hq, OF_EUNSUPPORTED, "nseq * Hq must be <= 2^27");
+  REQUIRE(d->q_off || d->Tq % d->nseq == 0, OF_EINVAL, "without q_off, Tq must be a multiple of nseq");
+  REQUIRE(d->k_off || d->Tk % d->nseq == 0, OF_EINVAL, "without k_off, Tk must be a multiple of nseq");
+  REQUIRE(al4(d->q_off) && al4(d->k_off) && al4(d->q_len) && al4(d->k_len), OF_EALIGN,
+          "offsets and lengths must be 4-byte aligned");
+  memset(a, 0, sizeof(*a));
+  a->q.ld = d->ldq, a->q.hs = d->hsq;
+  a->k.ld = d->ldk, a->k.hs = d->hsk;
+  a->v.ld = d->ldv, a->v.hs = d->hsv;
+  a->o.ld = d->ldo, a->o.hs = d->hso;
+  of_status st;
+  if ((st = check_heads("q", d->Tq, d->Hq, d->D, &a->q.ld, &a->q.hs)) != OF_OK) return st;
+  if ((st = check_heads("k", d->Tk, d->Hkv, d->D, &a->k.ld, &a->k.hs)) != OF_OK) return st;
+  if ((st = check_heads("v", d->Tk, d->Hkv, d->D, &a->v.ld, &a->v.hs)) != OF_OK) return st;
+  if ((st = check_heads("o", d->Tq, d->Hq, d->D, &a->o.ld, &a->o.hs)) != OF_OK) return st;
+  a->q_off = d->q_off, a->k_off = d->k_off, a->q_len = d->q_len, a->k_len = d->k_len;
+  a->Tq = d->Tq, a->Tk = d->Tk;
+  a->nseq = (int)d->nseq;
+  a->Hq = d->Hq, a->Hkv = d->Hkv, a->G = d->Hq / d->Hkv, a->D = d->D;
+  a->causal = d->causal;
+  a->window = (int)std::min<int64_t>(d->window, 0x7fffffff);   // a wider one masks nothing that fits
+  a->scale = d->scale ? d->scale : (float)(1.0 / std::sqrt((double)d->D));
+  a->c = (float)((double)a->scale * 1.4426950408889634);
+  a->dG = make_fastdiv((uint32_t)a->G);
+  a->nsplit = 1;
+  return OF_OK;
+}
+
+// Whether 16-byte (n = 16 / es elements) or 4-element accesses of a tensor are aligned.
+bool heads_aligned(const HeadRows& x, int n, int es) {
+  return aligned_to(x.p, (size_t)n * es) && x.ld % n == 0 && x.hs % n == 0;
+}
+
+of_status check_attn_ws(size_t need, const void* ws, size_t ws_bytes) {
+  REQUIRE(ws_bytes >= need, OF_EWORKSPACE, "workspace of %zu bytes is smaller than the %zu needed", ws_bytes, need);
+  REQUIRE(need == 0 || ws != nullptr, OF_EWORKSPACE, "workspace is NULL");
+  REQUIRE(aligned_to(ws, 16), OF_EALIGN, "workspace must be 16-byte aligned");
+  return OF_OK;
+}
+}  // namespace
+
+of_status of_rotary_fwd(const of_rotary_desc* d, const void* x, const int64_t* pos, void* y, void* stream) {
+  return rotary_entry(d, x, pos, y, false, stream);
+}
+
+of_status of_rotary_bwd(const of_rotary_desc* d, const void* dy, const int64_t* pos, void* dx, void* stream) {
+  return rotary_entry(d, dy, pos, dx, true, stream);
+}
+
+size_t of_attn_workspace_size(const of_attn_desc* d, int32_t op) {
+  AttnArgs a;
+  if (op != OF_ATTN_FWD && op != OF_ATTN_BWD) {
+    fail(OF_EINVAL, "op %d is not an of_attn_op", (int)op);
+    return 0;
+  }
+  if (check_attn(d, op == OF_ATTN_BWD, &a) != OF_OK) return 0;
+  return op == OF_ATTN_FWD ? attn_fwd_ws_bytes(a)
+                           : attn_bwd_ws_bytes(a, d->dtype == OF_BF16, d->grad_dtype == OF_BF16);
+}
+
+of_status of_attn_fwd(const of_attn_desc* d, const void* q, const void* k, const void* v, void* o, float* lse,
+                      void* ws, size_t ws_bytes, void* stream) {
+  AttnArgs a;
+  of_status st = check_attn(d, false, &a);
+  if (st != OF_OK) return st;
+  REQUIRE(q && k && v && o, OF_EINVAL, "q, k, v and o are required");
+  const bool bf16 = d->dtype == OF_BF16;
+  const int es = bf16 ? 2 : 4;
+  REQUIRE(aligned_to(q, es) && aligned_to(k, es) && aligned_to(v, es) && aligned_to(o, es), OF_EALIGN,
+          "q, k, v and o must be %d-byte aligned", es);
+  REQUIRE(al4(lse), OF_EALIGN, "lse must be 4-byte aligned");
+  REQUIRE(o != q && o != k && o != v, OF_EINVAL, "o must not alias an input");
+  if ((st = check_attn_ws(attn_fwd_ws_bytes(a), ws, ws_bytes)) != OF_OK) return st;
+  a.q.p = const_cast<void*>(q), a.k.p = const_cast<void*>(k), a.v.p = const_cast<void*>(v), a.o.p = o;
+  a.lse = lse;
+  a.ovec = heads_aligned(a.o, 4, es);
+  const int n = 16 / es;
+  const bool vec = d->D % n == 0 && heads_aligned(a.q, n, es) && heads_aligned(a.k, n, es) && heads_aligned(a.v, n, es);
+  return hip_status(attn_fwd_launch(a, bf16, vec, ws, (hipStream_t)stream), "of_attn_fwd launch");
+}
+
+of_status of_attn_bwd(const of_attn_desc* d, const void* q, const void* k, const void* v, const void* o,
+                      const float* lse, const void* dout, void* dq, void* dk, void* dv, void* ws, size_t ws_bytes,
+                      void* stream) {
+  AttnArgs a;
+  of_status st = check_attn(d, true, &a);
+  if (st != OF_OK) return st;
+  REQUIRE(q && k && v && o && lse && dout && dq && dk && dv, OF_EINVAL,
+          "q, k, v, o, lse, dout, dq, dk and dv are required");
+  const bool bf16 = d->dtype == OF_BF16, gbf = d->grad_dtype == OF_BF16;
+  const int es = bf16 ? 2 : 4, gs = gbf ? 2 : 4;
+  REQUIRE(aligned_to(q, es) && aligned_to(k, es) && aligned_to(v, es) && aligned_to(o, es), OF_EALIGN,
+          "q, k, v and o must be %d-byte aligned", es);
+  REQUIRE(aligned_to(dout, gs) && aligned_to(dq, gs) && aligned_to(dk, gs) && aligned_to(dv, gs), OF_EALIGN,
+          "dout, dq, dk and dv must be %d-byte aligned", gs);
+  REQUIRE(al4(lse), OF_EALIGN, "lse must be 4-byte aligned");
+  const void* in[5] = {q, k, v, o, dout};
+  for (const void* p : in)
+    REQUIRE(dq != p && dk != p && dv != p, OF_EINVAL, "dq, dk and dv must not alias an input");
+  REQUIRE(dq != dk && dk != dv && dq != dv, OF_EINVAL, "dq, dk and dv must be different buffers");
+  if ((st = check_attn_ws(attn_bwd_ws_bytes(a, bf16, gbf), ws, ws_bytes)) != OF_OK) return st;
+  a.q.p = const_cast<void*>(q), a.k.p = const_cast<void*>(k), a.v.p = const_cast<void*>(v);
+  a.dq = HeadRows{dq, a.q.ld, a.q.hs}, a.dk = HeadRows{dk, a.k.ld, a.k.hs}, a.dv = HeadRows{dv, a.v.ld, a.v.hs};
+  a.dout = HeadRows{const_cast<void*>(dout), a.o.ld, a.o.hs};
+  a.o.p = const_cast<void*>(o);
+  a.lse = const_cast<float*>(lse);
+  a.ovec = heads_aligned(a.dq, 4, gs) && heads_aligned(a.dk, 4, gs) && heads_aligned(a.dv, 4, gs);
+  const int n = 16 / es;
+  // (dO stored in another type than the operands' is copied to the workspace, where it is aligned)
+  const bool vec = d->D % n == 0 && heads_aligned(a.q, n, es) && heads_aligned(a.k, n, es) &&
+                   heads_aligned(a.v, n, es) && (bf16 != gbf || heads_aligned(a.dout, n, es));
+  return hip_status(attn_bwd_launch(a, bf16, gbf, vec, ws, (hipStream_t)stream), "of_attn_bwd launch");
+}
+
 }  // extern "C"
