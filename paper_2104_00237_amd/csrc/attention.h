@@ -10,6 +10,9 @@
 //     read in the registers' order and the probabilities never go through LDS.
 #pragma once
 
+#include <type_traits>
+#include <utility>
+
 #include "attention_seq.h"
 #include "gemm_common.h"
 
@@ -113,41 +116,76 @@ __device__ __forceinline__ typename Mma<T>::frag row_frag(const char* t, int x0,
   return *reinterpret_cast<const typename Mma<T>::frag*>(t + x * (SLOTS * 16) + (((2 * s + (lane >> 5)) ^ swz<SLOTS>(x)) << 4));
 }
 
-// Rows row0 .. row0 + n - 1 (n <= ROWS) of one head into a tile; the rest of the tile is zero, and so
-// are columns from D on.  NT threads.  VEC: 16-byte loads (pointer and strides are multiples of 16
-// bytes and D of a slot), else element by element.
+// 16 bytes a lane from memory to LDS, lane i to `lds` + 16 i.  (A function of its own, no template: in
+// the host pass the builtin has no 16-byte form, and a template that calls it is given up silently,
+// with the kernels that use it.)
+__device__ __forceinline__ void load_lds16(rsrc_t rs, char* lds, uint32_t off) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (__attribute__((address_space(3))) void*)lds, 16, off, 0, 0, 0);
+}
+
+// Loads of a tile's rows: rows row0 .. row0 + n - 1 (n <= ROWS) of one head; the rest of the tile is
+// zero, and so are columns from D on.  NT threads.
+// VEC (pointer and strides are multiples of 16 bytes and D of a slot): memory to LDS, 16 bytes a lane
+// and no registers.  A wavefront's load writes 1 KB in lane order, so the swizzle is applied to the
+// address a lane loads from; the offsets are the same for every tile.  Else element by element.
 template <typename T, int SLOTS, int ROWS, int NT, bool VEC>
-__device__ __forceinline__ void load_tile(char* tile, const HeadRows& x, int64_t row0, int head, int n, int D, int tid) {
-  constexpr int E = Mma<T>::E, ES = sizeof(T);
-  n = max(n, 0);
-  const rsrc_t rs = make_rsrc((const T*)x.p + (n ? row0 * x.ld + head * x.hs : 0), n ? (int)(((n - 1) * x.ld + D) * ES) : 0);
-  constexpr int PER = ROWS * SLOTS / NT;
+struct TileLoad {
+  static constexpr int E = Mma<T>::E, ES = sizeof(T), PER = ROWS * SLOTS / NT;
   static_assert(PER * NT == ROWS * SLOTS, "whole slots per thread");
-  au32x4_t v[PER];
+  // the swizzle repeats every 16 rows: load i is load i % OFFS, some whole 16 rows further
+  static constexpr int OFFS = PER < 16 * SLOTS / NT ? PER : 16 * SLOTS / NT > 0 ? 16 * SLOTS / NT : 1;
+  static constexpr int FURTHER = OFFS * NT / SLOTS;   // rows
+  uint32_t off[OFFS];
+  uint32_t step;
+
+  __device__ __forceinline__ TileLoad(const HeadRows& x, int D, int tid) {
+    step = (uint32_t)(x.ld * FURTHER * ES);
 #pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const int id = tid + i * NT, r = id / SLOTS, s = id % SLOTS;
-    const uint32_t at = (uint32_t)(r * x.ld * ES) + s * 16;
-    if constexpr (VEC) {
-      v[i] = __builtin_bit_cast(au32x4_t, __builtin_amdgcn_raw_buffer_load_b128(rs, r < n && s * E < D ? at : kOOB, 0, 0));
-    } else if constexpr (ES == 4) {
-#pragma unroll
-      for (int e = 0; e < E; ++e)
-        v[i][e] = __builtin_amdgcn_raw_buffer_load_b32(rs, r < n && s * E + e < D ? at + 4 * e : kOOB, 0, 0);
-    } else {
-#pragma unroll
-      for (int e = 0; e < E; e += 2) {
-        const uint32_t lo = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rs, r < n && s * E + e < D ? at + 2 * e : kOOB, 0, 0);
-        const uint32_t hi = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rs, r < n && s * E + e + 1 < D ? at + 2 * e + 2 : kOOB, 0, 0);
-        v[i][e / 2] = lo | hi << 16;
-      }
+    for (int i = 0; i < OFFS; ++i) {
+      const int id = tid + i * NT, r = id / SLOTS, s = (id % SLOTS) ^ swz<SLOTS>(r);
+      off[i] = s * E < D ? (uint32_t)(r * x.ld * ES) + s * 16 : kOOB;
     }
   }
+  __device__ __forceinline__ void operator()(char* tile, const HeadRows& x, int64_t row0, int head, int n, int D, int tid) const {
+    n = min(n, ROWS);   // none: an empty buffer, all zeros
+    // (rows from n on lie beyond the buffer's end: ld >= D.  The end is checked against the vector
+    // offset, so the whole offset is in it.)
+    const rsrc_t rs = make_rsrc((const T*)x.p + row0 * x.ld + head * x.hs, n > 0 ? (int)(((n - 1) * x.ld + D) * ES) : 0);
+    if constexpr (VEC) {
+      const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
 #pragma unroll
-  for (int i = 0; i < PER; ++i) {
-    const int id = tid + i * NT, r = id / SLOTS, s = id % SLOTS;
-    *reinterpret_cast<au32x4_t*>(tile + r * (SLOTS * 16) + ((s ^ swz<SLOTS>(r)) << 4)) = v[i];
+      for (int i = 0; i < PER; ++i)
+        load_lds16(rs, tile + (wave * 64 + i * NT) * 16, off[i % OFFS] + (i / OFFS) * step);
+    } else {
+      au32x4_t v[PER];
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        const int id = tid + i * NT, r = id / SLOTS, d = ((id % SLOTS) ^ swz<SLOTS>(r)) * E;
+        const uint32_t at = off[i % OFFS] + (i / OFFS) * step;
+        if constexpr (ES == 4) {
+#pragma unroll
+          for (int e = 0; e < E; ++e)
+            v[i][e] = __builtin_amdgcn_raw_buffer_load_b32(rs, d + e < D ? at + 4 * e : kOOB, 0, 0);
+        } else {
+#pragma unroll
+          for (int e = 0; e < E; e += 2) {
+            const uint32_t lo = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rs, d + e < D ? at + 2 * e : kOOB, 0, 0);
+            const uint32_t hi = (uint16_t)__builtin_amdgcn_raw_buffer_load_b16(rs, d + e + 1 < D ? at + 2 * e + 2 : kOOB, 0, 0);
+            v[i][e / 2] = lo | hi << 16;
+          }
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < PER; ++i) *reinterpret_cast<au32x4_t*>(tile + (tid + i * NT) * 16) = v[i];
+    }
   }
+};
+
+// This wavefront's loads to LDS and LDS accesses are done, then everyone's.
+__device__ __forceinline__ void tile_barrier() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
 }
 
 // The lane's own row as B fragments: 16 bytes at slot 2 s + h for every step s.
@@ -191,6 +229,16 @@ __device__ __forceinline__ void store_own(T* row, const acc16_t (&acc)[NB], floa
           if (d + j < D) row[d + j] = Mma<T>::from(e[j]);
       }
     }
+}
+
+// f(0) .. f(N - 1) with constants: registers are indexed statically.
+template <int... I, class F>
+__device__ __forceinline__ void each_of(std::integer_sequence<int, I...>, F&& f) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, class F>
+__device__ __forceinline__ void each(F&& f) {
+  each_of(std::make_integer_sequence<int, N>{}, f);
 }
 
 template <int N>

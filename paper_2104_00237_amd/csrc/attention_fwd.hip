@@ -13,10 +13,11 @@ constexpr int BM = 32 * NW;         // rows: (query, head of the group) pairs, 3
 // Rows r of a key head's group: query r / G, head r % G, so that the query heads that share a key
 // head share its tiles.  BN: keys of a tile.
 template <typename T, int DP, int BN, bool VEC>
-__global__ __launch_bounds__(256) void attn_fwd_kernel(AttnArgs a) {
+__global__ __launch_bounds__(256, sizeof(T) == 2 && DP <= 128 ? 2 : 1) void attn_fwd_kernel(AttnArgs a) {
   constexpr int ES = sizeof(T), SLOTS = DP * ES / 16, NS = SLOTS / 2, NB = DP / 32, NK = BN / 32;
   typedef typename Mma<T>::frag frag;
-  __shared__ __attribute__((aligned(1024))) char sk[BN * SLOTS * 16], sv[BN * SLOTS * 16];
+  constexpr int TB = BN * SLOTS * 16;
+  __shared__ __attribute__((aligned(1024))) char sk0[TB], sk1[TB], sv0[TB], sv1[TB];
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   int64_t w = blockIdx.x;
@@ -55,12 +56,17 @@ __global__ __launch_bounds__(256) void attn_fwd_kernel(AttnArgs a) {
   zero_acc(acc);
   float m = -INFINITY, l = 0.f;
 
-  for (int t = t0; t < t1; ++t) {
+  const TileLoad<T, SLOTS, BN, 256, VEC> lk(a.k, a.D, tid), lv(a.v, a.D, tid);
+  auto request = [&](char* k, char* v, int t) {
+    lk(k, a.k, kv.beg + t * BN, hk, kv.len - t * BN, a.D, tid);
+    lv(v, a.v, kv.beg + t * BN, hk, kv.len - t * BN, a.D, tid);
+  };
+  // One barrier a tile: tile t has landed and tile t - 1 has been read, so tile t + 1 is requested
+  // into its place and has the time of tile t's products to arrive.
+  auto step = [&](const char* sk, const char* sv, char* kn, char* vn, int t) {
     const int j0 = t * BN;
-    __syncthreads();
-    load_tile<T, SLOTS, BN, 256, VEC>(sk, a.k, kv.beg + j0, hk, min(BN, kv.len - j0), a.D, tid);
-    load_tile<T, SLOTS, BN, 256, VEC>(sv, a.v, kv.beg + j0, hk, min(BN, kv.len - j0), a.D, tid);
-    __syncthreads();
+    tile_barrier();
+    if (t + 1 < t1) request(kn, vn, t + 1);
     acc16_t z[NK];
     zero_acc(z);
 #pragma unroll
@@ -108,6 +114,11 @@ __global__ __launch_bounds__(256) void attn_fwd_kernel(AttnArgs a) {
         for (int b = 0; b < NB; ++b)
           acc[b] = Mma<T>::mma(Mma<T>::template tr<SLOTS>(sv, n * 32 + u * Mma<T>::TR, b * 32, lane), p, acc[b]);
       }
+  };
+  if (t0 < t1) request(sk0, sv0, t0);
+  for (int t = t0; t < t1; t += 2) {
+    step(sk0, sv0, sk1, sv1, t);
+    if (t + 1 < t1) step(sk1, sv1, sk0, sv0, t + 1);
   }
   l += other_half(l);
   if (!has) return;
@@ -195,7 +206,7 @@ hipError_t attn_fwd_launch(AttnArgs a, bool bf16, bool vec, void* ws, hipStream_
     return launch<uint16_t, 256, 64>(a, vec, stream);
   }
   if (a.D <= 64) return launch<float, 64, 64>(a, vec, stream);
-  if (a.D <= 128) return launch<float, 128, 64>(a, vec, stream);
+  if (a.D <= 128) return launch<float, 128, 32>(a, vec, stream);
   return launch<float, 256, 32>(a, vec, stream);
 }
 

@@ -470,7 +470,7 @@ struct AttnArgs {
   int64_t Tq, Tk;
   int nseq, Hq, Hkv, G, D;
   int causal, window;      // window 0: none
-  float scale, c;          // c = scale * log2(e)
+  float scale, c, rc;      // c = scale * log2(e), rc = 1 / c
   FastDiv dG;
   int nsplit;
   int ovec;                // stores of 4 elements are aligned

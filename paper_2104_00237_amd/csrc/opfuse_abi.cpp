@@ -1275,6 +1275,7 @@ of_status check_attn(const of_attn_desc* d, bool bwd, AttnArgs* a) {
   a->window = (int)std::min<int64_t>(d->window, 0x7fffffff);   // a wider one masks nothing that fits
   a->scale = d->scale ? d->scale : (float)(1.0 / std::sqrt((double)d->D));
   a->c = (float)((double)a->scale * 1.4426950408889634);
+  a->rc = (float)(1.0 / ((double)a->scale * 1.4426950408889634));
   a->dG = make_fastdiv((uint32_t)a->G);
   a->nsplit = 1;
   return OF_OK;
