@@ -31,10 +31,16 @@ constexpr float kLog2e = 1.44269504088896340736f;
 constexpr float kLn2 = 0.69314718055994530942f;
 
 // ------------------------------------------------------------------- tiles
-// A tile in LDS: rows of DP elements (DP * sizeof(T) bytes, 16-byte slots), slot s of row x at slot
+// A tile in LDS: rows of 16-byte slots (a power of two of them), slot s of row x at slot
 // s ^ swz(x).  Rows are read as fragments (16 bytes of 32 rows at one slot: 16 consecutive rows take
 // all 64 banks) and transposed (four consecutive rows of one 64-byte block, again all banks), so the
 // two low bits of x go to the block bits of the slot and the next two below them.
+// 16-byte slots of a row of `bytes` (a power of two, at least 8).
+constexpr int slots_of(int bytes) {
+  int s = 8;
+  while (s * 16 < bytes) s *= 2;
+  return s;
+}
 template <int SLOTS>
 __device__ __forceinline__ int swz(int x) {
   if constexpr (SLOTS == 8) return (((x >> 1) & 1) << 2) | ((x >> 2) & 3);   // two rows take the banks
@@ -249,8 +255,19 @@ __device__ __forceinline__ void zero_acc(acc16_t (&a)[N]) {
     for (int k = 0; k < 16; ++k) a[i][k] = 0.f;
 }
 
-// The other lane half's value of the same column.
-__device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
+// f of a lane's value and the other half's of the same column.
+template <class F>
+__device__ __forceinline__ float with_half(float x, F&& f) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float half_sum(float x) {
+  return with_half(x, [](float a, float b) { return a + b; });
+}
+
+// v_maximum3_f32: a NaN stays (fmaxf would drop it, and takes an instruction more for each operand
+// to make it canonical first)
+__device__ __forceinline__ float maxi(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
 

@@ -62,7 +62,7 @@ __device__ __forceinline__ float dot_own(const afloatx4_t (&a)[NS], const afloat
 // to T when it is stored in another type, [Tq, Hq, D].
 template <typename T, typename G, int DP, int BN, int RD, bool VEC>
 __global__ __launch_bounds__(256, sizeof(T) == 2 && DP <= 128 ? 2 : 1) void attn_dq_kernel(AttnArgs a, T* copy) {
-  constexpr int ES = sizeof(T), SLOTS = DP * ES / 16, NS = SLOTS / 2, NB = DP / 32, NK = BN / 32, U = 32 / Mma<T>::TR;
+  constexpr int ES = sizeof(T), SLOTS = slots_of(DP * ES), NS = DP * ES / 32, NB = DP / 32, NK = BN / 32, U = 32 / Mma<T>::TR;
   constexpr bool INIT = ES == 2;   // S starts from -lse / scale
   typedef typename Mma<T>::frag frag;
   constexpr int TB = BN * SLOTS * 16;
@@ -71,7 +71,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && DP <= 128 ? 2 : 1) void attn
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   int64_t w = blockIdx.x;
   const int hk = (int)(w % a.Hkv);
-  w /= a.Hkv;
+  w = paired(w / a.Hkv, gridDim.x / a.Hkv, 256 / a.Hkv);
   int s;
   int64_t tile;
   find_tile(a.q_off, a.Tq, a.nseq, a.G, BM, w, s, tile);
@@ -102,8 +102,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && DP <= 128 ? 2 : 1) void attn
   else
     round_own(fo, (const G*)a.dout.p + row * a.dout.ld + (int64_t)h * a.dout.hs, copy + (row * a.Hq + h) * a.D, has, a.D, lane);
   load_own<T, NS, VEC>(fq, (const T*)a.o.p + row * a.o.ld + (int64_t)h * a.o.hs, has, a.D, lane);
-  delta = dot_own(fq, fo);
-  delta += other_half(delta);
+  delta = half_sum(dot_own(fq, fo));
   load_own<T, NS, VEC>(fq, (const T*)a.q.p + row * a.q.ld + (int64_t)h * a.q.hs, has, a.D, lane);
   // a row that saw no key (lse -inf) or does not exist has no probabilities: exp2(s - inf) = 0
   const float lse = a.lse[stat], lse2 = has && lse > -INFINITY ? lse * kLog2e : INFINITY;
@@ -188,7 +187,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && DP <= 128 ? 2 : 1) void attn
     // here (O of n keys is about V / sqrt(n), so the error falls as 1 / sqrt(n) against dP).
     if (t1 - t0 <= kExactKeys / BN) {
       walk(std::true_type{});
-      delta += more + other_half(more);
+      delta += half_sum(more);
       tile_barrier();    // the last tile has been read
     }
   }
@@ -208,7 +207,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && DP <= 128 ? 2 : 1) void attn
 // compiler spills (2.7 times the time), and with 64 own keys it shuffles sums between register files.
 template <typename T, typename G, int DP, int DO, int BQ, int RD, int OCC, bool VEC>
 __global__ __launch_bounds__(256, OCC) void attn_dkv_kernel(AttnArgs a) {
-  constexpr int ES = sizeof(T), SLOTS = DP * ES / 16, NS = SLOTS / 2, NB = DO / 32, U = 32 / Mma<T>::TR;
+  constexpr int ES = sizeof(T), SLOTS = slots_of(DP * ES), NS = DP * ES / 32, NB = DO / 32, U = 32 / Mma<T>::TR;
   constexpr int TB = BQ * SLOTS * 16;
   constexpr bool INIT = ES == 2;   // S starts from -lse / scale
   typedef typename Mma<T>::frag frag;
@@ -221,8 +220,9 @@ __global__ __launch_bounds__(256, OCC) void attn_dkv_kernel(AttnArgs a) {
   w /= a.Hkv;
   const int split = (int)(w % a.nsplit);
   w /= a.nsplit;
+  static_assert(DP % DO == 0, "whole parts");
   const int d0 = (int)(w % (DP / DO)) * DO;   // first column of dK and dV
-  w /= DP / DO;
+  w = paired(w / (DP / DO), gridDim.x / (a.Hkv * a.nsplit * (DP / DO)), 256 / (a.Hkv * a.nsplit * (DP / DO)));
   if (d0 >= a.D) return;
   int s;
   int64_t tile;
@@ -392,7 +392,7 @@ namespace {
 // us unsplit, in 2 parts 658 + 18 us for their sum, in 4 parts 675 + 26, in 8 706 + 61.
 // 4 x 1024 tokens, 16 heads of 64 (512 workgroups): unsplit 42, in 2 parts 42 + 18.
 int bwd_splits(const AttnArgs& a, bool bf16) {
-  const int parts = a.D <= 128 ? 1 : bf16 ? 2 : 4, queries = bf16 && a.D <= 128 ? 64 : 32;
+  const int parts = a.D <= 128 ? 1 : bf16 ? 2 : (a.D + 63) / 64, queries = bf16 && a.D <= 128 ? 64 : 32;
   const int64_t wgs = attn_tiles(a.Tk, a.nseq, a.k_off != nullptr, 1, BK) * a.Hkv * parts;
   const int64_t rows = std::min<int64_t>(a.Tq / a.nseq, a.window ? 2 * (int64_t)a.window + 128 : a.Tq);
   const int64_t tiles = rows * a.G / queries;
@@ -405,7 +405,7 @@ size_t stat_bytes(const AttnArgs& a) { return (((size_t)a.Hq * a.Tq + 3) & ~(siz
 size_t copy_bytes(const AttnArgs& a) { return ((size_t)a.Hq * a.Tq * a.D * 2 + 15) & ~(size_t)15; }
 
 template <typename T, typename G, int DP, int DO, int BQ, int RD, int OCC, int BN, bool VEC>
-hipError_t launch_vec(AttnArgs a, T* copy, hipStream_t stream) {
+hipError_t launch_as(AttnArgs a, T* copy, hipStream_t stream) {
   const int64_t nq = attn_tiles(a.Tq, a.nseq, a.q_off != nullptr, a.G, BM) * a.Hkv;
   hipLaunchKernelGGL((attn_dq_kernel<T, G, DP, BN, sizeof(T) == 2 && DP == 64 ? 2 : 1, VEC>), dim3((unsigned)nq), dim3(256), 0, stream, a, copy);
   hipError_t e = hipGetLastError();
@@ -419,12 +419,6 @@ hipError_t launch_vec(AttnArgs a, T* copy, hipStream_t stream) {
   hipLaunchKernelGGL((attn_sum_kernel<G>), dim3((unsigned)ns), dim3(256), 0, stream, a);
   return hipGetLastError();
 }
-template <typename T, typename G, int DP, int DO, int BQ, int RD, int OCC, int BN>
-hipError_t launch_any(const AttnArgs& a, bool vec, T* copy, hipStream_t stream) {
-  return vec ? launch_vec<T, G, DP, DO, BQ, RD, OCC, BN, true>(a, copy, stream)
-             : launch_vec<T, G, DP, DO, BQ, RD, OCC, BN, false>(a, copy, stream);
-}
-
 template <typename T, typename G>
 hipError_t launch(AttnArgs a, bool vec, void* ws, hipStream_t stream) {
   constexpr bool conv = sizeof(T) != sizeof(G);
@@ -432,14 +426,29 @@ hipError_t launch(AttnArgs a, bool vec, void* ws, hipStream_t stream) {
   T* copy = conv ? (T*)((char*)ws + stat_bytes(a)) : nullptr;
   a.nsplit = bwd_splits(a, sizeof(T) == 2);
   a.part = (float*)((char*)ws + stat_bytes(a) + (conv ? copy_bytes(a) : 0));
+  // widths between the powers of two have their own products where the loads are whole slots
   if constexpr (sizeof(T) == 2) {
-    if (a.D <= 64) return launch_any<T, G, 64, 64, 64, 2, 2, 64>(a, vec, copy, stream);
-    if (a.D <= 128) return launch_any<T, G, 128, 128, 64, 3, 1, 64>(a, vec, copy, stream);
-    return launch_any<T, G, 256, 128, 32, 2, 1, 32>(a, vec, copy, stream);
+    if (!vec) {
+      if (a.D <= 64) return launch_as<T, G, 64, 64, 64, 2, 2, 64, false>(a, copy, stream);
+      if (a.D <= 128) return launch_as<T, G, 128, 128, 64, 3, 1, 64, false>(a, copy, stream);
+      return launch_as<T, G, 256, 128, 32, 2, 1, 32, false>(a, copy, stream);
+    }
+    if (a.D <= 64) return launch_as<T, G, 64, 64, 64, 2, 2, 64, true>(a, copy, stream);
+    if (a.D <= 96) return launch_as<T, G, 96, 96, 64, 3, 1, 64, true>(a, copy, stream);
+    if (a.D <= 128) return launch_as<T, G, 128, 128, 64, 3, 1, 64, true>(a, copy, stream);
+    if (a.D <= 192) return launch_as<T, G, 192, 96, 32, 2, 1, 32, true>(a, copy, stream);
+    return launch_as<T, G, 256, 128, 32, 2, 1, 32, true>(a, copy, stream);
   } else {
-    if (a.D <= 64) return launch_any<T, G, 64, 64, 32, 2, 1, 32>(a, vec, copy, stream);
-    if (a.D <= 128) return launch_any<T, G, 128, 128, 32, 1, 1, 32>(a, vec, copy, stream);
-    return launch_any<T, G, 256, 64, 32, 1, 1, 32>(a, vec, copy, stream);
+    if (!vec) {
+      if (a.D <= 64) return launch_as<T, G, 64, 64, 32, 2, 1, 32, false>(a, copy, stream);
+      if (a.D <= 128) return launch_as<T, G, 128, 128, 32, 1, 1, 32, false>(a, copy, stream);
+      return launch_as<T, G, 256, 64, 32, 1, 1, 32, false>(a, copy, stream);
+    }
+    if (a.D <= 64) return launch_as<T, G, 64, 64, 32, 2, 1, 32, true>(a, copy, stream);
+    if (a.D <= 96) return launch_as<T, G, 96, 96, 32, 2, 1, 32, true>(a, copy, stream);
+    if (a.D <= 128) return launch_as<T, G, 128, 128, 32, 1, 1, 32, true>(a, copy, stream);
+    if (a.D <= 192) return launch_as<T, G, 192, 64, 32, 1, 1, 32, true>(a, copy, stream);
+    return launch_as<T, G, 256, 64, 32, 1, 1, 32, true>(a, copy, stream);
   }
 }
 }  // namespace

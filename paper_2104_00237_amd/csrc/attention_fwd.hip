@@ -14,7 +14,7 @@ constexpr int BM = 32 * NW;         // rows: (query, head of the group) pairs, 3
 // head share its tiles.  BN: keys of a tile.
 template <typename T, int DP, int BN, bool VEC>
 __global__ __launch_bounds__(256, sizeof(T) == 2 && DP <= 128 ? 2 : 1) void attn_fwd_kernel(AttnArgs a) {
-  constexpr int ES = sizeof(T), SLOTS = DP * ES / 16, NS = SLOTS / 2, NB = DP / 32, NK = BN / 32;
+  constexpr int ES = sizeof(T), SLOTS = slots_of(DP * ES), NS = DP * ES / 32, NB = DP / 32, NK = BN / 32;
   typedef typename Mma<T>::frag frag;
   constexpr int TB = BN * SLOTS * 16;
   __shared__ __attribute__((aligned(1024))) char sk0[TB], sk1[TB], sv0[TB], sv1[TB];
@@ -24,7 +24,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && DP <= 128 ? 2 : 1) void attn
   const int hk = (int)(w % a.Hkv);
   w /= a.Hkv;
   const int split = (int)(w % a.nsplit);
-  w /= a.nsplit;
+  w = paired(w / a.nsplit, gridDim.x / (a.Hkv * a.nsplit), 256 / (a.Hkv * a.nsplit));
   int s;
   int64_t tile;
   find_tile(a.q_off, a.Tq, a.nseq, a.G, BM, w, s, tile);
@@ -54,7 +54,8 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && DP <= 128 ? 2 : 1) void attn
   load_own<T, NS, VEC>(fq, (const T*)a.q.p + (q.beg + i) * a.q.ld + (int64_t)h * a.q.hs, has, a.D, lane);
   acc16_t acc[NB];
   zero_acc(acc);
-  float m = -INFINITY, l = 0.f;
+  float m = -INFINITY, ms = 0.f, l = 0.f;
+  constexpr float GROW = 8.f;
 
   const TileLoad<T, SLOTS, BN, 256, VEC> lk(a.k, a.D, tid), lv(a.v, a.D, tid);
   auto request = [&](char* k, char* v, int t) {
@@ -86,25 +87,30 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && DP <= 128 ? 2 : 1) void attn
 #pragma unroll
     for (int n = 0; n < NK; ++n)
 #pragma unroll
-      for (int k = 0; k < 16; ++k) top = fmaxf(top, z[n][k]);
-    top = fmaxf(top, other_half(top)) * a.c;
-    const float mn = fmaxf(m, top);
-    const float ms = mn == -INFINITY ? 0.f : mn;      // no key so far: exp2(-inf - 0) = 0
-    const float f = exp2_fast(m - ms);
-    m = mn;
-    float sum = 0.f;
+      for (int k = n == 0; k < 16; ++k) top = maxi(top, z[n][k]);
+    top = with_half(top, maxi) * a.c;
+    // m is raised only where the maximum has grown by more than 2^GROW: P up to 2^GROW is as exact, and
+    // most tiles then have no sums to scale
+    if (__any(top > m + GROW)) {
+      const float mn = maxi(m, top);
+      ms = mn == -INFINITY ? 0.f : mn;      // no key so far: exp2(-inf - 0) = 0
+      const float f = exp2_fast(m - ms);
+      m = mn;
+      l *= f;
+#pragma unroll
+      for (int b = 0; b < NB; ++b)
+#pragma unroll
+        for (int k = 0; k < 16; ++k) acc[b][k] *= f;
+    }
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int n = 0; n < NK; ++n)
 #pragma unroll
       for (int k = 0; k < 16; ++k) {
         z[n][k] = exp2_fast(__fmaf_rn(z[n][k], a.c, -ms));
-        sum += z[n][k];
+        sum[k & 3] += z[n][k];
       }
-    l = l * f + sum;
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-      for (int k = 0; k < 16; ++k) acc[b][k] *= f;
+    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
 #pragma unroll
     for (int n = 0; n < NK; ++n)
 #pragma unroll
@@ -120,7 +126,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && DP <= 128 ? 2 : 1) void attn
     step(sk0, sv0, sk1, sv1, t);
     if (t + 1 < t1) step(sk1, sv1, sk0, sv0, t + 1);
   }
-  l += other_half(l);
+  l = half_sum(l);
   if (!has) return;
   const int64_t stat = (int64_t)h * a.Tq + q.beg + i;
   if (a.nsplit > 1) {      // this split's sums; attn_join_kernel puts them together
@@ -134,18 +140,19 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && DP <= 128 ? 2 : 1) void attn
     }
     return;
   }
-  store_own((T*)a.o.p + (q.beg + i) * a.o.ld + (int64_t)h * a.o.hs, acc, l > 0.f ? 1.f / l : l == 0.f ? 0.f : l, a.D, a.ovec, lane);
+  store_own((T*)a.o.p + (q.beg + i) * a.o.ld + (int64_t)h * a.o.hs, acc, l == 0.f ? 0.f : 1.f / l, a.D, a.ovec, lane);
   if (a.lse && half == 0) a.lse[stat] = l == 0.f ? -INFINITY : __fmaf_rn(m, kLn2, logf(l));
 }
 
-// Joins the splits of a row: O = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s.  A wavefront a row.
+// Joins the splits of a row: O = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s.  A wavefront a row: its
+// lanes hold the splits' statistics (at most 64), then columns; the splits' loads do not wait for
+// each other (8 sequences of one token, 16 splits: 17 -> 5 us).
 template <typename T>
 __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
   const int lane = threadIdx.x & 63;
-  const int64_t w = blockIdx.x;
   int s;
   int64_t tile;
-  find_tile(a.q_off, a.Tq, a.nseq, a.Hq, 4, w, s, tile);
+  find_tile(a.q_off, a.Tq, a.nseq, a.Hq, 4, blockIdx.x, s, tile);
   const SeqRows q = seq_rows(a.q_off, a.q_len, a.Tq, a.nseq, s);
   const int64_t r = tile * 4 + (threadIdx.x >> 6);
   if (tile < 0 || r >= (int64_t)q.len * a.Hq) return;
@@ -153,38 +160,55 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
   const int h = (int)(r - i * a.Hq);
   const int64_t rows = (int64_t)a.Hq * a.Tq, stat = h * a.Tq + q.beg + i;
   const float* st = a.part + a.nsplit * rows * a.D + stat * 2;
-  float m = -INFINITY, l = 0.f;
-  for (int k = 0; k < a.nsplit; ++k) m = fmaxf(m, st[k * rows * 2]);
-  const float ms = m == -INFINITY ? 0.f : m;
-  for (int k = 0; k < a.nsplit; ++k) l += exp2_fast(st[k * rows * 2] - ms) * st[k * rows * 2 + 1];
-  const float inv = l > 0.f ? 1.f / l : l == 0.f ? 0.f : l;
+  const float mine = lane < a.nsplit ? st[lane * rows * 2] : -INFINITY;
+  const float sum = lane < a.nsplit ? st[lane * rows * 2 + 1] : 0.f;
+  float m = mine;
+#pragma unroll
+  for (int k = 32; k > 0; k >>= 1) m = maxi(m, __shfl_xor(m, k));
+  const float f = exp2_fast(mine - (m == -INFINITY ? 0.f : m));   // a split that saw no key: 0
+  float l = f * sum;
+#pragma unroll
+  for (int k = 32; k > 0; k >>= 1) l += __shfl_xor(l, k);
+  const float inv = l == 0.f ? 0.f : 1.f / l;
   T* o = (T*)a.o.p + (q.beg + i) * a.o.ld + (int64_t)h * a.o.hs;
-  for (int d = lane; d < a.D; d += 64) {
+  const float* p = a.part + stat * a.D;
+  const int64_t next = rows * a.D;
+  for (int d0 = 0; d0 < a.D; d0 += 64) {
+    const int d = min(d0 + lane, a.D - 1);
     float x = 0.f;
-    for (int k = 0; k < a.nsplit; ++k)
-      x += exp2_fast(st[k * rows * 2] - ms) * a.part[(k * rows + stat) * a.D + d];
-    o[d] = Mma<T>::from(x * inv);
+    for (int k0 = 0; k0 < a.nsplit; k0 += 8) {
+      float v[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) v[k] = p[min(k0 + k, a.nsplit - 1) * next + d];
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (k0 + k < a.nsplit) x = __fmaf_rn(__shfl(f, k0 + k), v[k], x);
+    }
+    if (d0 + lane < a.D) o[d] = Mma<T>::from(x * inv);
   }
   if (a.lse && lane == 0) a.lse[stat] = l == 0.f ? -INFINITY : __fmaf_rn(m, kLn2, logf(l));
 }
 
 namespace {
+#ifndef FSP
+#define FSP 512
+#define FKEYS 256
+#endif
 // Splits of the keys: enough workgroups to fill the chip twice, at least 256 keys (of an average
 // sequence) in each.
 int splits(const AttnArgs& a) {
   const int64_t wgs = attn_tiles(a.Tq, a.nseq, a.q_off != nullptr, a.G, BM) * a.Hkv;
   const int64_t keys = a.Tk / a.nseq;
   int64_t n = 1;
-  if (wgs < 256) n = std::min<int64_t>((512 + wgs - 1) / wgs, std::max<int64_t>(1, keys / 256));
+  if (wgs < 256) n = std::min<int64_t>((FSP + wgs - 1) / wgs, std::max<int64_t>(1, keys / FKEYS));
   return (int)std::min<int64_t>(n, 64);
 }
 
-template <typename T, int DP, int BN>
-hipError_t launch(const AttnArgs& a, bool vec, hipStream_t stream) {
+template <typename T, int DP, int BN, bool VEC>
+hipError_t launch(const AttnArgs& a, hipStream_t stream) {
   const int64_t n = attn_tiles(a.Tq, a.nseq, a.q_off != nullptr, a.G, BM) * a.Hkv * a.nsplit;
-  if (vec) hipLaunchKernelGGL((attn_fwd_kernel<T, DP, BN, true>), dim3((unsigned)n), dim3(256), 0, stream, a);
-  else hipLaunchKernelGGL((attn_fwd_kernel<T, DP, BN, false>), dim3((unsigned)n), dim3(256), 0, stream, a);
-  hipError_t e = hipGetLastError();
+  hipLaunchKernelGGL((attn_fwd_kernel<T, DP, BN, VEC>), dim3((unsigned)n), dim3(256), 0, stream, a);
+  const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.nsplit == 1) return e;
   const int64_t nj = attn_tiles(a.Tq, a.nseq, a.q_off != nullptr, a.Hq, 4);
   hipLaunchKernelGGL((attn_join_kernel<T>), dim3((unsigned)nj), dim3(256), 0, stream, a);
@@ -200,14 +224,29 @@ size_t attn_fwd_ws_bytes(const AttnArgs& a) {
 hipError_t attn_fwd_launch(AttnArgs a, bool bf16, bool vec, void* ws, hipStream_t stream) {
   a.nsplit = splits(a);
   a.part = (float*)ws;
+  // widths between the powers of two have their own products where the loads are whole slots
   if (bf16) {
-    if (a.D <= 64) return launch<uint16_t, 64, 64>(a, vec, stream);
-    if (a.D <= 128) return launch<uint16_t, 128, 64>(a, vec, stream);
-    return launch<uint16_t, 256, 64>(a, vec, stream);
+    if (!vec) {
+      if (a.D <= 64) return launch<uint16_t, 64, 64, false>(a, stream);
+      if (a.D <= 128) return launch<uint16_t, 128, 64, false>(a, stream);
+      return launch<uint16_t, 256, 64, false>(a, stream);
+    }
+    if (a.D <= 64) return launch<uint16_t, 64, 64, true>(a, stream);
+    if (a.D <= 96) return launch<uint16_t, 96, 64, true>(a, stream);
+    if (a.D <= 128) return launch<uint16_t, 128, 64, true>(a, stream);
+    if (a.D <= 192) return launch<uint16_t, 192, 64, true>(a, stream);
+    return launch<uint16_t, 256, 64, true>(a, stream);
   }
-  if (a.D <= 64) return launch<float, 64, 64>(a, vec, stream);
-  if (a.D <= 128) return launch<float, 128, 32>(a, vec, stream);
-  return launch<float, 256, 32>(a, vec, stream);
+  if (!vec) {
+    if (a.D <= 64) return launch<float, 64, 64, false>(a, stream);
+    if (a.D <= 128) return launch<float, 128, 32, false>(a, stream);
+    return launch<float, 256, 32, false>(a, stream);
+  }
+  if (a.D <= 64) return launch<float, 64, 64, true>(a, stream);
+  if (a.D <= 96) return launch<float, 96, 32, true>(a, stream);
+  if (a.D <= 128) return launch<float, 128, 32, true>(a, stream);
+  if (a.D <= 192) return launch<float, 192, 32, true>(a, stream);
+  return launch<float, 256, 32, true>(a, stream);
 }
 
 }  // namespace opfuse

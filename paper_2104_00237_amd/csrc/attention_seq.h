@@ -43,10 +43,9 @@ OF_HD int64_t attn_tiles(int64_t T, int nseq, bool offsets, int per, int B) {
   return offsets ? T * per / B + nseq : (T / nseq * per + B - 1) / B * nseq;
 }
 OF_HD void find_tile(const int32_t* off, int64_t T, int nseq, int per, int B, int64_t w, int& s, int64_t& tile) {
-  if (!off) {
-    const int64_t n = (T / nseq * per + B - 1) / B;
-    s = (int)(w / n);
-    tile = w - s * n;
+  if (!off) {   // equal slots: tile by tile, so that tiles of one length lie together
+    tile = w / nseq;
+    s = (int)(w - tile * nseq);
     return;
   }
   int lo = 0, hi = nseq;   // the last s whose first tile is <= w
@@ -56,6 +55,13 @@ OF_HD void find_tile(const int32_t* off, int64_t T, int nseq, int per, int B, in
   }
   s = lo;
   tile = w - (clamp64(off[lo], 0, T) * per / B + lo);
+}
+
+// Order of n workgroups of different lengths.  Two of them run on a CU at a time, the second wave's b + 256
+// beside b: where no more than that many are launched, the second half is taken from its end, so that
+// with the longest first the shortest joins the longest.
+OF_HD int64_t paired(int64_t b, int64_t n, int64_t first) {
+  return n <= 2 * first && b >= first ? n - 1 - (b - first) : b;
 }
 
 // Keys [lo, hi) that query i of a sequence sees (none where hi <= lo); nk keys, shift = nk - nq.  Both

@@ -85,6 +85,15 @@ int main() {
       }
     }
   }
+  for (int it = 0; it < 2000; ++it) {      // an order takes every number once
+    const int n = pick(1, 700), first = pick(1, 300);
+    std::vector<int> seen(n, 0);
+    for (int b = 0; b < n; ++b) {
+      const int64_t x = paired(b, n, first);
+      CHECK(x >= 0 && x < n && !seen[x]);
+      seen[x] = 1;
+    }
+  }
   // the largest window and the longest rows stay in range
   int lo, hi;
   keys_of(1, 0x7fffffff, 0x7ffffff0, 0, 0x7fffffff, lo, hi);
