@@ -61,7 +61,7 @@ __device__ __forceinline__ float dot_own(const afloatx4_t (&a)[NS], const afloat
 // delta and dQ: own rows are queries (all heads of a key head's group), keys stream.  copy: dO rounded
 // to T when it is stored in another type, [Tq, Hq, D].
 template <typename T, typename G, int DP, int BN, int RD, bool VEC>
-__global__ __launch_bounds__(256, sizeof(T) == 2 && DP <= 128 ? 2 : 1) void attn_dq_kernel(AttnArgs a, T* copy) {
+__global__ __launch_bounds__(256, DP <= (sizeof(T) == 2 ? 128 : 64) ? 2 : 1) void attn_dq_kernel(AttnArgs a, T* copy) {
   constexpr int ES = sizeof(T), SLOTS = slots_of(DP * ES), NS = DP * ES / 32, NB = DP / 32, NK = BN / 32, U = 32 / Mma<T>::TR;
   constexpr bool INIT = ES == 2;   // S starts from -lse / scale
   typedef typename Mma<T>::frag frag;
@@ -69,9 +69,9 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && DP <= 128 ? 2 : 1) void attn
   __shared__ __attribute__((aligned(1024))) char sk0[TB], sk1[TB], sv0[TB], sv1[TB];
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  int64_t w = blockIdx.x;
-  const int hk = (int)(w % a.Hkv);
-  w = paired(w / a.Hkv, gridDim.x / a.Hkv, 256 / a.Hkv);
+  uint32_t w = blockIdx.x;   // (32-bit divisions: a 64-bit one is 120 instructions)
+  const int hk = (int)(w % (uint32_t)a.Hkv);
+  w = paired(w / (uint32_t)a.Hkv, gridDim.x / (uint32_t)a.Hkv, 256u / (uint32_t)a.Hkv);
   int s;
   int64_t tile;
   find_tile(a.q_off, a.Tq, a.nseq, a.G, BM, w, s, tile);
@@ -215,14 +215,15 @@ __global__ __launch_bounds__(256, OCC) void attn_dkv_kernel(AttnArgs a) {
   __shared__ __attribute__((aligned(16))) float sl[2][BQ], sd[2][BQ];
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  int64_t w = blockIdx.x;
-  const int hk = (int)(w % a.Hkv);
-  w /= a.Hkv;
-  const int split = (int)(w % a.nsplit);
-  w /= a.nsplit;
+  uint32_t w = blockIdx.x;
+  const int hk = (int)(w % (uint32_t)a.Hkv);
+  w /= (uint32_t)a.Hkv;
+  const int split = (int)(w % (uint32_t)a.nsplit);
+  w /= (uint32_t)a.nsplit;
   static_assert(DP % DO == 0, "whole parts");
   const int d0 = (int)(w % (DP / DO)) * DO;   // first column of dK and dV
-  w = paired(w / (DP / DO), gridDim.x / (a.Hkv * a.nsplit * (DP / DO)), 256 / (a.Hkv * a.nsplit * (DP / DO)));
+  const uint32_t per_tile = (uint32_t)(a.Hkv * a.nsplit * (DP / DO));
+  w = paired(w / (DP / DO), gridDim.x / per_tile, 256u / per_tile);
   if (d0 >= a.D) return;
   int s;
   int64_t tile;
@@ -252,14 +253,14 @@ __global__ __launch_bounds__(256, OCC) void attn_dkv_kernel(AttnArgs a) {
 
   // tiles of queries, all heads of the group one after the other, and this split's run of them
   const int nt = max((qhi - qlo + BQ - 1) / BQ, 0);
-  const int64_t all = (int64_t)nt * a.G, run = (all + a.nsplit - 1) / a.nsplit;
-  const int64_t first = min(split * run, all);
-  const int64_t total = min(run, all - first);
+  const int all = nt * a.G, run = (int)((uint32_t)(all + a.nsplit - 1) / (uint32_t)a.nsplit);   // < 2^31: Tq Hq is
+  const int first = min(split * run, all);
+  const int total = min(run, all - first);
   const TileLoad<T, SLOTS, BQ, 256, VEC> lq(a.q, a.D, tid), ld_(a.dout, a.D, tid);
   float nl = 0.f, nd = 0.f;    // statistics of the tile on its way
-  int g1 = nt ? (int)(first / nt) : 0, i1 = qlo + (int)(first - (int64_t)g1 * nt) * BQ;   // its head and first query
+  int g1 = nt ? (int)((uint32_t)first / (uint32_t)nt) : 0, i1 = qlo + (first - g1 * nt) * BQ;   // its head and first query
   int i0 = i1;
-  int64_t left = total;
+  int left = total;
   auto request = [&](char* q1, char* o1) {
     const int h = hk * a.G + (left > 0 ? g1 : 0), n = left > 0 ? q.len - i1 : 0;   // past the run: zeros
     --left;
@@ -332,7 +333,7 @@ __global__ __launch_bounds__(256, OCC) void attn_dkv_kernel(AttnArgs a) {
           if constexpr (b == 0) own = Mma<T>::pack(p, u);
           ak[b] = Mma<T>::mma(f, own, ak[b]);
         }
-        if constexpr (OCC == 1) __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_sched_barrier(0);
       });
     });
     i0 += BQ;
@@ -341,7 +342,7 @@ __global__ __launch_bounds__(256, OCC) void attn_dkv_kernel(AttnArgs a) {
   // (two tiles a turn, a missing second one as zeros: a branch around it would make the compiler move
   // accumulators about)
   if (total > 0) request(sq0, so0);
-  for (int64_t t = 0; t < total; t += 2) {
+  for (int t = 0; t < total; t += 2) {
     step(sq0, so0, sl[0], sd[0], sq1, so1);
     step(sq1, so1, sl[1], sd[1], sq0, so0);
   }
@@ -370,8 +371,8 @@ __global__ __launch_bounds__(256) void attn_sum_kernel(AttnArgs a) {
   const int n = (int)min((int64_t)SUM_ROWS, R - r0) * a.D;
   const int64_t one = a.Tk * a.Hkv * a.D;
   for (int e = threadIdx.x; e < n; e += 256) {
-    const int x = e / a.D, d = e - x * a.D;
-    const int64_t row = (r0 + x) / a.Hkv;
+    const int x = (int)((uint32_t)e / (uint32_t)a.D), d = e - x * a.D;
+    const int64_t row = (uint32_t)(r0 + x) / (uint32_t)a.Hkv;
     const int hk = (int)(r0 + x - row * a.Hkv);
     const float* p = a.part + ((kv.beg + row) * a.Hkv + hk) * a.D + d;
     float k = p[0], v = p[one];

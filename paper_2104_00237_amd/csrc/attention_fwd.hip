@@ -6,25 +6,25 @@
 namespace opfuse {
 
 namespace {
-constexpr int NW = 4;               // wavefronts of a workgroup
-constexpr int BM = 32 * NW;         // rows: (query, head of the group) pairs, 32 a wavefront
+constexpr int BM = 128;   // rows of a workgroup: (query, head of the group) pairs, 32 for each of its four wavefronts
 }  // namespace
 
 // Rows r of a key head's group: query r / G, head r % G, so that the query heads that share a key
 // head share its tiles.  BN: keys of a tile.
 template <typename T, int DP, int BN, bool VEC>
-__global__ __launch_bounds__(256, sizeof(T) == 2 && DP <= 128 ? 2 : 1) void attn_fwd_kernel(AttnArgs a) {
+__global__ __launch_bounds__(256, DP <= (sizeof(T) == 2 ? 128 : 96) ? 2 : 1) void attn_fwd_kernel(AttnArgs a) {
   constexpr int ES = sizeof(T), SLOTS = slots_of(DP * ES), NS = DP * ES / 32, NB = DP / 32, NK = BN / 32;
   typedef typename Mma<T>::frag frag;
   constexpr int TB = BN * SLOTS * 16;
   __shared__ __attribute__((aligned(1024))) char sk0[TB], sk1[TB], sv0[TB], sv1[TB];
   const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  int64_t w = blockIdx.x;
-  const int hk = (int)(w % a.Hkv);
-  w /= a.Hkv;
-  const int split = (int)(w % a.nsplit);
-  w = paired(w / a.nsplit, gridDim.x / (a.Hkv * a.nsplit), 256 / (a.Hkv * a.nsplit));
+  uint32_t w = blockIdx.x;   // (32-bit divisions: a 64-bit one is 120 instructions)
+  const int hk = (int)(w % (uint32_t)a.Hkv);
+  w /= (uint32_t)a.Hkv;
+  const int split = (int)(w % (uint32_t)a.nsplit);
+  const uint32_t per_tile = (uint32_t)(a.Hkv * a.nsplit);
+  w = paired(w / (uint32_t)a.nsplit, gridDim.x / per_tile, 256u / per_tile);
   int s;
   int64_t tile;
   find_tile(a.q_off, a.Tq, a.nseq, a.G, BM, w, s, tile);
@@ -46,7 +46,7 @@ __global__ __launch_bounds__(256, sizeof(T) == 2 && DP <= 128 ? 2 : 1) void attn
   keys_of(a.causal, a.window, fdiv(r1 - 1, a.dG), shift, kv.len, lo1, khi);
   klo = klo / BN;                           // in tiles from here on
   const int nt = max((khi + BN - 1) / BN - klo, 0);
-  const int per = (nt + a.nsplit - 1) / a.nsplit;
+  const int per = (int)((uint32_t)(nt + a.nsplit - 1) / (uint32_t)a.nsplit);
   const int t0 = klo + min(split * per, nt), t1 = klo + min(split * per + per, nt);
   const unsigned span = has ? max(hi - lo, 0) : 0;
 
@@ -156,7 +156,7 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
   const SeqRows q = seq_rows(a.q_off, a.q_len, a.Tq, a.nseq, s);
   const int64_t r = tile * 4 + (threadIdx.x >> 6);
   if (tile < 0 || r >= (int64_t)q.len * a.Hq) return;
-  const int64_t i = r / a.Hq;
+  const int64_t i = (uint32_t)r / (uint32_t)a.Hq;
   const int h = (int)(r - i * a.Hq);
   const int64_t rows = (int64_t)a.Hq * a.Tq, stat = h * a.Tq + q.beg + i;
   const float* st = a.part + a.nsplit * rows * a.D + stat * 2;
@@ -190,17 +190,13 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
 }
 
 namespace {
-#ifndef FSP
-#define FSP 512
-#define FKEYS 256
-#endif
 // Splits of the keys: enough workgroups to fill the chip twice, at least 256 keys (of an average
 // sequence) in each.
 int splits(const AttnArgs& a) {
   const int64_t wgs = attn_tiles(a.Tq, a.nseq, a.q_off != nullptr, a.G, BM) * a.Hkv;
   const int64_t keys = a.Tk / a.nseq;
   int64_t n = 1;
-  if (wgs < 256) n = std::min<int64_t>((FSP + wgs - 1) / wgs, std::max<int64_t>(1, keys / FKEYS));
+  if (wgs < 256) n = std::min<int64_t>((512 + wgs - 1) / wgs, std::max<int64_t>(1, keys / 256));
   return (int)std::min<int64_t>(n, 64);
 }
 
@@ -238,11 +234,11 @@ hipError_t attn_fwd_launch(AttnArgs a, bool bf16, bool vec, void* ws, hipStream_
     return launch<uint16_t, 256, 64, true>(a, stream);
   }
   if (!vec) {
-    if (a.D <= 64) return launch<float, 64, 64, false>(a, stream);
+    if (a.D <= 64) return launch<float, 64, 32, false>(a, stream);
     if (a.D <= 128) return launch<float, 128, 32, false>(a, stream);
     return launch<float, 256, 32, false>(a, stream);
   }
-  if (a.D <= 64) return launch<float, 64, 64, true>(a, stream);
+  if (a.D <= 64) return launch<float, 64, 32, true>(a, stream);
   if (a.D <= 96) return launch<float, 96, 32, true>(a, stream);
   if (a.D <= 128) return launch<float, 128, 32, true>(a, stream);
   if (a.D <= 192) return launch<float, 192, 32, true>(a, stream);

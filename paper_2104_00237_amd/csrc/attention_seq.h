@@ -28,8 +28,8 @@ OF_HD SeqRows seq_rows(const int32_t* off, const int32_t* len, int64_t T, int ns
     b = clamp64(off[s], 0, T);
     e = clamp64(off[s + 1], b, T);
   } else {
-    const int64_t slot = T / nseq;
-    b = s * slot;
+    const uint32_t slot = (uint32_t)T / (uint32_t)nseq;   // T < 2^31
+    b = (int64_t)s * slot;
     e = b + slot;
   }
   return SeqRows{b, (int)(len ? clamp64(len[s], 0, e - b) : e - b)};
@@ -44,8 +44,9 @@ OF_HD int64_t attn_tiles(int64_t T, int nseq, bool offsets, int per, int B) {
 }
 OF_HD void find_tile(const int32_t* off, int64_t T, int nseq, int per, int B, int64_t w, int& s, int64_t& tile) {
   if (!off) {   // equal slots: tile by tile, so that tiles of one length lie together
-    tile = w / nseq;
-    s = (int)(w - tile * nseq);
+    const uint32_t t = (uint32_t)w / (uint32_t)nseq;   // (a grid has fewer than 2^31 workgroups)
+    tile = t;
+    s = (int)((uint32_t)w - t * (uint32_t)nseq);
     return;
   }
   int lo = 0, hi = nseq;   // the last s whose first tile is <= w
