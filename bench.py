@@ -38,7 +38,7 @@ import numpy as np
 ROOT = os.path.dirname(os.path.abspath(__file__))
 sys.path.insert(0, ROOT)
 
-from workloads import get_config, make_params, make_batch  # noqa: E402
+from workloads import get_config, make_params, make_batch, qkv_width  # noqa: E402
 
 PEAK_HBM = 8.0e12          # bytes/s
 PEAK_FP32_MFMA = 157.3e12  # flop/s
@@ -163,14 +163,15 @@ def tblock_launches(cfg):
     """Per-launch costs of the bf16 Transformer blocks.  Contractions take bf16
     operands: the weight is read as its 2-byte shadow, activations and
     gradients as fp32; the fused update also rewrites the shadow.  LayerNorm
-    and the residual adds count as `extra` bytes of their block."""
+    and the residual adds count as `extra` bytes of their block; attention (its
+    launches are classes of their own) is not counted."""
     M, d, f, nb = cfg["batch"], cfg["hidden"], cfg["ffn"], cfg["blocks"]
     h = n_state(cfg["opt"])
     G = min(64, max(1, (M + 63) // 64))
     out = []
     for b in range(1, nb + 1):
         p = f"blk{b}."
-        for name, N, K, act_prev, gelu in (("qkv", 3 * d, d, False, False),
+        for name, N, K, act_prev, gelu in (("qkv", qkv_width(cfg), d, False, False),
                                            ("proj", d, d, False, False),
                                            ("fc1", f, d, False, True),
                                            ("fc2", d, f, True, False)):

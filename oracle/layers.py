@@ -19,6 +19,8 @@ Definitions (the readings where the paper is silent):
   conv3x3     cross-correlation, stride 1, zero padding 1, NHWC / [Cout,3,3,Cin]
   dwconv3x3   the same per channel (depthwise, multiplier 1), filter [3,3,C],
               stride 1 or 2
+  rotary      pairs turned by position times base^(-2i/rot)
+  attention   softmax(q k^T / sqrt(D)) v per head, masked by position
   avgpool     mean over the spatial positions of each channel
   maxpool2x2  stride 2; the argmax is the first maximum of the window in
               row-major order (strict >), reported as its window position 0..3
@@ -160,6 +162,88 @@ class SliceCols(Op):
     def backward(self, shape, dy):
         dx = np.zeros(shape)
         dx[:, self.lo:self.hi] = dy
+        return (dx,), ()
+
+
+class Rotary(Op):
+    """Rotary positions of the first `heads` heads of width D of a packed row: row t is at
+    position t % seq_len, pair i < rot/2 turns by that times base^(-2i/rot); pairs
+    (i, i + rot/2), or (2i, 2i + 1) when interleaved.  bf16: input and output are
+    stored as bf16."""
+
+    def __init__(self, heads, D, seq_len, rot, base, interleaved=False, bf16=False):
+        super().__init__()
+        self.heads, self.D, self.seq_len, self.rot = heads, D, seq_len, rot
+        self.base, self.interleaved, self.bf16 = base, interleaved, bf16
+
+    def _turn(self, x, sign):
+        y = x.copy()
+        i = np.arange(self.rot // 2)
+        a = (np.arange(x.shape[0]) % self.seq_len)[:, None] * self.base ** (-2.0 * i / self.rot)
+        c, s = np.cos(a), sign * np.sin(a)
+        p, q = (2 * i, 2 * i + 1) if self.interleaved else (i, i + self.rot // 2)
+        for h in range(self.heads):
+            u, v = x[:, h * self.D + p], x[:, h * self.D + q]
+            y[:, h * self.D + p], y[:, h * self.D + q] = u * c - v * s, u * s + v * c
+        return y
+
+    def forward(self, x):
+        return _maybe_bf16(self._turn(_maybe_bf16(x, self.bf16), 1.0), self.bf16), None
+
+    def backward(self, _, dy):
+        return (self._turn(dy, -1.0),), ()
+
+
+class Attention(Op):
+    """Softmax attention of packed rows [heads query heads, kv_heads key heads, kv_heads value
+    heads] of width D, over sequences of seq_len rows: query i sees key j <= i if causal, and
+    |i - j| < window if window; scale 1 / sqrt(D).  bf16: the rows and the output are stored
+    as bf16, the incoming gradient is rounded to bf16 as an operand."""
+
+    def __init__(self, heads, kv_heads, D, seq_len, causal, window=0, bf16=False):
+        super().__init__()
+        self.heads, self.kv_heads, self.D, self.seq_len = heads, kv_heads, D, seq_len
+        self.causal, self.window, self.bf16 = causal, window, bf16
+
+    def _parts(self, x):
+        """(sequence, query head, slices of its q, k, v) of a packed array."""
+        D, L, G = self.D, self.seq_len, self.heads // self.kv_heads
+        for s in range(x.shape[0] // L):
+            r = slice(s * L, s * L + L)
+            for h in range(self.heads):
+                k = self.heads + h // G
+                v = k + self.kv_heads
+                yield r, h, (r, slice(h * D, h * D + D)), (r, slice(k * D, k * D + D)), \
+                    (r, slice(v * D, v * D + D))
+
+    def _p(self, q, k):
+        far = np.arange(self.seq_len)[:, None] - np.arange(self.seq_len)[None]
+        hide = np.zeros(far.shape, bool)
+        if self.causal:
+            hide |= far < 0
+        if self.window:
+            hide |= np.abs(far) >= self.window
+        z = np.where(hide, -np.inf, q @ k.T / np.sqrt(self.D))
+        e = np.exp(z - z.max(axis=1, keepdims=True))     # (a row always sees itself)
+        return e / e.sum(axis=1, keepdims=True)
+
+    def forward(self, x):
+        x = _maybe_bf16(x, self.bf16)
+        o = np.zeros((x.shape[0], self.heads * self.D))
+        for r, h, q, k, v in self._parts(x):
+            o[r, h * self.D:(h + 1) * self.D] = self._p(x[q], x[k]) @ x[v]
+        return _maybe_bf16(o, self.bf16), x
+
+    def backward(self, x, dy):
+        dy = _maybe_bf16(dy, self.bf16)
+        dx = np.zeros_like(x)
+        for r, h, q, k, v in self._parts(x):
+            p, do = self._p(x[q], x[k]), dy[r, h * self.D:(h + 1) * self.D]
+            dp = do @ x[v].T
+            ds = p * (dp - (p * dp).sum(axis=1, keepdims=True)) / np.sqrt(self.D)
+            dx[q] += ds @ x[k]
+            dx[k] += ds.T @ x[q]
+            dx[v] += p.T @ do
         return (dx,), ()
 
 

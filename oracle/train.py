@@ -289,12 +289,24 @@ def new_model(cfg, init=None, seed=0):
         d = cfg["hidden"]
         bf16 = cfg["dtype"] == "bf16"
         cur = "input"
+        att = cfg.get("attention")
+
+        def context(p):
+            """The out-projection's input: the V third of qkv, or attention."""
+            if not att:
+                return [(L.SliceCols(2 * d, 3 * d), [p + "qkv"], p + "v")]
+            H, Hk, D, Ls, rope = att["heads"], att["kv_heads"], d // att["heads"], att["seq_len"], att.get("rope")
+            turn = [(L.Rotary(H + Hk, D, Ls, rope["rot"], rope["base"], rope["interleaved"], bf16),
+                     [p + "qkv"], p + "rot")] if rope else []
+            return turn + [(L.Attention(H, Hk, D, Ls, att["causal"], att.get("window", 0), bf16),
+                            [p + "rot" if rope else p + "qkv"], p + "v")]
+
         for b in range(1, cfg["blocks"] + 1):
             p = f"blk{b}."
             nodes += [
                 (L.LayerNorm(P(p + "ln1.weight"), P(p + "ln1.bias"), cfg["ln_eps"]), [cur], p + "a"),
                 (L.Linear(P(p + "qkv.weight"), P(p + "qkv.bias"), bf16), [p + "a"], p + "qkv"),
-                (L.SliceCols(2 * d, 3 * d), [p + "qkv"], p + "v"),
+                *context(p),
                 (L.Linear(P(p + "proj.weight"), P(p + "proj.bias"), bf16), [p + "v"], p + "o"),
                 (L.Add(), [cur, p + "o"], p + "h"),
                 (L.LayerNorm(P(p + "ln2.weight"), P(p + "ln2.bias"), cfg["ln_eps"]), [p + "h"], p + "c"),

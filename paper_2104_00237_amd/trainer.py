@@ -437,6 +437,47 @@ class LayerNormOp:
                              stream if stream is not None else tr._s())
 
 
+class AttentionOp:
+    """Softmax attention of a packed QKV buffer [M, (Hq + 2 Hkv) D] (query heads, key
+    heads, value heads) of `dtype`, the rotary positions of its queries and keys
+    applied in place first.  No parameters; gradients are fp32."""
+
+    kind = "attention"
+
+    def __init__(self, att, M, d, dtype):
+        H, Hk, Ls = att["heads"], att["kv_heads"], att["seq_len"]
+        D = d // H
+        self.width = d + 2 * Hk * D
+        self.size = 2 if dtype == L.OF_BF16 else 4
+        self.k, self.v = d, d + Hk * D          # first elements of the key and value heads
+        self.desc = L.OfAttnDesc(Tq=M, Tk=M, nseq=M // Ls, Hq=H, Hkv=Hk, D=D, dtype=dtype,
+                                 grad_dtype=L.OF_F32, causal=int(att["causal"]),
+                                 window=att.get("window", 0), ldq=self.width, ldk=self.width,
+                                 ldv=self.width)
+        rope = att.get("rope")
+        self.rope = self.rope_bwd = None
+        if rope:
+            hyper = dict(T=M, seq_len=Ls, H=H + Hk, D=D, rot=rope["rot"], base=rope["base"],
+                         interleaved=int(rope["interleaved"]), ldx=self.width, ldy=self.width)
+            self.rope = L.OfRotaryDesc(dtype=dtype, **hyper)
+            self.rope_bwd = L.OfRotaryDesc(dtype=L.OF_F32, **hyper)
+
+    def ws(self):
+        return max(L.of_attn_workspace_size(self.desc, op) for op in (L.OF_ATTN_FWD, L.OF_ATTN_BWD))
+
+    def fwd(self, tr, qkv, o, lse):
+        if self.rope is not None:
+            L.of_rotary_fwd(self.rope, qkv, None, qkv, tr._s())
+        L.of_attn_fwd(self.desc, qkv, qkv + self.k * self.size, qkv + self.v * self.size, o, lse,
+                      *tr.ws_main_args(), tr._s())
+
+    def bwd(self, tr, qkv, o, lse, do, dqkv):
+        L.of_attn_bwd(self.desc, qkv, qkv + self.k * self.size, qkv + self.v * self.size, o, lse, do,
+                      dqkv, dqkv + 4 * self.k, dqkv + 4 * self.v, *tr.ws_main_args(), tr._s())
+        if self.rope is not None:
+            L.of_rotary_bwd(self.rope_bwd, dqkv, None, dqkv, tr._s())
+
+
 def _ff_prologue(tr, op):
     """Whether forward-fusion applies op's pending update in its forward's W-tile
     loads (else a previous launch carries it, or a pass of its own runs)."""
@@ -662,7 +703,9 @@ class ChainNet:
 class TBlockNet:
     """Pre-LN residual blocks with bf16-operand linears (the tblock workload):
 
-        a = LN1(x); qkv = a Wqkv^T + b; v = qkv[:, 2d:3d]   (identity attention)
+        a = LN1(x); qkv = a Wqkv^T + b
+        v = qkv[:, 2d:3d]   (identity attention), or with cfg["attention"]
+        v = attention(rotary(q), rotary(k), v) of the parts of qkv
         h = x + v Wproj^T + b
         c = LN2(h); u = c W1^T + b; g = GELU(u); y = h + g W2^T + b
 
@@ -692,6 +735,11 @@ class TBlockNet:
         acts = shadow and bf16_acts
         xb = L.OF_IO_X_BF16 if acts else 0
         yb = L.OF_IO_Y_BF16 if acts else 0
+        att = cfg.get("attention")
+        # attention reads q, k, v as they are stored; its gradients are fp32 like every other
+        self.attn = AttentionOp(att, M, d, L.OF_BF16 if acts else L.OF_F32) if att else None
+        self.ws_main_bytes = self.attn.ws() if att else 0
+        qw = self.attn.width if att else 3 * d
         self.blocks = []
         self.ops = []
         for b in range(1, nb + 1):
@@ -702,7 +750,7 @@ class TBlockNet:
                 qkv=LinearOp(p + "qkv", pb(p + "qkv.weight", shadow), pb(p + "qkv.bias"), M, "none",
                              dt, io=xb | yb),
                 proj=LinearOp(p + "proj", pb(p + "proj.weight", shadow), pb(p + "proj.bias"), M,
-                              "none", dt, ldx=3 * d, io=xb),
+                              "none", dt, ldx=0 if att else 3 * d, io=xb),
                 ln2=LayerNormOp(p + "ln2", pb(p + "ln2.weight", rows=G), pb(p + "ln2.bias", rows=G),
                                 M, d, eps, y_bf16=acts),
                 fc1=LinearOp(p + "fc1", pb(p + "fc1.weight", shadow), pb(p + "fc1.bias"), M, "gelu",
@@ -722,17 +770,22 @@ class TBlockNet:
             return torch.empty(shape, **act)
 
         for blk in self.blocks:
-            blk.update(a=ta(M, d), mu1=t(M), rs1=t(M), qkv_out=ta(M, 3 * d), h=t(M, d),
+            blk.update(a=ta(M, d), mu1=t(M), rs1=t(M), qkv_out=ta(M, qw), h=t(M, d),
                        c=ta(M, d), mu2=t(M), rs2=t(M), u=t(M, f), g=ta(M, f), y=t(M, d),
                        gy=t(M, d), gu=t(M, f), gc=t(M, d), gh=t(M, d), ga=t(M, d),
-                       # the Q and K thirds of the QKV gradient stay zero
-                       gqkv=torch.zeros((M, 3 * d), **f32))
+                       # (identity attention: the Q and K thirds of the QKV gradient stay zero)
+                       gqkv=torch.zeros((M, qw), **f32))
+            if att:
+                blk.update(ctx=ta(M, d), lse=t(att["heads"], M), gctx=t(M, d))
         self.gx = t(M, d)   # gradient w.r.t. the network input (not used further)
         self.out = self.blocks[-1]["y"]
         self.gout = self.blocks[-1]["gy"]
 
     def _v(self, blk):
-        """Address of the V third of the block's QKV output."""
+        """Address of the out-projection's input: the attention output, or the V third of
+        the block's QKV output."""
+        if self.attn is not None:
+            return blk["ctx"].data_ptr()
         q = blk["qkv_out"]
         return q.data_ptr() + 2 * self.d * q.element_size()
 
@@ -769,6 +822,12 @@ class TBlockNet:
                 op.fwd(tr, xin, blk["a"].data_ptr(), blk["mu1"].data_ptr(), blk["rs1"].data_ptr())
             elif name == "qkv":
                 op.fwd(tr, blk["a"].data_ptr(), blk["qkv_out"].data_ptr(), carry=carry)
+                if self.attn is not None:
+                    tr._t1("fwd", tr.stream)
+                    tr._t0("attn", tr.stream, self.attn)
+                    self.attn.fwd(tr, blk["qkv_out"].data_ptr(), blk["ctx"].data_ptr(),
+                                  blk["lse"].data_ptr())
+                    tr._t1("attn", tr.stream)
             elif name == "proj":     # h = x + attention output (residual in the epilogue)
                 op.fwd(tr, self._v(blk), blk["h"].data_ptr(), carry=carry, res=xin)
             elif name == "ln2":
@@ -780,7 +839,8 @@ class TBlockNet:
             else:                    # y = h + MLP output, the next block's input
                 op.fwd(tr, blk["g"].data_ptr(), blk["y"].data_ptr(), carry=carry,
                        res=blk["h"].data_ptr())
-            tr._t1("fwd", tr.stream)
+            if name != "qkv" or self.attn is None:
+                tr._t1("fwd", tr.stream)
             for o in carried:
                 o.updated = True     # their updates are enqueued with this launch
             if name == "fc2":
@@ -867,7 +927,11 @@ class TBlockNet:
             self._ln_bwd(blk["ln2"], P["gc"], P["h"], P["mu2"], P["rs2"], P["gy"], P["gh"], fused,
                          done)
             self._linear_bwd(blk["proj"], P["gh"], self._v(blk), None, L.OF_ACT_NONE,
-                             P["gqkv"] + 8 * d, fused, done)
+                             P["gqkv"] + 8 * d if self.attn is None else P["gctx"], fused, done)
+            if self.attn is not None:
+                self.tr._t0("attn_bwd", self.tr.stream, self.attn)
+                self.attn.bwd(self.tr, P["qkv_out"], P["ctx"], P["lse"], P["gctx"], P["gqkv"])
+                self.tr._t1("attn_bwd", self.tr.stream)
             self._linear_bwd(blk["qkv"], P["gqkv"], P["a"], None, L.OF_ACT_NONE, P["ga"], fused,
                              done)
             self._ln_bwd(blk["ln1"], P["ga"], self._block_in(k, x), P["mu1"], P["rs1"], P["gh"],
@@ -1024,7 +1088,8 @@ class MBNet:
                 blk = self.residual_of.get(id(op))
                 op.fwd(tr, src.data_ptr(), dst.data_ptr(), carry=carry,
                        res=blk["x"].data_ptr() if blk is not None else None)
-            tr._t1("fwd", tr.stream)
+            if name != "qkv" or self.attn is None:
+                tr._t1("fwd", tr.stream)
             for o in carried:
                 o.updated = True     # their updates are enqueued with this launch
             if op is self.head:
@@ -1219,6 +1284,7 @@ class Trainer:
         wsm = max([op.ws(w) for op in self.ops for w in (0, 1, 2)] + [16])
         wsm = max([wsm] + [op.ws(L.OF_LINEAR_BWD_MERGED) for op in self.ops if op.kind == "linear"
                            and op.merge_dgrad])
+        wsm = max(wsm, getattr(self.net, "ws_main_bytes", 0))
         wss = max([op.ws(2) for op in self.ops] + [16])
         if cfg["loss"] == "mse":
             wsm = max(wsm, L.of_mse_workspace_size(*self.net.out.shape))

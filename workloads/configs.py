@@ -15,6 +15,13 @@ Model families:
               h = x + OutProj(V(QKV(LN1(x))))     (attention replaced by identity,
                                                     so the context is the V third)
               y = h + FC2(GELU(FC1(LN2(h))))
+          `attention` (optional): softmax attention instead of the identity.  The
+          rows are sequences of `seq_len`; `heads` query heads and `kv_heads` key
+          and value heads of width hidden / heads; `causal`; `window` (0: none);
+          `rope`: the rotary positions of queries and keys (base, rot: the leading
+          elements of a head that are turned, interleaved: pair layout), or absent.
+          QKV then has hidden + 2 * kv_heads * (hidden / heads) outputs: the query
+          heads, the key heads, the value heads.
   vgg     3x3 convolutions (stride 1, zero pad 1, bias, ReLU) with output
           channels `channels`; a 2x2 max-pool after the convolutions listed in
           `pool_after` (1-based); a final linear classifier on the 1x1 map.
@@ -61,6 +68,17 @@ CONFIGS = {
                  weight_decay=0.01),
         ln_eps=1e-5,
     ),
+    # The same blocks with causal attention over 4 sequences of 1024 rows: 16 query
+    # heads of 64 share 4 key and value heads, rotary positions.
+    "attn12": dict(
+        kind="tblock", blocks=12, hidden=1024, ffn=4096, batch=4096,
+        loss="mse", dtype="bf16", steps=10,
+        opt=dict(kind="adamw", lr=1e-4, beta1=0.9, beta2=0.999, eps=1e-8,
+                 weight_decay=0.01),
+        ln_eps=1e-5,
+        attention=dict(heads=16, kv_heads=4, seq_len=1024, causal=True, window=0,
+                       rope=dict(base=10000.0, rot=64, interleaved=False)),
+    ),
     # VGG-11-style convolution stack on 32x32x3 images, SGD with momentum.
     "vgg11": dict(
         kind="vgg", channels=[64, 128, 256, 256, 512, 512, 512, 512],
@@ -105,6 +123,9 @@ _REDUCED = {
     "mlp4tied": {},
     "mlp8x1024": dict(dims=[200, 168, 168, 168, 10], batch=72, steps=4),
     "tblock12": dict(blocks=2, hidden=96, ffn=160, batch=136, steps=3),
+    "attn12": dict(blocks=2, hidden=96, ffn=160, batch=136, steps=3,
+                   attention=dict(heads=4, kv_heads=2, seq_len=68, causal=True, window=0,
+                                  rope=dict(base=10000.0, rot=16, interleaved=True))),
     # The full learning rate (0.1, no normalisation layers) diverges within a few
     # steps at this size; the reduced run uses 0.01 so that K-step parity compares
     # a training trajectory rather than an overflow.
@@ -165,6 +186,16 @@ def mbv2_blocks(cfg):
     return out
 
 
+def qkv_width(cfg):
+    """Outputs of a tblock workload's QKV linear."""
+    a = cfg.get("attention")
+    if not a:
+        return 3 * cfg["hidden"]
+    if cfg["hidden"] % a["heads"] or a["heads"] % a["kv_heads"] or cfg["batch"] % a["seq_len"]:
+        raise ValueError("hidden / heads, heads / kv_heads and batch / seq_len must be whole")
+    return cfg["hidden"] + 2 * a["kv_heads"] * (cfg["hidden"] // a["heads"])
+
+
 def param_specs(cfg):
     """Trainable tensors in model order: list of (name, shape, init, fan_in).
 
@@ -188,8 +219,8 @@ def param_specs(cfg):
             specs += [
                 (p + "ln1.weight", (d,), "ones", d),
                 (p + "ln1.bias", (d,), "zeros", d),
-                (p + "qkv.weight", (3 * d, d), "kaiming", d),
-                (p + "qkv.bias", (3 * d,), "zeros", d),
+                (p + "qkv.weight", (qkv_width(cfg), d), "kaiming", d),
+                (p + "qkv.bias", (qkv_width(cfg),), "zeros", d),
                 (p + "proj.weight", (d, d), "kaiming", d),
                 (p + "proj.bias", (d,), "zeros", d),
                 (p + "ln2.weight", (d,), "ones", d),
@@ -258,6 +289,9 @@ def describe(cfg):
         s = "mlp " + "-".join(map(str, cfg["dims"]))
     elif k == "tblock":
         s = f"tblock x{cfg['blocks']} d{cfg['hidden']} ffn{cfg['ffn']}"
+        if cfg.get("attention"):
+            a = cfg["attention"]
+            s += f" attention {a['heads']}/{a['kv_heads']} heads seq{a['seq_len']}"
     elif k == "mbv2":
         s = f"mbv2 {len(mbv2_blocks(cfg))} blocks stem{cfg['stem']} head{cfg['head']} img{cfg['image']}"
     else:
