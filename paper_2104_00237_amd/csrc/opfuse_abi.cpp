@@ -1154,7 +1154,7 @@ of_status check_heads(const char* name, int64_t T, int64_t H, int64_t D, int64_t
           (long long)*ld, (long long)*hs);
   REQUIRE(*ld <= (1LL << 22) && *hs <= (1LL << 40), OF_EUNSUPPORTED,
           "%s: row stride must be <= 2^22 and head stride <= 2^40", name);
-  REQUIRE(*ld >= (H - 1) * *hs + D || *hs >= (T - 1) * *ld + D, OF_EINVAL,
+  REQUIRE(*ld >= (__int128)(H - 1) * *hs + D || *hs >= (__int128)(T - 1) * *ld + D, OF_EINVAL,
           "%s: rows overlap (row stride %lld, head stride %lld)", name, (long long)*ld, (long long)*hs);
   return OF_OK;
 }
@@ -1173,7 +1173,8 @@ of_status check_rotary(const of_rotary_desc* d, const void* x, const int64_t* po
           "T must be < 2^31 and H * D <= 2^22");
   REQUIRE(d->interleaved == 0 || d->interleaved == 1, OF_EINVAL, "interleaved must be 0 or 1");
   REQUIRE(d->dtype == OF_F32 || d->dtype == OF_BF16, OF_EINVAL, "dtype %d is not an of_dtype", (int)d->dtype);
-  REQUIRE(d->seq_len >= 0 && d->pos0 >= 0, OF_EINVAL, "seq_len and pos0 must be >= 0");
+  REQUIRE(d->seq_len >= 0 && d->pos0 >= 0 && d->pos0 <= (1LL << 52), OF_EINVAL,
+          "seq_len and pos0 must be >= 0, pos0 <= 2^52");
   REQUIRE(std::isfinite(d->base) && d->base > 1.0, OF_EINVAL, "base must be finite and > 1");
   REQUIRE(d->scaling >= OF_ROPE_NONE && d->scaling <= OF_ROPE_BANDS, OF_EINVAL,
           "scaling %d is not an of_rope_scaling", (int)d->scaling);
@@ -1250,8 +1251,8 @@ of_status check_attn(const of_attn_desc* d, bool bwd, AttnArgs* a) {
   REQUIRE(d->causal == 0 || d->causal == 1, OF_EINVAL, "causal must be 0 or 1");
   REQUIRE(d->window >= 0, OF_EINVAL, "window must be >= 0 (0: none)");
   REQUIRE(std::isfinite(d->scale) && d->scale >= 0.f, OF_EINVAL, "scale must be finite and >= 0 (0: 1 / sqrt(D))");
-  REQUIRE(d->Tq < (1LL << 31) && d->Tk < (1LL << 31) && d->Tq <= ((1LL << 31) - 1) / d->Hq, OF_EUNSUPPORTED,
-          "Tq * Hq and Tk must be < 2^31");
+  REQUIRE(d->Tq <= ((1LL << 31) - 1) / d->Hq && d->Tk <= ((1LL << 31) - 1) / d->Hkv, OF_EUNSUPPORTED,
+          "Tq * Hq and Tk * Hkv must be < 2^31");
   REQUIRE(d->nseq <= (1LL << 27) / d->Hq, OF_EUNSUPPORTED, "nseq * Hq must be <= 2^27");
   REQUIRE(d->q_off || d->Tq % d->nseq == 0, OF_EINVAL, "without q_off, Tq must be a multiple of nseq");
   REQUIRE(d->k_off || d->Tk % d->nseq == 0, OF_EINVAL, "without k_off, Tk must be a multiple of nseq");
@@ -1363,7 +1364,7 @@ of_status of_attn_bwd(const of_attn_desc* d, const void* q, const void* k, const
   const int n = 16 / es;
   // (dO stored in another type than the operands' is copied to the workspace, where it is aligned)
   const bool vec = d->D % n == 0 && heads_aligned(a.q, n, es) && heads_aligned(a.k, n, es) &&
-                   heads_aligned(a.v, n, es) && (bf16 != gbf || heads_aligned(a.dout, n, es));
+                   heads_aligned(a.v, n, es) && heads_aligned(a.o, n, es) && (bf16 != gbf || heads_aligned(a.dout, n, es));
   return hip_status(attn_bwd_launch(a, bf16, gbf, vec, ws, (hipStream_t)stream), "of_attn_bwd launch");
 }
 

@@ -1088,8 +1088,7 @@ class MBNet:
                 blk = self.residual_of.get(id(op))
                 op.fwd(tr, src.data_ptr(), dst.data_ptr(), carry=carry,
                        res=blk["x"].data_ptr() if blk is not None else None)
-            if name != "qkv" or self.attn is None:
-                tr._t1("fwd", tr.stream)
+            tr._t1("fwd", tr.stream)
             for o in carried:
                 o.updated = True     # their updates are enqueued with this launch
             if op is self.head:

@@ -36,7 +36,7 @@ def test_rotary(fn):
     bad(L.OF_EINVAL, x=None)
     bad(L.OF_EINVAL, y=None)
     for kw in (dict(T=0), dict(H=0), dict(D=0), dict(rot=0), dict(rot=3), dict(rot=66), dict(rot=-2), dict(interleaved=2),
-               dict(dtype=7), dict(seq_len=-1), dict(pos0=-1), dict(base=1.0), dict(base=float("nan")), dict(scaling=4),
+               dict(dtype=7), dict(seq_len=-1), dict(pos0=-1), dict(pos0=1 << 60), dict(base=1.0), dict(base=float("nan")), dict(scaling=4),
                dict(scaling=-1), dict(scaling=L.OF_ROPE_LINEAR), dict(scaling=L.OF_ROPE_BASE, factor=float("inf")),
                dict(scaling=L.OF_ROPE_BANDS, factor=2.0), dict(mscale=-1.0), dict(mscale=float("nan")),
                dict(scaling=L.OF_ROPE_BANDS, factor=2.0, orig_len=10.0, low_turns=4.0, high_turns=4.0),
@@ -66,7 +66,8 @@ BAD = [(L.OF_EINVAL, dict(Tq=0)), (L.OF_EINVAL, dict(Tk=0)), (L.OF_EINVAL, dict(
        (L.OF_EINVAL, dict(Hkv=0)), (L.OF_EINVAL, dict(Hq=3)), (L.OF_EINVAL, dict(D=0)), (L.OF_EUNSUPPORTED, dict(D=257)),
        (L.OF_EINVAL, dict(dtype=3)), (L.OF_EINVAL, dict(grad_dtype=3)), (L.OF_EINVAL, dict(causal=2)),
        (L.OF_EINVAL, dict(window=-1)), (L.OF_EINVAL, dict(scale=-1.0)), (L.OF_EINVAL, dict(scale=float("nan"))),
-       (L.OF_EUNSUPPORTED, dict(Tq=1 << 30)), (L.OF_EUNSUPPORTED, dict(Tk=1 << 31)),
+       (L.OF_EUNSUPPORTED, dict(Tq=1 << 30)), (L.OF_EUNSUPPORTED, dict(Tk=1 << 31)), (L.OF_EUNSUPPORTED, dict(Tk=1 << 30)),
+       (L.OF_EUNSUPPORTED, dict(Hq=1 << 29, Hkv=1 << 29, hsq=1 << 40)),
        (L.OF_EUNSUPPORTED, dict(nseq=1 << 26, Tq=1 << 26, Tk=1 << 26)), (L.OF_EINVAL, dict(Tq=65)),
        (L.OF_EINVAL, dict(Tk=65)), (L.OF_EALIGN, dict(q_off=FAKE + 2)), (L.OF_EALIGN, dict(k_len=FAKE + 1)),
        (L.OF_EINVAL, dict(ldq=63)), (L.OF_EINVAL, dict(hsk=63)), (L.OF_EINVAL, dict(ldv=100)),

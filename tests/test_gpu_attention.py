@@ -197,6 +197,51 @@ def test_longer_sequences(gpu, dtype):
     Call([500], [800], Hq=1, Hkv=1, D=128, dtype=dtype).fwd().bwd().check()
 
 
+@pytest.mark.parametrize("D", [64, 96, 128, 192, 256])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_split_backward(gpu, dtype, D):
+    """Few key tiles, many queries: dK and dV in parts over the queries of several heads, and their sum."""
+    c = Call([1200, 40], [300, 40], Hq=4, Hkv=1, D=D, dtype=dtype, causal=1, tail=2)
+    stats = 4 * (4 * c.Tq + 3)
+    assert c.ws[L.OF_ATTN_BWD][1] > stats
+    c.fwd().bwd().check()
+    Call([700], [700], Hq=4, Hkv=2, D=D, dtype=dtype, causal=1, window=90, slots=True, grad="f32").fwd().bwd().check()
+
+
+def test_offsets_with_lengths(gpu):
+    """Slots of different sizes, given by offsets, filled in part: keys in a cache, packed queries."""
+    c = Call([3, 40, 1, 17], [100, 40, 9, 64], Hq=4, Hkv=2, D=64, causal=1, slots=True)
+    c.d.q_off, c.d.k_off = c.keep[0].data_ptr(), c.keep[1].data_ptr()
+    c.fwd().bwd().check()
+
+
+@pytest.mark.parametrize("name", ["q", "k", "v", "o", "do", "dq", "dk", "dv"])
+def test_one_tensor_off_alignment(gpu, name):
+    """Each tensor alone two bytes off a 16-byte address, the others on one."""
+    c = Call([70, 9], [70, 9], Hq=4, Hkv=2, D=64, causal=1)
+    setattr(c, name, c.place(getattr(c, name).cpu(), "rows", 1))
+    c.fwd().bwd().check()
+
+
+def test_more_queries_than_keys_in_a_window(gpu):
+    for causal in (0, 1):
+        Call([300], [70], Hq=2, Hkv=1, D=64, causal=causal, window=20).fwd().bwd().check()
+        Call([70], [300], Hq=2, Hkv=1, D=64, causal=causal, window=20).fwd().bwd().check()
+
+
+def test_large_logits(gpu):
+    """Maxima that grow from tile to tile by more and by less than the kernel's step of its running
+    maximum, in both orders; rows of one huge logit.  (fp32: the logits' own error grows with them, and
+    the bound with it.)"""
+    for dtype in ("bf16", "f32"):
+        c = Call([260], [260], Hq=1, Hkv=1, D=64, dtype=dtype)
+        f = torch.linspace(0.1, 6.0, 260, device=gpu)[:, None, None]
+        c.k.copy_(c.k.float() * f)
+        c.fwd().bwd().check()
+        c.k.copy_(c.k.flip(0))
+        c.fwd().bwd().check()
+
+
 def test_many_sequences(gpu):
     lens = [(i * 7) % 13 for i in range(300)]
     Call(lens, lens, Hq=2, Hkv=1, D=16, causal=1).fwd().bwd().check()
