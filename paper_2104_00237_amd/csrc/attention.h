@@ -194,26 +194,44 @@ __device__ __forceinline__ void tile_barrier() {
   __builtin_amdgcn_sched_barrier(0);
 }
 
-// The lane's own row as B fragments: 16 bytes at slot 2 s + h for every step s.
+// The lane's own row as B fragments: 16 bytes at slot 2 s + h for step s.
+template <typename T, bool VEC>
+__device__ __forceinline__ typename Mma<T>::frag own_frag(const T* row, bool has, int s, int D, int lane) {
+  constexpr int E = Mma<T>::E;
+  const int d = (2 * s + (lane >> 5)) * E;
+  typename Mma<T>::frag f = Mma<T>::zero();
+  if constexpr (VEC) {
+    if (has && d < D) f = *reinterpret_cast<const typename Mma<T>::frag*>(row + d);
+  } else {
+    T t[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      t[e] = 0;
+      if (has && d + e < D) t[e] = row[d + e];
+    }
+    f = __builtin_bit_cast(typename Mma<T>::frag, t);
+  }
+  return f;
+}
 template <typename T, int NS, bool VEC>
 __device__ __forceinline__ void load_own(typename Mma<T>::frag (&f)[NS], const T* row, bool has, int D, int lane) {
-  constexpr int E = Mma<T>::E;
 #pragma unroll
-  for (int s = 0; s < NS; ++s) {
-    const int d = (2 * s + (lane >> 5)) * E;
-    f[s] = Mma<T>::zero();
-    if constexpr (VEC) {
-      if (has && d < D) f[s] = *reinterpret_cast<const typename Mma<T>::frag*>(row + d);
-    } else {
-      T t[E];
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        t[e] = 0;
-        if (has && d + e < D) t[e] = row[d + e];
-      }
-      f[s] = __builtin_bit_cast(typename Mma<T>::frag, t);
-    }
-  }
+  for (int s = 0; s < NS; ++s) f[s] = own_frag<T, VEC>(row, has, s, D, lane);
+}
+// Own rows stay in registers, but for wide fp32 rows, which do not fit beside the sums: those are
+// loaded again (from the caches) OD steps before each use, whose four MFMAs take 256 cycles.
+template <typename T, int DP>
+constexpr bool kKeepOwn = sizeof(T) == 2 || DP <= 128;
+constexpr int OD = 4;
+
+// A lane number, with FRESH one that the compiler knows nothing of: a fragment's LDS addresses are then
+// computed where it is read instead of held in registers by the dozen.  For the kernels that spill
+// otherwise (forward, fp32, width 256: 903 -> 409 us; backward 4275 -> 2006); where they do not it
+// costs (forward, fp32, width 128: 163 -> 207 us; bf16, 256: 67 -> 95).
+template <bool FRESH>
+__device__ __forceinline__ int fresh(int lane) {
+  if constexpr (FRESH) asm volatile("" : "+v"(lane));
+  return lane;
 }
 
 // Accumulators [d, own row] times f, stored to the lane's row.

@@ -64,6 +64,7 @@ template <typename T, typename G, int DP, int BN, int RD, bool VEC>
 __global__ __launch_bounds__(256, DP <= (sizeof(T) == 2 ? 128 : 64) ? 2 : 1) void attn_dq_kernel(AttnArgs a, T* copy) {
   constexpr int ES = sizeof(T), SLOTS = slots_of(DP * ES), NS = DP * ES / 32, NB = DP / 32, NK = BN / 32, U = 32 / Mma<T>::TR;
   constexpr bool INIT = ES == 2;   // S starts from -lse / scale
+  constexpr bool FRESH = ES == 4 ? DP >= 128 : !VEC && DP == 256;
   typedef typename Mma<T>::frag frag;
   constexpr int TB = BN * SLOTS * 16;
   __shared__ __attribute__((aligned(1024))) char sk0[TB], sk1[TB], sv0[TB], sv1[TB];
@@ -95,15 +96,28 @@ __global__ __launch_bounds__(256, DP <= (sizeof(T) == 2 ? 128 : 64) ? 2 : 1) voi
   const unsigned span = has ? max(hi - lo, 0) : 0;
 
   const int64_t row = q.beg + i, stat = (int64_t)h * a.Tq + row;
-  frag fq[NS], fo[NS];
-  float delta;
-  if constexpr (sizeof(T) == sizeof(G))
-    load_own<T, NS, VEC>(fo, (const T*)a.dout.p + row * a.dout.ld + (int64_t)h * a.dout.hs, has, a.D, lane);
+  constexpr bool KEEP = kKeepOwn<T, DP>;
+  frag fq[KEEP ? NS : 1], fo[KEEP ? NS : 1];
+  const T* prow = (const T*)a.dout.p + row * a.dout.ld + (int64_t)h * a.dout.hs;
+  const T* qrow = (const T*)a.q.p + row * a.q.ld + (int64_t)h * a.q.hs;
+  const T* orow = (const T*)a.o.p + row * a.o.ld + (int64_t)h * a.o.hs;
+  float delta = 0.f;
+  if constexpr (!KEEP) {
+    for (int s = 0; s < NS; ++s) {
+      fq[0] = own_frag<T, VEC>(orow, has, s, a.D, lane);
+      fo[0] = own_frag<T, VEC>(prow, has, s, a.D, lane);
+      delta += dot_own(fq, fo);
+    }
+    delta = half_sum(delta);
+  } else if constexpr (sizeof(T) == sizeof(G))
+    load_own<T, NS, VEC>(fo, prow, has, a.D, lane);
   else
     round_own(fo, (const G*)a.dout.p + row * a.dout.ld + (int64_t)h * a.dout.hs, copy + (row * a.Hq + h) * a.D, has, a.D, lane);
-  load_own<T, NS, VEC>(fq, (const T*)a.o.p + row * a.o.ld + (int64_t)h * a.o.hs, has, a.D, lane);
-  delta = half_sum(dot_own(fq, fo));
-  load_own<T, NS, VEC>(fq, (const T*)a.q.p + row * a.q.ld + (int64_t)h * a.q.hs, has, a.D, lane);
+  if constexpr (KEEP) {
+    load_own<T, NS, VEC>(fq, orow, has, a.D, lane);
+    delta = half_sum(dot_own(fq, fo));
+    load_own<T, NS, VEC>(fq, qrow, has, a.D, lane);
+  }
   // a row that saw no key (lse -inf) or does not exist has no probabilities: exp2(s - inf) = 0
   const float lse = a.lse[stat], lse2 = has && lse > -INFINITY ? lse * kLog2e : INFINITY;
   const float z0 = INIT ? -lse2 * a.rc : 0.f;
@@ -141,20 +155,25 @@ __global__ __launch_bounds__(256, DP <= (sizeof(T) == 2 ? 128 : 64) ? 2 : 1) voi
         }
       }
       auto fetch = [&](auto I) __attribute__((always_inline)) {
-        if constexpr (I < N1) return row_frag<T, SLOTS>(sk, n, I, lane);
-        else if constexpr (I < N2) return row_frag<T, SLOTS>(sv, n, I - N1, lane);
-        else return Mma<T>::template tr<SLOTS>(sk, n + (I - N2) / NB * Mma<T>::TR, (I - N2) % NB * 32, lane);
+        if constexpr (I < N1) return row_frag<T, SLOTS>(sk, n, I, fresh<FRESH>(lane));
+        else if constexpr (I < N2) return row_frag<T, SLOTS>(sv, n, I - N1, fresh<FRESH>(lane));
+        else return Mma<T>::template tr<SLOTS>(sk, n + (I - N2) / NB * Mma<T>::TR, (I - N2) % NB * 32, fresh<FRESH>(lane));
       };
-      frag ring[RD + 1], own;
+      frag ring[RD + 1], own, mine[KEEP ? 1 : OD + 1];
+      auto fetch_own = [&](auto I) __attribute__((always_inline)) {
+        if constexpr (!KEEP && I < N2) mine[I % (OD + 1)] = own_frag<T, VEC>(I < N1 ? qrow : prow, has, I < N1 ? I : I - N1, a.D, lane);
+      };
+      if constexpr (!KEEP) each<OD>(fetch_own);
       each<RD>([&](auto I) __attribute__((always_inline)) { ring[I] = fetch(I); });
       each<N3>([&](auto I) __attribute__((always_inline)) {
         if constexpr (I + RD < N3) ring[(I + RD) % (RD + 1)] = fetch(std::integral_constant<int, I + RD>{});
+        fetch_own(std::integral_constant<int, I + OD>{});
         const frag f = ring[I % (RD + 1)];
         if constexpr (I < N1) {
-          z = Mma<T>::mma(f, fq[I], z);
+          z = Mma<T>::mma(f, KEEP ? fq[KEEP ? I : 0] : mine[KEEP ? 0 : I % (OD + 1)], z);
         } else if constexpr (I < N2) {
           constexpr int i = I - N1;
-          p = Mma<T>::mma(f, fo[i], p);
+          p = Mma<T>::mma(f, KEEP ? fo[KEEP ? i : 0] : mine[KEEP ? 0 : I % (OD + 1)], p);
 #pragma unroll
           for (int k = 16 * i / NS; k < 16 * (i + 1) / NS; ++k)
             z[k] = exp2_fast(INIT ? z[k] * a.c : __fmaf_rn(z[k], a.c, -lse2));
@@ -210,6 +229,7 @@ __global__ __launch_bounds__(256, OCC) void attn_dkv_kernel(AttnArgs a) {
   constexpr int ES = sizeof(T), SLOTS = slots_of(DP * ES), NS = DP * ES / 32, NB = DO / 32, U = 32 / Mma<T>::TR;
   constexpr int TB = BQ * SLOTS * 16;
   constexpr bool INIT = ES == 2;   // S starts from -lse / scale
+  constexpr bool FRESH = ES == 4 ? DP >= 128 : !VEC && DP == 256;
   typedef typename Mma<T>::frag frag;
   __shared__ __attribute__((aligned(1024))) char sq0[TB], sq1[TB], so0[TB], so1[TB];
   __shared__ __attribute__((aligned(16))) float sl[2][BQ], sd[2][BQ];
@@ -244,9 +264,14 @@ __global__ __launch_bounds__(256, OCC) void attn_dkv_kernel(AttnArgs a) {
   const unsigned span = has ? max(hi - lo, 0) : 0;
 
   const int64_t row = kv.beg + j;
-  frag fk[NS], fv[NS];
-  load_own<T, NS, VEC>(fk, (const T*)a.k.p + row * a.k.ld + (int64_t)hk * a.k.hs, has, a.D, lane);
-  load_own<T, NS, VEC>(fv, (const T*)a.v.p + row * a.v.ld + (int64_t)hk * a.v.hs, has, a.D, lane);
+  constexpr bool KEEP = kKeepOwn<T, DP>;
+  frag fk[KEEP ? NS : 1], fv[KEEP ? NS : 1];
+  const T* krow = (const T*)a.k.p + row * a.k.ld + (int64_t)hk * a.k.hs;
+  const T* vrow = (const T*)a.v.p + row * a.v.ld + (int64_t)hk * a.v.hs;
+  if constexpr (KEEP) {
+    load_own<T, NS, VEC>(fk, krow, has, a.D, lane);
+    load_own<T, NS, VEC>(fv, vrow, has, a.D, lane);
+  }
   acc16_t ak[NB], av[NB];
   zero_acc(ak);
   zero_acc(av);
@@ -304,21 +329,26 @@ __global__ __launch_bounds__(256, OCC) void attn_dkv_kernel(AttnArgs a) {
         }
       }
       auto fetch = [&](auto I) __attribute__((always_inline)) {
-        if constexpr (I < N1) return row_frag<T, SLOTS>(sq, x, I, lane);
-        else if constexpr (I < N2) return row_frag<T, SLOTS>(so, x, I - N1, lane);
-        else if constexpr (I < N3) return Mma<T>::template tr<SLOTS>(so, x + (I - N2) / NB * Mma<T>::TR, d0 + (I - N2) % NB * 32, lane);
-        else return Mma<T>::template tr<SLOTS>(sq, x + (I - N3) / NB * Mma<T>::TR, d0 + (I - N3) % NB * 32, lane);
+        if constexpr (I < N1) return row_frag<T, SLOTS>(sq, x, I, fresh<FRESH>(lane));
+        else if constexpr (I < N2) return row_frag<T, SLOTS>(so, x, I - N1, fresh<FRESH>(lane));
+        else if constexpr (I < N3) return Mma<T>::template tr<SLOTS>(so, x + (I - N2) / NB * Mma<T>::TR, d0 + (I - N2) % NB * 32, fresh<FRESH>(lane));
+        else return Mma<T>::template tr<SLOTS>(sq, x + (I - N3) / NB * Mma<T>::TR, d0 + (I - N3) % NB * 32, fresh<FRESH>(lane));
       };
-      frag ring[RD + 1], own;
+      frag ring[RD + 1], own, mine[KEEP ? 1 : OD + 1];
+      auto fetch_own = [&](auto I) __attribute__((always_inline)) {
+        if constexpr (!KEEP && I < N2) mine[I % (OD + 1)] = own_frag<T, VEC>(I < N1 ? krow : vrow, has, I < N1 ? I : I - N1, a.D, lane);
+      };
+      if constexpr (!KEEP) each<OD>(fetch_own);
       each<RD>([&](auto I) __attribute__((always_inline)) { ring[I] = fetch(I); });
       each<N4>([&](auto I) __attribute__((always_inline)) {
         if constexpr (I + RD < N4) ring[(I + RD) % (RD + 1)] = fetch(std::integral_constant<int, I + RD>{});
+        fetch_own(std::integral_constant<int, I + OD>{});
         const frag f = ring[I % (RD + 1)];
         if constexpr (I < N1) {
-          z = Mma<T>::mma(f, fk[I], z);
+          z = Mma<T>::mma(f, KEEP ? fk[KEEP ? I : 0] : mine[KEEP ? 0 : I % (OD + 1)], z);
         } else if constexpr (I < N2) {
           constexpr int i = I - N1;
-          p = Mma<T>::mma(f, fv[i], p);
+          p = Mma<T>::mma(f, KEEP ? fv[KEEP ? i : 0] : mine[KEEP ? 0 : I % (OD + 1)], p);
 #pragma unroll
           for (int k = 16 * i / NS; k < 16 * (i + 1) / NS; ++k)
             z[k] = exp2_fast(INIT ? z[k] * a.c : __fmaf_rn(z[k], a.c, l[INIT ? 0 : k]));
@@ -393,7 +423,7 @@ namespace {
 // us unsplit, in 2 parts 658 + 18 us for their sum, in 4 parts 675 + 26, in 8 706 + 61.
 // 4 x 1024 tokens, 16 heads of 64 (512 workgroups): unsplit 42, in 2 parts 42 + 18.
 int bwd_splits(const AttnArgs& a, bool bf16) {
-  const int parts = a.D <= 128 ? 1 : bf16 ? 2 : (a.D + 63) / 64, queries = bf16 && a.D <= 128 ? 64 : 32;
+  const int parts = a.D <= 128 ? 1 : 2, queries = bf16 && a.D <= 128 ? 64 : 32;
   const int64_t wgs = attn_tiles(a.Tk, a.nseq, a.k_off != nullptr, 1, BK) * a.Hkv * parts;
   const int64_t rows = std::min<int64_t>(a.Tq / a.nseq, a.window ? 2 * (int64_t)a.window + 128 : a.Tq);
   const int64_t tiles = rows * a.G / queries;
@@ -443,13 +473,13 @@ hipError_t launch(AttnArgs a, bool vec, void* ws, hipStream_t stream) {
     if (!vec) {
       if (a.D <= 64) return launch_as<T, G, 64, 64, 32, 2, 1, 32, false>(a, copy, stream);
       if (a.D <= 128) return launch_as<T, G, 128, 128, 32, 1, 1, 32, false>(a, copy, stream);
-      return launch_as<T, G, 256, 64, 32, 1, 1, 32, false>(a, copy, stream);
+      return launch_as<T, G, 256, 128, 32, 1, 1, 32, false>(a, copy, stream);
     }
     if (a.D <= 64) return launch_as<T, G, 64, 64, 32, 2, 1, 32, true>(a, copy, stream);
     if (a.D <= 96) return launch_as<T, G, 96, 96, 32, 2, 1, 32, true>(a, copy, stream);
     if (a.D <= 128) return launch_as<T, G, 128, 128, 32, 1, 1, 32, true>(a, copy, stream);
-    if (a.D <= 192) return launch_as<T, G, 192, 64, 32, 1, 1, 32, true>(a, copy, stream);
-    return launch_as<T, G, 256, 64, 32, 1, 1, 32, true>(a, copy, stream);
+    if (a.D <= 192) return launch_as<T, G, 192, 96, 32, 1, 1, 32, true>(a, copy, stream);
+    return launch_as<T, G, 256, 128, 32, 1, 1, 32, true>(a, copy, stream);
   }
 }
 }  // namespace

@@ -14,6 +14,7 @@ constexpr int BM = 128;   // rows of a workgroup: (query, head of the group) pai
 template <typename T, int DP, int BN, bool VEC>
 __global__ __launch_bounds__(256, DP <= (sizeof(T) == 2 ? 128 : 96) ? 2 : 1) void attn_fwd_kernel(AttnArgs a) {
   constexpr int ES = sizeof(T), SLOTS = slots_of(DP * ES), NS = DP * ES / 32, NB = DP / 32, NK = BN / 32;
+  constexpr bool FRESH = ES == 4 ? DP == 256 || (!VEC && DP == 128) : !VEC && DP == 256;
   typedef typename Mma<T>::frag frag;
   constexpr int TB = BN * SLOTS * 16;
   __shared__ __attribute__((aligned(1024))) char sk0[TB], sk1[TB], sv0[TB], sv1[TB];
@@ -73,7 +74,7 @@ __global__ __launch_bounds__(256, DP <= (sizeof(T) == 2 ? 128 : 96) ? 2 : 1) voi
 #pragma unroll
     for (int n = 0; n < NK; ++n)
 #pragma unroll
-      for (int u = 0; u < NS; ++u) z[n] = Mma<T>::mma(row_frag<T, SLOTS>(sk, n * 32, u, lane), fq[u], z[n]);
+      for (int u = 0; u < NS; ++u) z[n] = Mma<T>::mma(row_frag<T, SLOTS>(sk, n * 32, u, fresh<FRESH>(lane)), fq[u], z[n]);
     if (j0 < lo1 || j0 + BN > hi0 || r1 - r0 < BM) {   // some row does not see some key
 #pragma unroll
       for (int n = 0; n < NK; ++n)
@@ -118,7 +119,7 @@ __global__ __launch_bounds__(256, DP <= (sizeof(T) == 2 ? 128 : 96) ? 2 : 1) voi
         const frag p = Mma<T>::pack(z[n], u);
 #pragma unroll
         for (int b = 0; b < NB; ++b)
-          acc[b] = Mma<T>::mma(Mma<T>::template tr<SLOTS>(sv, n * 32 + u * Mma<T>::TR, b * 32, lane), p, acc[b]);
+          acc[b] = Mma<T>::mma(Mma<T>::template tr<SLOTS>(sv, n * 32 + u * Mma<T>::TR, b * 32, fresh<FRESH>(lane)), p, acc[b]);
       }
   };
   if (t0 < t1) request(sk0, sv0, t0);
