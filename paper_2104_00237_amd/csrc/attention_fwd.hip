@@ -1,5 +1,13 @@
 // Softmax attention, forward: O = softmax(scale Q K^T + mask) V and lse = log sum exp, one pass over
 // the keys with a running maximum and sum (the probabilities never reach memory).
+//
+// Bound by instruction issue.  Of 32 rows and 64 keys at width 64 a wavefront has 16 MFMAs (512 cycles)
+// and about 140 vector instructions, 32 of them exponentials at a quarter of the rate (1000 cycles);
+// at width 128 the MFMAs take 1024.  Two wavefronts a SIMD fill each other's gaps; LDS delivers a
+// fragment of a tile to every wavefront for one MFMA (half its rate at width 128).
+// Measured: 16384 tokens, 16/4 heads of 128, causal 1.03 ms, 1.07 PFLOP/s (a library product of
+// 16384^3: 1.33), MFMAs busy 58 % of the time; 4 x 1024 tokens, 16 heads of 64, causal 22 us; fp32,
+// 16 ragged sequences, 12 heads of 80: 123 us, 65 TFLOP/s (a library product of 8192^3: 154).
 
 #include "attention.h"
 
@@ -147,7 +155,7 @@ __global__ __launch_bounds__(256, DP <= (sizeof(T) == 2 ? 128 : 96) ? 2 : 1) voi
 
 // Joins the splits of a row: O = sum_s 2^(m_s - m) O_s / sum_s 2^(m_s - m) l_s.  A wavefront a row: its
 // lanes hold the splits' statistics (at most 64), then columns; the splits' loads do not wait for
-// each other (8 sequences of one token, 16 splits: 17 -> 5 us).
+// each other (8 sequences of one token, 16 splits: 17 -> 7.5 us).
 template <typename T>
 __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
   const int lane = threadIdx.x & 63;

@@ -8,6 +8,8 @@ of the operand type (bf16 2^-8, fp32 2^-24), g that of the gradients' type, e = 
              subtraction of the maximum or of lse, whose own error is that of a sum of nk terms:
              |dz| <= ez = (D + 4) e scale (|q| . |k|) + 4 e max|z| + (nk + 8) e
              (exp2 is within 2 e relative; log2 e is one rounding of the factor, in the 4 e |z|)
+             In the backward the D sums may start from -lse / scale: each of their partial sums is
+             larger by at most |lse| / scale, so ez grows by (D + 4) e |lse|.
   P          relative error rp = 2 ez (numerator and row sum), then one rounding u as an operand
              (0 in fp32, where the operand is the value)
   o          |do| <= (rp + u + (nk + 4) e) (P @ |v|) + u |o|
@@ -60,6 +62,7 @@ def forward(q, k, v, ok, scale, dtype):
 def backward(q, k, v, do, ok, scale, dtype, grad_dtype):
     """One head: (dq, dk, dv) and their bounds."""
     o, lse, bo, _, (p, rp) = forward(q, k, v, ok, scale, dtype)
+    rp = rp + 2 * (q.shape[1] + 4) * E * torch.where(ok.any(1), lse, 0.0).abs()[:, None]
     q, k, v, do = q.double(), k.double(), v.double(), do.double()
     nk, D = k.shape
     nq = q.shape[0]
