@@ -776,7 +776,7 @@ typedef struct of_attn_desc {
   int64_t ldk, hsk;      /* layout of k and dk */
   int64_t ldv, hsv;      /* layout of v and dv */
   int64_t ldo, hso;      /* layout of o and dout */
-  float scale;           /* 0 means 1 / sqrt(D) */
+  float scale;           /* 0 means 1 / sqrt(D); else 2^-100 .. 2^100 */
   const int32_t *q_off, *k_off, *q_len, *k_len;
 } of_attn_desc;
 

@@ -454,7 +454,8 @@ struct RotaryArgs {
   float mscale, sign;              // factors of the cosines and the sines
   double w[kRotMax / 2];           // turns per position of each pair
 };
-hipError_t rotary_launch(RotaryArgs a, bool bf16, hipStream_t stream);
+bool rotary_rows(RotaryArgs& a, bool bf16);   // sets rows; whether 16-byte accesses are aligned
+hipError_t rotary_launch(const RotaryArgs& a, bool bf16, bool vec, hipStream_t stream);
 // A [T, H, D] tensor: element (t, h, d) is p[t * ld + h * hs + d].
 struct HeadRows {
   void* p;

@@ -11,6 +11,7 @@
 #include <string>
 #include <unordered_map>
 
+#include "attention_seq.h"
 #include "common.h"
 
 using namespace opfuse;
@@ -1159,6 +1160,9 @@ of_status check_heads(const char* name, int64_t T, int64_t H, int64_t D, int64_t
   return OF_OK;
 }
 
+// A launch has fewer than 2^32 threads: workgroups of 256.
+constexpr int64_t kGridMax = 1LL << 24;
+
 bool aligned_to(const void* p, size_t n) { return ((uintptr_t)p) % n == 0; }
 
 of_status check_rotary(const of_rotary_desc* d, const void* x, const int64_t* pos, const void* y, bool inverse,
@@ -1232,7 +1236,10 @@ of_status rotary_entry(const of_rotary_desc* d, const void* x, const int64_t* po
   memset(&a, 0, sizeof(a));
   const of_status st = check_rotary(d, x, pos, y, inverse, &a);
   if (st != OF_OK) return st;
-  return hip_status(rotary_launch(a, d->dtype == OF_BF16, (hipStream_t)stream),
+  const bool bf16 = d->dtype == OF_BF16, vec = rotary_rows(a, bf16);
+  REQUIRE((a.T + a.rows - 1) / a.rows < kGridMax, OF_EUNSUPPORTED, "T must be < 2^24 times the %d rows of a workgroup",
+          a.rows);
+  return hip_status(rotary_launch(a, bf16, vec, (hipStream_t)stream),
                     inverse ? "of_rotary_bwd launch" : "of_rotary_fwd launch");
 }
 
@@ -1251,8 +1258,13 @@ of_status check_attn(const of_attn_desc* d, bool bwd, AttnArgs* a) {
   REQUIRE(d->causal == 0 || d->causal == 1, OF_EINVAL, "causal must be 0 or 1");
   REQUIRE(d->window >= 0, OF_EINVAL, "window must be >= 0 (0: none)");
   REQUIRE(std::isfinite(d->scale) && d->scale >= 0.f, OF_EINVAL, "scale must be finite and >= 0 (0: 1 / sqrt(D))");
-  REQUIRE(d->Tq <= ((1LL << 31) - 1) / d->Hq && d->Tk <= ((1LL << 31) - 1) / d->Hkv, OF_EUNSUPPORTED,
-          "Tq * Hq and Tk * Hkv must be < 2^31");
+  // (lse / scale and scale * log2 e stay finite)
+  REQUIRE(d->scale == 0.f || (d->scale >= 0x1p-100f && d->scale <= 0x1p100f), OF_EUNSUPPORTED,
+          "scale must be 0 or in [2^-100, 2^100]");
+  // (a tile's last row number, up to 128 further, is an int too)
+  constexpr int64_t kRows = (1LL << 31) - 1024;
+  REQUIRE(d->Tq <= kRows / d->Hq && d->Tk <= kRows / d->Hkv, OF_EUNSUPPORTED,
+          "Tq * Hq and Tk * Hkv must be <= 2^31 - 1024");
   REQUIRE(d->nseq <= (1LL << 27) / d->Hq, OF_EUNSUPPORTED, "nseq * Hq must be <= 2^27");
   REQUIRE(d->q_off || d->Tq % d->nseq == 0, OF_EINVAL, "without q_off, Tq must be a multiple of nseq");
   REQUIRE(d->k_off || d->Tk % d->nseq == 0, OF_EINVAL, "without k_off, Tk must be a multiple of nseq");
@@ -1279,6 +1291,10 @@ of_status check_attn(const of_attn_desc* d, bool bwd, AttnArgs* a) {
   a->rc = (float)(1.0 / ((double)a->scale * 1.4426950408889634));
   a->dG = make_fastdiv((uint32_t)a->G);
   a->nsplit = 1;
+  // tiles of 128 rows; dK and dV in two parts of the columns
+  REQUIRE(attn_tiles(a->Tq, a->nseq, a->q_off, a->G, 128) * a->Hkv < kGridMax &&
+              (!bwd || attn_tiles(a->Tk, a->nseq, a->k_off, 1, 128) * a->Hkv * 2 < kGridMax),
+          OF_EUNSUPPORTED, "more than 2^24 workgroups: Tq * Hq / 128 + nseq * Hkv (backward: Tk * Hkv / 64 + 2 nseq * Hkv)");
   return OF_OK;
 }
 

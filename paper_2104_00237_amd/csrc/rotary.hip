@@ -123,7 +123,7 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
   }
 }
 
-hipError_t rotary_launch(RotaryArgs a, bool bf16, hipStream_t stream) {
+bool rotary_rows(RotaryArgs& a, bool bf16) {
   const int V = bf16 ? 8 : 4, es = bf16 ? 2 : 4;
   auto lines = [&](const void* p, int64_t ld, int64_t hs) {
     return aligned16(p) && ld * es % 16 == 0 && hs * es % 16 == 0;
@@ -132,6 +132,10 @@ hipError_t rotary_launch(RotaryArgs a, bool bf16, hipStream_t stream) {
                    lines(a.y, a.ldy, a.hsy);
   const int per = a.H * ((vec ? (a.interleaved ? a.rot : a.rot / 2) / V : a.rot / 2) + (a.D - a.rot) / (vec ? V : 1));
   a.rows = (int)std::max<int64_t>(1, std::min<int64_t>({8, ROT_LDS / (a.rot / 2), 1024 / std::max(per, 1)}));
+  return vec;
+}
+
+hipError_t rotary_launch(const RotaryArgs& a, bool bf16, bool vec, hipStream_t stream) {
   const dim3 grid((unsigned)((a.T + a.rows - 1) / a.rows));
   auto go = [&](auto* kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, a); };
   if (bf16) {

@@ -45,6 +45,7 @@ def test_rotary(fn):
     bad(L.OF_EUNSUPPORTED, D=600, rot=600)
     bad(L.OF_EUNSUPPORTED, T=1 << 31)
     bad(L.OF_EUNSUPPORTED, H=1 << 20)
+    bad(L.OF_EUNSUPPORTED, T=1 << 24, H=256)    # one row a workgroup: 2^32 threads
     bad(L.OF_EUNSUPPORTED, ldx=1 << 23)
     bad(L.OF_EALIGN, x=FAKE + 2)
     bad(L.OF_EALIGN, y=FAKE + 1, dtype=L.OF_BF16)
@@ -71,7 +72,18 @@ BAD = [(L.OF_EINVAL, dict(Tq=0)), (L.OF_EINVAL, dict(Tk=0)), (L.OF_EINVAL, dict(
        (L.OF_EUNSUPPORTED, dict(nseq=1 << 26, Tq=1 << 26, Tk=1 << 26)), (L.OF_EINVAL, dict(Tq=65)),
        (L.OF_EINVAL, dict(Tk=65)), (L.OF_EALIGN, dict(q_off=FAKE + 2)), (L.OF_EALIGN, dict(k_len=FAKE + 1)),
        (L.OF_EINVAL, dict(ldq=63)), (L.OF_EINVAL, dict(hsk=63)), (L.OF_EINVAL, dict(ldv=100)),
-       (L.OF_EINVAL, dict(ldo=64, hso=64 * 63)), (L.OF_EUNSUPPORTED, dict(ldo=(1 << 22) + 8))]
+       (L.OF_EINVAL, dict(ldo=64, hso=64 * 63)), (L.OF_EUNSUPPORTED, dict(ldo=(1 << 22) + 8)),
+       (L.OF_EUNSUPPORTED, dict(scale=2.0 ** -101)), (L.OF_EUNSUPPORTED, dict(scale=2.0 ** 101)),
+       # a launch has fewer than 2^32 threads; the last tile's row numbers are ints
+       (L.OF_EUNSUPPORTED, dict(nseq=1 << 23, Tq=1 << 23, Tk=1 << 23)),
+       (L.OF_EUNSUPPORTED, dict(nseq=1, Hq=1, Hkv=1, Tk=(1 << 31) - 512))]
+
+
+def test_attention_backward_workgroups():
+    d = attn(nseq=1, Hq=1, Hkv=1, Tk=1 << 30)      # two column parts of 2^23 tiles of keys
+    assert L.of_attn_workspace_size(d, L.OF_ATTN_FWD) > 0
+    assert L.of_attn_workspace_size(d, L.OF_ATTN_BWD) == 0
+    assert "workgroups" in L.of_last_error()
 
 
 @pytest.mark.parametrize("want,kw", BAD, ids=str)
