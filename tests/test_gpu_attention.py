@@ -66,10 +66,11 @@ class Call:
             self.ws[op] = (torch.full((max(n, 16) // 4,), PAD, device=gpu), n)
 
     def place(self, x, layout, shift):
-        """x on the device: rows of heads, heads behind each other, rows with a gap; `shift` elements
-        off the allocation's alignment."""
+        """x on the device: rows of heads, heads behind each other, rows with a gap, rows or heads so far
+        apart that offsets pass 32 bits; `shift` elements off the allocation's alignment."""
         T, H, D = x.shape
-        ld, hs = {"rows": (H * D, D), "heads": (D, T * D), "gap": (H * D + 8, D), "odd": (H * D + 3, D)}[layout]
+        ld, hs = {"rows": (H * D, D), "heads": (D, T * D), "gap": (H * D + 8, D), "odd": (H * D + 3, D),
+                  "wide": (1 << 21, D), "far": (D, (1 << 31) + 64)}[layout]
         size = (T - 1) * ld + (H - 1) * hs + D + shift
         flat = torch.zeros(size, dtype=x.dtype, device=self.gpu)
         y = flat[shift:].as_strided((T, H, D), (ld, hs, 1))
@@ -158,6 +159,15 @@ def test_head_widths(gpu, dtype, D):
 def test_layouts(gpu, dtype, layout, shift):
     for D in (64, 36):
         Call([66, 80], [66, 80], Hq=4, Hkv=2, D=D, dtype=dtype, causal=1, layout=layout, shift=shift).fwd().bwd().check()
+
+
+@pytest.mark.parametrize("dtype,layout,shift", [("bf16", "wide", 0), ("bf16", "wide", 1), ("bf16", "far", 0), ("f32", "far", 0)])
+def test_offsets_past_32_bits(gpu, dtype, layout, shift):
+    """Row 1024 of rows 2^21 elements apart is 2^31 elements on; head 1 of heads 2^31 apart."""
+    c = Call([3, 1090], [3, 1090], Hq=2, Hkv=2, D=64, dtype=dtype, causal=1, window=200, layout=layout, shift=shift)
+    c.fwd().bwd().check()
+    del c
+    torch.cuda.empty_cache()
 
 
 @pytest.mark.parametrize("Hq,Hkv", [(1, 1), (6, 2), (7, 1), (8, 8), (16, 2), (130, 1)])

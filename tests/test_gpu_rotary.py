@@ -129,6 +129,27 @@ def test_far_and_negative_positions(gpu):
     run(gpu, 7, 2, 64, 64, 0, "f32", pos=pos)
 
 
+@pytest.mark.parametrize("ld,hs", [(1 << 21, 64), (64, (1 << 31) + 64)], ids=["rows", "heads"])
+def test_offsets_past_32_bits(gpu, ld, hs):
+    """Rows or heads so far apart that offsets pass 32 bits give what a contiguous call gives."""
+    T, H, D = 1100, 2, 64
+    x = torch.randn(T, H, D, device=gpu).to(torch.bfloat16)
+    y = torch.empty_like(x)
+    far = [torch.empty((T - 1) * ld + (H - 1) * hs + D, dtype=x.dtype, device=gpu).as_strided((T, H, D), (ld, hs, 1))
+           for _ in range(2)]
+    far[0].copy_(x)
+    d = L.OfRotaryDesc(T=T, H=H, D=D, rot=D, dtype=L.OF_BF16, base=10000.0)
+    w = L.OfRotaryDesc(T=T, H=H, D=D, rot=D, dtype=L.OF_BF16, base=10000.0, ldx=ld, hsx=hs, ldy=ld, hsy=hs)
+    s = torch.cuda.current_stream().cuda_stream
+    L.of_rotary_fwd(d, x.data_ptr(), None, y.data_ptr(), s)
+    L.of_rotary_fwd(w, far[0].data_ptr(), None, far[1].data_ptr(), s)
+    torch.cuda.synchronize()
+    assert torch.equal(far[1].contiguous(), y)
+    assert torch.equal(far[0].contiguous(), x)
+    del far
+    torch.cuda.empty_cache()
+
+
 def test_turns_back(gpu):
     """The backward of the forward's output is the input again (a turn is orthogonal): two turns' bounds."""
     t, kind, half = TYPES["f32"]
