@@ -67,7 +67,7 @@ __device__ __forceinline__ float dot_own(const afloatx4_t (&a)[NS], const afloat
 }  // namespace
 
 // delta and dQ: own rows are queries (all heads of a key head's group), keys stream.  copy: dO rounded
-// to T when it is stored in another type, [Tq, Hq, D].
+// to T when it is stored in another type (copy_strides).
 template <typename T, typename G, int DP, int BN, int RD, bool VEC>
 __global__ __launch_bounds__(256, DP <= (sizeof(T) == 2 ? 128 : 64) ? 2 : 1) void attn_dq_kernel(AttnArgs a, T* copy) {
   constexpr int ES = sizeof(T), SLOTS = slots_of(DP * ES), NS = DP * ES / 32, NB = DP / 32, NK = BN / 32, U = 32 / Mma<T>::TR;
@@ -120,7 +120,7 @@ __global__ __launch_bounds__(256, DP <= (sizeof(T) == 2 ? 128 : 64) ? 2 : 1) voi
   } else if constexpr (sizeof(T) == sizeof(G))
     load_own<T, NS, VEC>(fo, prow, has, a.D, lane);
   else
-    round_own(fo, (const G*)a.dout.p + row * a.dout.ld + (int64_t)h * a.dout.hs, copy + (row * a.Hq + h) * a.D, has, a.D, lane);
+    round_own(fo, (const G*)a.dout.p + row * a.dout.ld + (int64_t)h * a.dout.hs, copy + stat * a.D, has, a.D, lane);
   if constexpr (KEEP) {
     load_own<T, NS, VEC>(fq, orow, has, a.D, lane);
     delta = half_sum(dot_own(fq, fo));
@@ -450,7 +450,10 @@ hipError_t launch_as(AttnArgs a, T* copy, hipStream_t stream) {
   hipLaunchKernelGGL((attn_dq_kernel<T, G, DP, BN, sizeof(T) == 2 && DP == 64 ? 2 : 1, VEC>), dim3((unsigned)nq), dim3(256), 0, stream, a, copy);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if (copy) a.dout = HeadRows{copy, (int64_t)a.Hq * a.D, a.D};
+  if (copy) {
+    a.dout.p = copy;
+    copy_strides(a.Tq, a.D, a.dout.ld, a.dout.hs);
+  }
   const int64_t nk = attn_tiles(a.Tk, a.nseq, a.k_off != nullptr, 1, BK) * (DP / DO) * a.Hkv * a.nsplit;
   hipLaunchKernelGGL((attn_dkv_kernel<T, G, DP, DO, BQ, RD, OCC, VEC>), dim3((unsigned)nk), dim3(256), 0, stream, a);
   e = hipGetLastError();

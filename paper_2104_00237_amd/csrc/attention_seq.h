@@ -16,6 +16,19 @@ namespace opfuse {
 
 OF_HD int64_t clamp64(int64_t x, int64_t lo, int64_t hi) { return x < lo ? lo : x > hi ? hi : x; }
 
+// Row strides are at most this many elements: a tile's loads count bytes from its first row in 32 bits
+// (64 rows of 2-byte or 32 of 4-byte elements: below 2^30), and columns behind the width are sent to
+// offset 2^31, which has to lie behind the tile's last row.
+constexpr int64_t kRowStrideMax = 1LL << 22;
+
+// Strides of dO's rounded copy in a backward's workspace: head after head, so that the row stride does
+// not grow with the heads (with rows of all heads, H D = 2^26 would wrap the loads' 32 bits at row 32).
+// Row t of head h is row h T + t, as in the row statistics.
+OF_HD void copy_strides(int64_t T, int D, int64_t& ld, int64_t& hs) {
+  ld = D;
+  hs = T * D;
+}
+
 // Rows [beg, beg + len) of a sequence.  Offsets and lengths come from device memory the host has
 // not seen: whatever they hold, the result lies inside [0, T).
 struct SeqRows {

@@ -1153,7 +1153,7 @@ of_status check_heads(const char* name, int64_t T, int64_t H, int64_t D, int64_t
   if (*ld == 0) *ld = H * D;
   REQUIRE(*ld >= D && *hs >= D, OF_EINVAL, "%s: row stride %lld and head stride %lld must be 0 or >= D", name,
           (long long)*ld, (long long)*hs);
-  REQUIRE(*ld <= (1LL << 22) && *hs <= (1LL << 40), OF_EUNSUPPORTED,
+  REQUIRE(*ld <= kRowStrideMax && *hs <= (1LL << 40), OF_EUNSUPPORTED,
           "%s: row stride must be <= 2^22 and head stride <= 2^40", name);
   REQUIRE(*ld >= (__int128)(H - 1) * *hs + D || *hs >= (__int128)(T - 1) * *ld + D, OF_EINVAL,
           "%s: rows overlap (row stride %lld, head stride %lld)", name, (long long)*ld, (long long)*hs);
