@@ -411,8 +411,8 @@ def median_step_ms(torch, cfg, ordering, batches, warmup, steps):
     return float(np.median([evs[t].elapsed_time(evs[t + 1]) for t in range(steps)]))
 
 
-STAGES = {"forward": ("fwd", "fwd_ff", "loss"),
-          "backward": ("dgrad", "wgrad", "wgrad_bf", "ln_bwd", "add"),
+STAGES = {"forward": ("fwd", "fwd_ff", "attn", "loss"),
+          "backward": ("dgrad", "wgrad", "wgrad_bf", "ln_bwd", "attn_bwd", "add"),
           "optimizer": ("opt", "clip")}
 
 
