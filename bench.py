@@ -163,8 +163,7 @@ def tblock_launches(cfg):
     """Per-launch costs of the bf16 Transformer blocks.  Contractions take bf16
     operands: the weight is read as its 2-byte shadow, activations and
     gradients as fp32; the fused update also rewrites the shadow.  LayerNorm
-    and the residual adds count as `extra` bytes of their block; attention (its
-    launches are classes of their own) is not counted."""
+    and the residual adds count as `extra` bytes of their block."""
     M, d, f, nb = cfg["batch"], cfg["hidden"], cfg["ffn"], cfg["blocks"]
     h = n_state(cfg["opt"])
     G = min(64, max(1, (M + 63) // 64))
@@ -188,6 +187,8 @@ def tblock_launches(cfg):
                 wgrad_bf=(fl, yb + xb + upd_w + upd_b),
                 extra=0,
             ))
+        if cfg.get("attention"):
+            out.append(attention_launches(cfg, p))
         for name in ("ln1", "ln2"):
             md = 4 * M * d
             # fwd R x W y, mean, rstd; bwd R dy, x, dres W dx (+ the parameter pass
@@ -197,6 +198,29 @@ def tblock_launches(cfg):
                             fwd=None, fwd_ff=None, dgrad=None, wgrad=None, wgrad_bf=None,
                             extra=extra))
     return out
+
+
+def attention_launches(cfg, p):
+    """A block's attention, rotary positions included: forward and gradient (`dgrad`).
+    2 and 5 products of 2 D flops for each pair of a query and a key it sees (what
+    the gradient has to compute, not the 7 its two kernels do).  Q, K, V and the
+    output are read and written as they are stored (bf16 in the bf16 blocks), the
+    gradients in fp32; rotary positions are turned in place."""
+    a, M, d = cfg["attention"], cfg["batch"], cfg["hidden"]
+    H, L, D, w = a["heads"], a["seq_len"], d // a["heads"], a.get("window", 0) or a["seq_len"]
+    pairs = sum(min(L, i + 1 if a["causal"] else i + w) - max(0, i - w + 1) for i in range(L))
+    product = 2 * pairs * (M // L) * H * D
+    es = 2 if cfg["dtype"] == "bf16" else 4
+    qkv, o, stats = M * qkv_width(cfg), M * d, 4 * M * H
+    turned, turns = 0, 0
+    if a.get("rope"):
+        turned = 2 * M * (H + a["kv_heads"]) * D
+        turns = 3 * M * (H + a["kv_heads"]) * a["rope"]["rot"]
+    return dict(name=p + "attn", kind="attn", M=M, N=d, K=0, nparams=0, dtype=cfg["dtype"],
+                fwd=(2 * product + turns, es * (qkv + o + turned) + stats),
+                fwd_ff=(2 * product + turns, es * (qkv + o + turned) + stats),
+                dgrad=(5 * product + turns, es * (qkv + o) + 4 * (o + qkv + turned) + stats),
+                wgrad=None, wgrad_bf=None, extra=0)
 
 
 def mbv2_launches(cfg):
