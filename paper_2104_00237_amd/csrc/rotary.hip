@@ -72,9 +72,14 @@ __global__ __launch_bounds__(256) void rotary_kernel(RotaryArgs a) {
     const int64_t t = t0 + r;
     const double pos = a.pos ? (double)a.pos[t] : (double)(a.pos0 + t % a.seq_len);
     const double turns = pos * a.w[k];
+    // half turns in [-1, 1], and what their rounding to fp32 leaves (at most pi 2^-25 = 1.6 half steps of 1,
+    // as much as everything else in an element): to first order, its square is below 1e-14
+    const double x = 2.0 * (turns - rint(turns));
+    const float near = (float)x, rest = (float)(x - near) * 3.14159265f;
     float s, c;
-    sincospif((float)(2.0 * (turns - rint(turns))), &s, &c);
-    cs[i] = make_float2(c * a.mscale, s * a.sign);   // sign: +-mscale
+    sincospif(near, &s, &c);
+    // sign: +-mscale
+    cs[i] = make_float2(__fmaf_rn(-s, rest, c) * a.mscale, __fmaf_rn(c, rest, s) * a.sign);
   }
   __syncthreads();
   // items of a head: turned pieces (V pairs in the half layout, V elements of neighbouring pairs,
