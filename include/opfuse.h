@@ -726,7 +726,8 @@ typedef struct of_rotary_desc {
   int64_t ldx, hsx;     /* layout of x and dx */
   int64_t ldy, hsy;     /* layout of y and dy */
   double base;          /* e.g. 10000 */
-  double factor, orig_len, low_turns, high_turns;   /* of the scaling; others ignored */
+  double factor, orig_len, low_turns, high_turns;   /* of the scaling; others ignored (frequencies that leave
+                                                       float64, times any position too, are refused) */
   float mscale;         /* factor of the turned elements; 0 means 1 */
 } of_rotary_desc;
 

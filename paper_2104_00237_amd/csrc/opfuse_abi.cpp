@@ -1225,6 +1225,9 @@ of_status check_rotary(const of_rotary_desc* d, const void* x, const int64_t* po
           std::min(1.0, std::max(0.0, (d->orig_len * w / kTurn - d->low_turns) / (d->high_turns - d->low_turns)));
       w = keep * w + (1.0 - keep) * w / d->factor;
     }
+    // (a small factor can take them past float64, times a position too: the turn would be a NaN)
+    REQUIRE(std::isfinite(w * 0x1p63), OF_EINVAL, "frequencies must be finite, also times 2^63 (base %g, factor %g)",
+            d->base, d->factor);
     a->w[i] = w / kTurn;
   }
   return OF_OK;
