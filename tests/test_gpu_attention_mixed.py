@@ -50,3 +50,38 @@ def test_heads_behind_each_other(gpu):
     assert sum(int(x.count_nonzero()) for x in dq.split(1 << 16)) == moved
     del q, o, do, dq, ws
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("layout,shift", [("rows", 0), ("heads", 0), ("odd", 1)])
+@pytest.mark.parametrize("D", [64, 96, 128, 192, 256])
+def test_split_over_the_queries(gpu, D, layout, shift):
+    """dK and dV in parts, from the copy of dO: few key tiles, many queries."""
+    c = Call([1200, 40], [300, 40], Hq=4, Hkv=1, D=D, grad="f32", causal=1, tail=2, layout=layout, shift=shift)
+    kept = 4 * (4 * c.Tq + 3) + 2 * 4 * c.Tq * D + 15      # statistics and the copy
+    assert c.ws[L.OF_ATTN_BWD][1] > kept
+    c.fwd().bwd().check()
+
+
+def test_split_with_padded_slots(gpu):
+    """Rows behind a length hold NaN, in dO too: they are neither copied nor summed."""
+    c = Call([1100, 0, 700], [260, 7, 90], Hq=4, Hkv=1, D=64, grad="f32", causal=1, slots=True)
+    assert c.ws[L.OF_ATTN_BWD][1] > 4 * (4 * c.Tq + 3) + 2 * 4 * c.Tq * 64 + 15
+    c.fwd().bwd().check()
+
+
+def test_as_a_training_step_calls_it(gpu):
+    """The full-size block: 4 sequences of 1024, 16/4 heads of 64, Q, K and V in packed rows and their
+    gradients in packed fp32 rows; dK and dV in parts, delta from O (more than 256 keys)."""
+    T, Hq, Hkv, D = 4096, 16, 4, 64
+    c = Call([1024] * 4, [1024] * 4, Hq=Hq, Hkv=Hkv, D=D, grad="f32", causal=1)
+    qkv = torch.cat([c.q, c.k, c.v], 1)
+    grads = torch.full((T, Hq + 2 * Hkv, D), 7.0, device=gpu)
+    parts = (slice(0, Hq), slice(Hq, Hq + Hkv), slice(Hq + Hkv, None))
+    c.q, c.k, c.v = (qkv[:, p] for p in parts)
+    c.dq, c.dk, c.dv = (grads[:, p] for p in parts)
+    c.d.ldq = c.d.ldk = c.d.ldv = (Hq + 2 * Hkv) * D
+    c.d.q_off = c.d.k_off = None
+    need = L.of_attn_workspace_size(c.d, L.OF_ATTN_BWD)
+    assert need > 4 * Hq * T + 2 * Hq * T * D
+    c.ws[L.OF_ATTN_BWD] = (torch.full((need // 4,), float("nan"), device=gpu), need)
+    c.fwd().bwd().check()
