@@ -321,8 +321,11 @@ def describe_layers(cfg):
                 f"(1x1 expand, depthwise 3x3, 1x1 project), 1x1 head {cfg['head']}, avg-pool, "
                 f"linear classifier; {cfg['image']}x{cfg['image']} input")
     if cfg["kind"] == "tblock":
+        a = cfg.get("attention")
+        att = (f", {'causal ' if a['causal'] else ''}attention {a['heads']}/{a['kv_heads']} heads over "
+               f"{a['seq_len']} rows") if a else ""
         return (f"{cfg['blocks']} pre-LN blocks, hidden {cfg['hidden']}, FFN {cfg['ffn']}, "
-                f"bf16 operands")
+                f"bf16 operands{att}")
     if cfg["kind"] == "mlp":
         return f"{len(cfg['dims']) - 1} linear, width {cfg['dims'][1]}"
     return (f"{len(cfg['channels'])} conv3x3 ({','.join(map(str, cfg['channels']))}), "

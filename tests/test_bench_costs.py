@@ -6,7 +6,7 @@ import re
 import pytest
 
 import bench
-from workloads import reduced_config
+from workloads import get_config, reduced_config
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
@@ -57,3 +57,8 @@ def test_a_step_with_attention_costs_its_products_and_rows(att, ordering):
         moved += 2 * turned * 2 + 2 * turned * 4                  # in place: bf16, then the fp32 gradients
     assert f1 - f0 == cfg["blocks"] * flops
     assert b1 - b0 == cfg["blocks"] * moved
+
+
+def test_the_record_names_the_attention():
+    assert "causal attention 16/4 heads over 1024 rows" in bench.describe_layers(get_config("attn12"))
+    assert "attention" not in bench.describe_layers(get_config("tblock12"))
