@@ -226,8 +226,10 @@ constexpr int OD = 4;
 
 // A lane number, with FRESH one that the compiler knows nothing of: a fragment's LDS addresses are then
 // computed where it is read instead of held in registers by the dozen.  For the kernels that spill
-// otherwise (forward, fp32, width 256: 903 -> 409 us; backward 4275 -> 2006); where they do not it
-// costs (forward, fp32, width 128: 163 -> 207 us; bf16, 256: 67 -> 95).
+// most otherwise (forward, fp32, width 256: 903 -> 409 us; backward 4275 -> 2006); elsewhere it
+// costs (forward, fp32, width 128: 163 -> 207 us; bf16, 256: 67 -> 95).  Registers that spill all the same:
+// forward 17 (bf16, 256), 36 (fp32, 192), 11 (bf16, 128, not VEC); dQ 50 (bf16, 256) and 355 with fp32
+// gradients (733 and 829 us traced: 4096 tokens, 16/4 heads), not VEC 24 (fp32, 256), 26 and 134 (bf16, 256), 61 (bf16, 128).
 template <bool FRESH>
 __device__ __forceinline__ int fresh(int lane) {
   if constexpr (FRESH) asm volatile("" : "+v"(lane));

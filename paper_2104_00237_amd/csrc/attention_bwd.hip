@@ -11,11 +11,13 @@
 // Accumulators start from what would be subtracted from them: S from -lse / scale (bf16 operands; for
 // fp32 operands that would round at lse's size) and dP from -delta, and masked elements from
 // -infinity, so that P = exp2(c S) and dS = P dP.
-
-// Measured: 8192 tokens, 16/4 heads of 128, causal 0.98 ms (700 TFLOP/s of the five products; dQ 410 us
-// with its three products at 1.0 PFLOP/s, dK and dV 660 us with their four at 0.83); 4 x 1024 tokens, 16
-// heads of 64 59 us; fp32, window 512, 8/4 heads of 64 253 us.  A step costs its MFMAs, its fragments'
-// LDS reads and, in dK and dV, a share of 28 vector cycles for each of 16 elements.
+//
+// Measured, whole calls: 8192 tokens, 16/4 heads of 128, causal 0.98 to 1.00 ms (690 TFLOP/s of the five
+// products); 4 x 1024 tokens, 16 heads of 64 59 us, 16/4 heads 67 us and with fp32 gradients 85 us; fp32,
+// window 512, 8/4 heads of 64 253 us.  Launch by launch, in a kernel trace that adds up to a tenth: the
+// first of these dQ 397 us, dK and dV 666, their sum 16; the 85 us dQ 47 (dO is read and its copy written
+// element by element), dK and dV 35, their sum 9.  A step costs its MFMAs, its fragments' LDS reads and,
+// in dK and dV, a share of 28 vector cycles for each of 16 elements.
 
 #include "attention.h"
 
@@ -427,7 +429,7 @@ __global__ __launch_bounds__(256) void attn_sum_kernel(AttnArgs a) {
 
 namespace {
 // Splits of the queries that stream past a key tile (128 keys): where the key tiles are fewer than two
-// workgroups a CU, at least eight tiles of queries (of an average sequence) in each.  Measured: 8192
+// workgroups a CU, at least eight tiles of queries (of an average sequence) in each.  Measured (traced): 8192
 // tokens, 16/4 heads of 128 (256 workgroups, the causal mask's longest twice the mean): dK and dV 1450
 // us unsplit, in 2 parts 658 + 18 us for their sum, in 4 parts 675 + 26, in 8 706 + 61.
 // 4 x 1024 tokens, 16 heads of 64 (512 workgroups): unsplit 42, in 2 parts 42 + 18.

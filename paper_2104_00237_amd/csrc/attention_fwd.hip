@@ -2,12 +2,15 @@
 // the keys with a running maximum and sum (the probabilities never reach memory).
 //
 // Bound by instruction issue.  Of 32 rows and 64 keys at width 64 a wavefront has 16 MFMAs (512 cycles)
-// and about 140 vector instructions, 32 of them exponentials at a quarter of the rate (1000 cycles);
-// at width 128 the MFMAs take 1024.  Two wavefronts a SIMD fill each other's gaps; LDS delivers a
+// and, where nothing is masked, about 200 vector instructions, 32 of them exponentials at a quarter of
+// the rate (1200 cycles); at width 128 the MFMAs take 1024.  Counted over whole kernels, MFMAs, masks,
+// entry and exit included: 189 a tile for 16384 tokens of width 128, 257 for 4 x 1024 of width 64, where
+// a wavefront has nine tiles on average.  Two wavefronts a SIMD fill each other's gaps; LDS delivers a
 // fragment of a tile to every wavefront for one MFMA (half its rate at width 128).
-// Measured: 16384 tokens, 16/4 heads of 128, causal 1.03 ms, 1.07 PFLOP/s (a library product of
-// 16384^3: 1.33), MFMAs busy 58 % of the time; 4 x 1024 tokens, 16 heads of 64, causal 22 us; fp32,
-// 16 ragged sequences, 12 heads of 80: 123 us, 65 TFLOP/s (a library product of 8192^3: 154).
+// Measured, whole calls (a kernel trace adds up to a tenth): 16384 tokens, 16/4 heads of 128, causal
+// 1.03 to 1.06 ms, 1.05 PFLOP/s (a library product of 16384^3: 1.33), MFMAs busy 58 % of the time; 4 x 1024
+// tokens, 16 heads of 64, causal 22 us; fp32, 16 ragged sequences, 12 heads of 80: 123 us, 65 TFLOP/s
+// (a library product of 8192^3: 154).
 
 #include "attention.h"
 
@@ -203,6 +206,9 @@ namespace {
 // twice, at least 512 keys (of an average sequence) in each and only from 2048 on: joining costs about
 // 7 us, the time of 8 tiles of 64 keys.  Measured: 8 sequences of one token, up to 8192 keys, 16/4 heads
 // (32 workgroups): 28 us in 16 parts, 34 in 32; 1024 queries of 16 heads: 25 us in 4 parts, 21 unsplit.
+// The rule sees the slots, not a window: then the window's tiles alone are shared out, and some parts
+// may have none.  8 sequences of one token in slots of 8192, causal window of 64 / 512 / 1024 / 2000 keys: 14
+// / 14 / 14 / 16 us in 16 parts, 8 / 18 / 29 / 51 us unsplit.
 int splits(const AttnArgs& a) {
   const int64_t wgs = attn_tiles(a.Tq, a.nseq, a.q_off != nullptr, a.G, BM) * a.Hkv;
   const int64_t keys = a.Tk / a.nseq;
