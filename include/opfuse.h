@@ -803,6 +803,92 @@ of_status of_attn_bwd(const of_attn_desc* d, const void* q, const void* k, const
                       const float* lse, const void* dout, void* dq, void* dk, void* dv, void* ws,
                       size_t ws_bytes, void* stream);
 
+/* ------------------------------------------------------ vocabulary losses */
+
+/*
+ * Losses of an output head over a large vocabulary (support operators: the paper defines none), which
+ * take the rows X [M, K] (row stride ldx) and the head W [V, K] and never keep the logits s = X W^T:
+ * the forward keeps a few numbers a row, the backward computes the logits again, a piece of the
+ * vocabulary at a time.  z = s, or softcap * tanh(s / softcap).
+ *
+ * Cross-entropy (of_vocab_xent_*): a label a row (int64 [M]); a negative one: the row does not count.
+ *   lse_m = log sum_v exp z_mv,  loss_m = lse_m - z_{m, label} + z_loss * lse_m^2
+ * Distillation (of_vocab_distill_*): a row has topk entries, each an id (int64 [M, topk]) and the
+ * teacher's logit t (teacher_dtype [M, topk]); a negative id: no entry, whatever its logit.  With q the
+ * softmax of t / temperature over the row's entries:
+ *   lse_m = log sum_v exp(z_mv / temperature),
+ *   loss_m = temperature^2 sum_j q_mj (log q_mj - z_{m, id_mj} / temperature + lse_m)
+ * A row without an entry, or with logits of -infinity only, does not count.  An id that stands more than
+ * once has the weights of all its entries in the gradient, and a term for each in the loss.
+ *
+ * A row that does not count has loss 0 and gives and gets no gradient, whatever its X holds; its lse is
+ * that of its X.  A label or id >= V makes the row's loss NaN (and the mean); the row counts and gets no
+ * gradient.  A logit of +infinity or NaN makes the row's lse NaN.
+ *
+ * dtype is the type in memory of X and of the head that is read (OF_F32: W->w; OF_BF16: W->w_bf16,
+ * uint16 bit patterns) and of the matrix-core operands; logits, statistics and sums are fp32 or wider.
+ * Any alignment to the elements' size is accepted.
+ */
+typedef struct of_vocab_desc {
+  int64_t M, V, K;        /* rows, vocabulary, width */
+  int64_t ldx;            /* row stride of X and dX; 0 means K; <= 2^21 */
+  int32_t dtype;          /* of_dtype of X and W */
+  int32_t grad_dtype;     /* backward: of_dtype of dX and dW (OF_BF16 only with dtype OF_BF16).  bf16 operands:
+                             the logits' gradient is rounded to bf16 as an operand, also for fp32 gradients */
+  int32_t topk;           /* distillation: entries of a row, 1 .. 1024; cross-entropy: 0 or 1 */
+  int32_t teacher_dtype;  /* distillation: of_dtype of the teacher's logits */
+  float softcap;          /* 0: none */
+  float z_loss;           /* cross-entropy: >= 0; distillation: 0 */
+  float temperature;      /* distillation: > 0, 0 means 1; cross-entropy: 0 or 1 */
+} of_vocab_desc;
+
+typedef enum of_vocab_op { OF_VOCAB_FWD = 0, OF_VOCAB_BWD = 1 /* bwd and bwd_fused */ } of_vocab_op;
+
+/* Bytes of workspace `op` needs for `d` (0 and OF_EINVAL or OF_EUNSUPPORTED in of_last_error() for an
+ * invalid descriptor).  16-byte aligned; its content does not matter. */
+size_t of_vocab_workspace_size(const of_vocab_desc* d, int32_t op);
+
+/*
+ * Forward.  loss, lse: fp32 [M]; zt: fp32 [M] (distillation [M, topk]): z of the label (of the entries), 0
+ * where there is none; mean: fp32 [1] or NULL: the sum of the losses over the number of rows that
+ * count (0 if none does).  lse and zt are kept for the backward.
+ */
+of_status of_vocab_xent_fwd(const of_vocab_desc* d, const void* x, const of_param* W, const int64_t* labels,
+                            float* loss, float* lse, float* zt, float* mean, void* ws, size_t ws_bytes, void* stream);
+of_status of_vocab_distill_fwd(const of_vocab_desc* d, const void* x, const of_param* W, const int64_t* ids,
+                               const void* teacher, float* loss, float* lse, float* zt, float* mean, void* ws,
+                               size_t ws_bytes, void* stream);
+
+/*
+ * Backward of sum_m dloss_m loss_m (dloss: fp32 [M]; NULL: of the mean).  With p = exp(z / T - lse):
+ *   cross-entropy  dz_v = dloss (p_v (1 + 2 z_loss lse) - [v = label])
+ *   distillation   dz_v = dloss T (p_v - sum of the q_j with id_j = v)
+ *   ds = dz (1 - (z / softcap)^2),  dX = ds W,  dW = ds^T X
+ * dx: grad_dtype [M, ldx]; dw: grad_dtype [V, K]; either may be NULL.  accumulate = 1 adds into dw (once
+ * rounded).  Elements of dx behind column K are left as they are.  dx and dw must not overlap an input or
+ * each other.  Deterministic: no sum depends on the order of workgroups.
+ */
+of_status of_vocab_xent_bwd(const of_vocab_desc* d, const void* x, const of_param* W, const int64_t* labels,
+                            const float* lse, const float* zt, const float* dloss, void* dx, void* dw,
+                            int32_t accumulate, void* ws, size_t ws_bytes, void* stream);
+of_status of_vocab_distill_bwd(const of_vocab_desc* d, const void* x, const of_param* W, const int64_t* ids,
+                               const void* teacher, const float* lse, const float* zt, const float* dloss, void* dx,
+                               void* dw, int32_t accumulate, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * Backward-fusion of the head (Section 3 "Backward-Fusion"; Appendix B.2, Alg. 3): dx as above (may be
+ * NULL), and `opt` updates W and its history (W->w, m, v, and w_bf16 when given) with dW (+ gW_partial,
+ * fp32 [V, K] or NULL: a shared head's earlier gradient) in the epilogue of dW's product: dW is never
+ * stored.  dx reads the old W.
+ */
+of_status of_vocab_xent_bwd_fused(const of_vocab_desc* d, const void* x, const of_param* W, const int64_t* labels,
+                                  const float* lse, const float* zt, const float* dloss, const float* gW_partial,
+                                  const of_opt* opt, void* dx, void* ws, size_t ws_bytes, void* stream);
+of_status of_vocab_distill_bwd_fused(const of_vocab_desc* d, const void* x, const of_param* W, const int64_t* ids,
+                                     const void* teacher, const float* lse, const float* zt, const float* dloss,
+                                     const float* gW_partial, const of_opt* opt, void* dx, void* ws, size_t ws_bytes,
+                                     void* stream);
+
 /* ---------------------------------------------------------- measurement */
 
 /*

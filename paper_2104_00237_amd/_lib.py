@@ -95,6 +95,15 @@ class OfAttnDesc(ctypes.Structure):
                 ("k_off", c_void_p), ("q_len", c_void_p), ("k_len", c_void_p)]
 
 
+OF_VOCAB_FWD, OF_VOCAB_BWD = 0, 1
+
+
+class OfVocabDesc(ctypes.Structure):
+    _fields_ = [("M", c_int64), ("V", c_int64), ("K", c_int64), ("ldx", c_int64), ("dtype", c_int32),
+                ("grad_dtype", c_int32), ("topk", c_int32), ("teacher_dtype", c_int32), ("softcap", c_float),
+                ("z_loss", c_float), ("temperature", c_float)]
+
+
 class OpfuseError(RuntimeError):
     def __init__(self, status, fn, msg):
         super().__init__(f"{fn}: {STATUS_NAMES.get(status, status)}: {msg}")
@@ -186,6 +195,17 @@ _SIGS = {
     "of_attn_fwd": (c_int32, [P(OfAttnDesc), c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
                               c_void_p, c_size_t, c_void_p]),
     "of_attn_bwd": (c_int32, [P(OfAttnDesc)] + [c_void_p] * 10 + [c_size_t, c_void_p]),
+    "of_vocab_workspace_size": (c_size_t, [P(OfVocabDesc), c_int32]),
+    "of_vocab_xent_fwd": (c_int32, [P(OfVocabDesc), c_void_p, P(OfParam)] + [c_void_p] * 6 + [c_size_t, c_void_p]),
+    "of_vocab_distill_fwd": (c_int32, [P(OfVocabDesc), c_void_p, P(OfParam)] + [c_void_p] * 7 + [c_size_t, c_void_p]),
+    "of_vocab_xent_bwd": (c_int32, [P(OfVocabDesc), c_void_p, P(OfParam)] + [c_void_p] * 6 +
+                          [c_int32, c_void_p, c_size_t, c_void_p]),
+    "of_vocab_distill_bwd": (c_int32, [P(OfVocabDesc), c_void_p, P(OfParam)] + [c_void_p] * 7 +
+                             [c_int32, c_void_p, c_size_t, c_void_p]),
+    "of_vocab_xent_bwd_fused": (c_int32, [P(OfVocabDesc), c_void_p, P(OfParam)] + [c_void_p] * 5 +
+                                [P(OfOpt), c_void_p, c_void_p, c_size_t, c_void_p]),
+    "of_vocab_distill_bwd_fused": (c_int32, [P(OfVocabDesc), c_void_p, P(OfParam)] + [c_void_p] * 6 +
+                                   [P(OfOpt), c_void_p, c_void_p, c_size_t, c_void_p]),
     "of_xent_fwd_bwd": (c_int32, [c_void_p, c_void_p, c_int64, c_int64, c_int64, c_void_p,
                                   c_void_p, c_void_p]),
     "of_mse_workspace_size": (c_size_t, [c_int64, c_int64]),
@@ -255,6 +275,10 @@ def of_attn_workspace_size(desc, op):
     return load().of_attn_workspace_size(ctypes.byref(desc), op)
 
 
+def of_vocab_workspace_size(desc, op):
+    return load().of_vocab_workspace_size(ctypes.byref(desc), op)
+
+
 def of_layernorm_partial_rows(M):
     return load().of_layernorm_partial_rows(M)
 
@@ -268,7 +292,9 @@ for _n in ("of_linear_fwd", "of_linear_fwd_carry", "of_linear_fwd_res", "of_conv
            "of_layernorm_fwd", "of_layernorm_fwd_bf16", "of_layernorm_bwd",
            "of_reduce_rows", "of_add", "of_dwconv_fwd", "of_dwconv_bwd_data",
            "of_dwconv_bwd_weight", "of_dwconv_wgrad_fused", "of_rotary_fwd", "of_rotary_bwd",
-           "of_attn_fwd", "of_attn_bwd"):
+           "of_attn_fwd", "of_attn_bwd", "of_vocab_xent_fwd", "of_vocab_xent_bwd",
+           "of_vocab_xent_bwd_fused", "of_vocab_distill_fwd", "of_vocab_distill_bwd",
+           "of_vocab_distill_bwd_fused"):
     globals()[_n] = _wrap(_n)
 del _n
 

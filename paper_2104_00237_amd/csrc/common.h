@@ -482,4 +482,31 @@ size_t attn_bwd_ws_bytes(const AttnArgs& a, bool bf16, bool grad_bf16);
 hipError_t attn_fwd_launch(AttnArgs a, bool bf16, bool vec, void* ws, hipStream_t stream);
 hipError_t attn_bwd_launch(AttnArgs a, bool bf16, bool grad_bf16, bool vec, void* ws, hipStream_t stream);
 
+// -------------------------------------------------------- vocabulary losses
+constexpr int kTopMax = 1024;      // entries of a row's target
+struct VocabArgs {
+  int64_t M, V, K, ldx;
+  bool bf16, gbf;                  // operands, gradients
+  const void* x;                   // [M, ldx]
+  of_param W;                      // [V, K]
+  // the target: cross-entropy has a label a row (teacher NULL, k = 1), distillation k entries
+  const int64_t* ids;              // [M, k]
+  const void* teacher;             // [M, k] logits
+  bool tbf;                        // the teacher's logits are bf16
+  int k;
+  float cap, z_loss, T;            // cap 0: none
+  float *loss, *lse, *zt, *mean;   // forward: [M], [M], [M, k], [1] or NULL
+  // backward
+  const float* dloss;              // [M] or NULL: the mean's
+  void *dx, *dw;                   // either may be NULL
+  int accumulate;
+  const float* gW;
+  bool fused;                      // update W with opt instead of storing dw
+  OptK opt;
+};
+// Sizes, types and k are read; the pointers are not.
+size_t vocab_ws_bytes(const VocabArgs& a, bool bwd);
+hipError_t vocab_fwd_launch(const VocabArgs& a, void* ws, hipStream_t stream);
+hipError_t vocab_bwd_launch(const VocabArgs& a, void* ws, hipStream_t stream);
+
 }  // namespace opfuse

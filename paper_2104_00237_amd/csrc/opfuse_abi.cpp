@@ -1387,4 +1387,179 @@ of_status of_attn_bwd(const of_attn_desc* d, const void* q, const void* k, const
   return hip_status(attn_bwd_launch(a, bf16, gbf, vec, ws, (hipStream_t)stream), "of_attn_bwd launch");
 }
 
+namespace {
+// Checks a descriptor and fills everything but the pointers.
+of_status check_vocab(const of_vocab_desc* d, bool bwd, VocabArgs* a) {
+  REQUIRE(d != nullptr, OF_EINVAL, "desc is NULL");
+  REQUIRE(d->M >= 1 && d->V >= 1 && d->K >= 1, OF_EINVAL, "M, V and K must be >= 1");
+  REQUIRE(d->ldx == 0 || d->ldx >= d->K, OF_EINVAL, "ldx must be 0 or >= K");
+  REQUIRE(d->dtype == OF_F32 || d->dtype == OF_BF16, OF_EINVAL, "dtype %d is not an of_dtype", (int)d->dtype);
+  REQUIRE(d->grad_dtype == OF_F32 || d->grad_dtype == OF_BF16, OF_EINVAL, "grad_dtype %d is not an of_dtype",
+          (int)d->grad_dtype);
+  REQUIRE(d->teacher_dtype == OF_F32 || d->teacher_dtype == OF_BF16, OF_EINVAL, "teacher_dtype %d is not an of_dtype",
+          (int)d->teacher_dtype);
+  REQUIRE(!bwd || d->grad_dtype == OF_F32 || d->dtype == OF_BF16, OF_EUNSUPPORTED,
+          "bf16 gradients need bf16 operands");
+  REQUIRE(d->topk >= 0, OF_EINVAL, "topk must be >= 0");
+  REQUIRE(d->topk <= kTopMax, OF_EUNSUPPORTED, "topk must be <= %d", kTopMax);
+  // (their reciprocals and squares stay in float's range)
+  for (const float v : {d->softcap, d->temperature}) {
+    REQUIRE(std::isfinite(v) && v >= 0.f, OF_EINVAL, "softcap and temperature must be finite and >= 0 (0: none)");
+    REQUIRE(v == 0.f || (v >= 0x1p-40f && v <= 0x1p40f), OF_EUNSUPPORTED,
+            "softcap and temperature must be 0 or in [2^-40, 2^40]");
+  }
+  REQUIRE(std::isfinite(d->z_loss) && d->z_loss >= 0.f, OF_EINVAL, "z_loss must be finite and >= 0");
+  memset(a, 0, sizeof(*a));
+  a->M = d->M, a->V = d->V, a->K = d->K;
+  a->ldx = d->ldx ? d->ldx : d->K;
+  REQUIRE(a->M <= (1LL << 22) && a->V <= (1LL << 22) && a->K <= (1LL << 20), OF_EUNSUPPORTED,
+          "M and V must be <= 2^22, K <= 2^20");
+  REQUIRE(a->ldx <= (1LL << 21), OF_EUNSUPPORTED, "ldx must be <= 2^21");
+  // the products address an operand's bytes in 32 bits
+  REQUIRE(a->M * a->ldx * (d->dtype == OF_BF16 ? 2 : 4) < (1LL << 31) && a->M * a->K * 4 < (1LL << 31), OF_EUNSUPPORTED,
+          "X must be < 2 GiB, and M * K < 2^29");
+  REQUIRE(a->M * std::max<int64_t>(d->topk, 1) < (1LL << 31), OF_EUNSUPPORTED, "M * topk must be < 2^31");
+  a->bf16 = d->dtype == OF_BF16;
+  a->gbf = d->grad_dtype == OF_BF16;
+  a->tbf = d->teacher_dtype == OF_BF16;
+  a->k = std::max<int32_t>(d->topk, 1);
+  a->cap = d->softcap;
+  a->z_loss = d->z_loss;
+  a->T = d->temperature ? d->temperature : 1.f;
+  return OF_OK;
+}
+
+// The arguments that every vocabulary loss takes.
+of_status check_vocab_call(const of_vocab_desc* d, bool bwd, bool distill, const void* x, const of_param* W,
+                           const int64_t* ids, const void* teacher, const float* lse, const float* zt, const void* ws,
+                           size_t ws_bytes, VocabArgs* a) {
+  of_status st = check_vocab(d, bwd, a);
+  if (st != OF_OK) return st;
+  REQUIRE(distill ? d->topk >= 1 : d->topk <= 1, OF_EINVAL,
+          distill ? "topk must be >= 1" : "topk must be 0 or 1 (a label a row)");
+  REQUIRE(distill || a->T == 1.f, OF_EINVAL, "temperature must be 0 or 1 (distillation has one)");
+  REQUIRE(!distill || d->z_loss == 0.f, OF_EINVAL, "z_loss must be 0 (cross-entropy has one)");
+  REQUIRE(x && W && ids && lse && zt && (!distill || teacher), OF_EINVAL,
+          distill ? "x, W, ids, teacher, lse and zt are required" : "x, W, labels, lse and zt are required");
+  const size_t es = a->bf16 ? 2 : 4;
+  const void* w = a->bf16 ? (const void*)W->w_bf16 : W->w;
+  REQUIRE(w != nullptr, OF_EINVAL, a->bf16 ? "W->w_bf16 is NULL" : "W->w is NULL");
+  REQUIRE(W->numel == a->V * a->K, OF_EINVAL, "W->numel is %lld, expected V * K = %lld", (long long)W->numel,
+          (long long)(a->V * a->K));
+  REQUIRE(aligned_to(x, es) && aligned_to(w, es), OF_EALIGN, "x and W must be %d-byte aligned", (int)es);
+  REQUIRE(aligned_to(ids, 8), OF_EALIGN, "labels and ids must be 8-byte aligned");
+  REQUIRE(!distill || aligned_to(teacher, a->tbf ? 2 : 4), OF_EALIGN, "teacher must be %d-byte aligned", a->tbf ? 2 : 4);
+  REQUIRE(al4(lse) && al4(zt), OF_EALIGN, "lse and zt must be 4-byte aligned");
+  if ((st = check_attn_ws(vocab_ws_bytes(*a, bwd), ws, ws_bytes)) != OF_OK) return st;
+  a->x = x;
+  a->W = *W;
+  a->ids = ids;
+  a->teacher = distill ? teacher : nullptr;
+  a->lse = const_cast<float*>(lse);
+  a->zt = const_cast<float*>(zt);
+  return OF_OK;
+}
+
+of_status vocab_fwd_entry(const of_vocab_desc* d, bool distill, const void* x, const of_param* W, const int64_t* ids,
+                          const void* teacher, float* loss, float* lse, float* zt, float* mean, void* ws,
+                          size_t ws_bytes, void* stream, const char* what) {
+  VocabArgs a;
+  const of_status st = check_vocab_call(d, false, distill, x, W, ids, teacher, lse, zt, ws, ws_bytes, &a);
+  if (st != OF_OK) return st;
+  REQUIRE(loss != nullptr, OF_EINVAL, "loss is required");
+  REQUIRE(al4(loss) && al4(mean), OF_EALIGN, "loss and mean must be 4-byte aligned");
+  REQUIRE(loss != lse && loss != zt && lse != zt && (!mean || (mean != loss && mean != lse && mean != zt)), OF_EINVAL,
+          "loss, lse, zt and mean must be different buffers");
+  a.loss = loss;
+  a.mean = mean;
+  return hip_status(vocab_fwd_launch(a, ws, (hipStream_t)stream), what);
+}
+
+// opt == NULL: dw, else the update.
+of_status vocab_bwd_entry(const of_vocab_desc* d, bool distill, const void* x, const of_param* W, const int64_t* ids,
+                          const void* teacher, const float* lse, const float* zt, const float* dloss, void* dx,
+                          void* dw, int32_t accumulate, const float* gW, const of_opt* opt, void* ws, size_t ws_bytes,
+                          void* stream, const char* what) {
+  VocabArgs a;
+  of_status st = check_vocab_call(d, true, distill, x, W, ids, teacher, lse, zt, ws, ws_bytes, &a);
+  if (st != OF_OK) return st;
+  const size_t gs = a.gbf ? 2 : 4;
+  REQUIRE(opt || dx || dw, OF_EINVAL, "dx and dw are both NULL");
+  REQUIRE(aligned_to(dx, gs) && aligned_to(dw, gs), OF_EALIGN, "dx and dw must be %d-byte aligned", (int)gs);
+  REQUIRE(al4(dloss) && al4(gW), OF_EALIGN, "fp32 pointers must be 4-byte aligned");
+  REQUIRE(accumulate == 0 || accumulate == 1, OF_EINVAL, "accumulate must be 0 or 1");
+  REQUIRE(!dx || (dx != x && dx != dw && dx != W->w && dx != W->w_bf16), OF_EINVAL, "dx must not alias x, W or dw");
+  REQUIRE(!dw || (dw != x && dw != W->w && dw != W->w_bf16), OF_EINVAL, "dw must not alias x or W");
+  a.dloss = dloss;
+  a.dx = dx;
+  a.dw = dw;
+  a.accumulate = accumulate;
+  if (opt) {
+    if ((st = check_opt(opt)) != OF_OK) return st;
+    if ((st = check_param(W, "W", a.V * a.K, *opt, true)) != OF_OK) return st;
+    REQUIRE(a.bf16 || W->w_bf16 == nullptr, OF_EINVAL, "W->w_bf16 is set but the descriptor's dtype is OF_F32");
+    a.fused = true;
+    a.gW = gW;
+    a.opt = make_optk(*opt);
+  }
+  return hip_status(vocab_bwd_launch(a, ws, (hipStream_t)stream), what);
+}
+
+of_status no_opt() { return fail(OF_EINVAL, "opt is NULL"); }
+}  // namespace
+
+size_t of_vocab_workspace_size(const of_vocab_desc* d, int32_t op) {
+  VocabArgs a;
+  if (op != OF_VOCAB_FWD && op != OF_VOCAB_BWD) {
+    fail(OF_EINVAL, "op %d is not an of_vocab_op", (int)op);
+    return 0;
+  }
+  if (check_vocab(d, op == OF_VOCAB_BWD, &a) != OF_OK) return 0;
+  return vocab_ws_bytes(a, op == OF_VOCAB_BWD);
+}
+
+of_status of_vocab_xent_fwd(const of_vocab_desc* d, const void* x, const of_param* W, const int64_t* labels,
+                            float* loss, float* lse, float* zt, float* mean, void* ws, size_t ws_bytes, void* stream) {
+  return vocab_fwd_entry(d, false, x, W, labels, nullptr, loss, lse, zt, mean, ws, ws_bytes, stream,
+                         "of_vocab_xent_fwd launch");
+}
+
+of_status of_vocab_distill_fwd(const of_vocab_desc* d, const void* x, const of_param* W, const int64_t* ids,
+                               const void* teacher, float* loss, float* lse, float* zt, float* mean, void* ws,
+                               size_t ws_bytes, void* stream) {
+  return vocab_fwd_entry(d, true, x, W, ids, teacher, loss, lse, zt, mean, ws, ws_bytes, stream,
+                         "of_vocab_distill_fwd launch");
+}
+
+of_status of_vocab_xent_bwd(const of_vocab_desc* d, const void* x, const of_param* W, const int64_t* labels,
+                            const float* lse, const float* zt, const float* dloss, void* dx, void* dw,
+                            int32_t accumulate, void* ws, size_t ws_bytes, void* stream) {
+  return vocab_bwd_entry(d, false, x, W, labels, nullptr, lse, zt, dloss, dx, dw, accumulate, nullptr, nullptr, ws,
+                         ws_bytes, stream, "of_vocab_xent_bwd launch");
+}
+
+of_status of_vocab_distill_bwd(const of_vocab_desc* d, const void* x, const of_param* W, const int64_t* ids,
+                               const void* teacher, const float* lse, const float* zt, const float* dloss, void* dx,
+                               void* dw, int32_t accumulate, void* ws, size_t ws_bytes, void* stream) {
+  return vocab_bwd_entry(d, true, x, W, ids, teacher, lse, zt, dloss, dx, dw, accumulate, nullptr, nullptr, ws,
+                         ws_bytes, stream, "of_vocab_distill_bwd launch");
+}
+
+of_status of_vocab_xent_bwd_fused(const of_vocab_desc* d, const void* x, const of_param* W, const int64_t* labels,
+                                  const float* lse, const float* zt, const float* dloss, const float* gW_partial,
+                                  const of_opt* opt, void* dx, void* ws, size_t ws_bytes, void* stream) {
+  if (opt == nullptr) return no_opt();
+  return vocab_bwd_entry(d, false, x, W, labels, nullptr, lse, zt, dloss, dx, nullptr, 0, gW_partial, opt, ws, ws_bytes,
+                         stream, "of_vocab_xent_bwd_fused launch");
+}
+
+of_status of_vocab_distill_bwd_fused(const of_vocab_desc* d, const void* x, const of_param* W, const int64_t* ids,
+                                     const void* teacher, const float* lse, const float* zt, const float* dloss,
+                                     const float* gW_partial, const of_opt* opt, void* dx, void* ws, size_t ws_bytes,
+                                     void* stream) {
+  if (opt == nullptr) return no_opt();
+  return vocab_bwd_entry(d, true, x, W, ids, teacher, lse, zt, dloss, dx, nullptr, 0, gW_partial, opt, ws, ws_bytes,
+                         stream, "of_vocab_distill_bwd_fused launch");
+}
+
 }  // extern "C"

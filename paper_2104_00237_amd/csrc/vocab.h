@@ -1,0 +1,100 @@
+// Row statistics, targets and tiles that the vocabulary losses' kernels share.
+//
+//   s = X W^T, z = s or cap tanh(s / cap), u = z / T, lse = log sum_v exp u_v
+//   cross-entropy  loss = lse - z_y + c lse^2              dz_v = g (p_v (1 + 2 c lse) - [v = y])
+//   distillation   loss = T^2 sum_j q_j (log q_j - u_j + lse)   dz_v = g T (p_v - sum of q_j with id_j = v)
+//   ds = dz (1 - (z / cap)^2)
+// Cross-entropy is distillation from one entry with q = 1 (T = 1, log q = 0) but for c.
+#pragma once
+
+#include "gemm_common.h"
+
+namespace opfuse {
+
+// A running maximum and the sum of exponentials below it.  m = -infinity: nothing yet, or logits of
+// -infinity only; a NaN logit makes the sum NaN (a maximum alone would pass over it).
+struct Stat {
+  float m, s;
+};
+__device__ __forceinline__ float stat_shift(float m) { return m == -INFINITY ? 0.f : m; }
+__device__ __forceinline__ Stat stat_join(Stat a, Stat b) {
+  const float m = fmaxf(a.m, b.m), t = stat_shift(m);
+  return Stat{m, __fadd_rn(__fmul_rn(a.s, expf(a.m - t)), __fmul_rn(b.s, expf(b.m - t)))};
+}
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) v = __fadd_rn(v, __shfl_xor(v, d));
+  return v;
+}
+__device__ __forceinline__ float wave_max(float v) {
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
+  return v;
+}
+
+__device__ __forceinline__ float vocab_cap(float s, float cap) { return cap > 0.f ? cap * tanhf(s / cap) : s; }
+
+// A row's target as a wavefront sees it: entry j has weight exp(t_j / T - top) / total.
+// Entries with a negative id are left out whatever their logit; a row none of whose entries has a
+// weight (none at all, or logits of -infinity only) does not count; an id past the vocabulary
+// makes the row's loss NaN and its gradient zero, as does nothing else.
+struct RowTarget {
+  float top, total;
+  bool counts, bad;
+  __device__ __forceinline__ float weight(float t) const { return __fdiv_rn(expf(t - top), total); }
+};
+__device__ __forceinline__ float teacher_logit(const VocabArgs& a, int64_t i) {
+  const float t = a.tbf ? __uint_as_float((uint32_t)((const uint16_t*)a.teacher)[i] << 16) : ((const float*)a.teacher)[i];
+  return __fdiv_rn(t, a.T);
+}
+__device__ __forceinline__ RowTarget row_target(const VocabArgs& a, int64_t row, int lane) {
+  RowTarget r{0.f, 1.f, false, false};
+  if (a.teacher == nullptr) {
+    const int64_t y = a.ids[row];
+    r.counts = y >= 0;
+    r.bad = y >= a.V;
+    return r;
+  }
+  const int64_t at = row * a.k;
+  float top = -INFINITY;
+  bool bad = false, nan = false;
+  for (int j = lane; j < a.k; j += 64) {
+    const int64_t id = a.ids[at + j];
+    if (id < 0) continue;
+    const float t = teacher_logit(a, at + j);
+    bad |= id >= a.V;
+    nan |= t != t;
+    top = fmaxf(top, t);
+  }
+  r.top = wave_max(top);
+  r.bad = __any(bad);
+  r.counts = r.top != -INFINITY || __any(nan);
+  r.top = stat_shift(r.top);
+  float total = 0.f;
+  for (int j = lane; j < a.k; j += 64)
+    if (a.ids[at + j] >= 0) total += expf(teacher_logit(a, at + j) - r.top);
+  total = wave_sum(total);
+  r.total = total == 0.f ? 1.f : total;
+  return r;
+}
+
+// The row's loss from its lse and the (capped) logits of its entries; every lane gets it.
+__device__ __forceinline__ float row_loss(const VocabArgs& a, int64_t row, float lse, int lane, bool* counts) {
+  const RowTarget r = row_target(a, row, lane);
+  *counts = r.counts;
+  if (!r.counts) return 0.f;
+  if (r.bad) return NAN;
+  if (a.teacher == nullptr) return __fmaf_rn(__fmul_rn(a.z_loss, lse), lse, __fsub_rn(lse, a.zt[row]));
+  float loss = 0.f;
+  const float log_total = logf(r.total);
+  for (int j = lane; j < a.k; j += 64) {
+    const int64_t i = row * a.k + j;
+    if (a.ids[i] < 0) continue;
+    const float t = teacher_logit(a, i), q = r.weight(t);
+    // (an entry of weight 0 adds nothing, also where its logarithm or logit is infinite)
+    if (q != 0.f) loss = __fmaf_rn(q, (t - r.top - log_total) - (__fdiv_rn(a.zt[i], a.T) - lse), loss);
+  }
+  return a.T * a.T * wave_sum(loss);
+}
+
+}  // namespace opfuse

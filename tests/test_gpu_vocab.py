@@ -1,0 +1,436 @@
+"""of_vocab_xent_* and of_vocab_distill_* against float64 (tests/vocab_reference.py has the bounds): both types,
+sizes around the tiles, labels left out, entries that are missing, repeated or of no weight, caps, strides,
+accumulation, updates, replayed captures, and what must not be touched."""
+import math
+
+import pytest
+import torch
+
+from paper_2104_00237_amd import _lib as L
+from tests.vocab_reference import Reference, near, target
+
+pytestmark = pytest.mark.gpu
+TYPES = {"f32": (torch.float32, L.OF_F32, 2.0 ** -24), "bf16": (torch.bfloat16, L.OF_BF16, 2.0 ** -8)}
+
+
+class Call:
+    """One head with its rows and targets on the GPU, and the calls on them."""
+
+    def __init__(self, gpu, M, V, K, dtype, k=0, T=1.0, cap=0.0, z_loss=0.0, gap=0, shift=0, given=False, ids=None,
+                 teacher=None, teacher_dtype="f32", grads=None, seed=0, x_scale=1.0):
+        g = torch.Generator().manual_seed(M * 7 + V * 3 + K + seed)
+        t, kind, _ = TYPES[dtype]
+        self.gpu, self.M, self.V, self.K, self.k, self.dtype = gpu, M, V, K, max(k, 1), dtype
+        self.T, self.cap, self.z_loss, self.distill = T, cap, z_loss, k > 0
+        self.grads = grads or dtype
+        w = (torch.randn(V, K, generator=g) * 2 / math.sqrt(K)).to(t)
+        if ids is None:
+            ids = torch.stack([torch.randperm(V, generator=g)[:self.k] for _ in range(M)]) if k else \
+                torch.randint(0, V, (M, 1), generator=g)
+            ids[torch.rand(M, self.k, generator=g) < 0.15] = -1
+        x = torch.randn(M, K, generator=g) * x_scale
+        x += 3 * torch.nn.functional.normalize(w[ids[:, 0].clamp_min(0)].float(), dim=1)
+        self.x, self.w, self.ids = x.to(t), w, ids
+        self.teacher = None
+        if k:
+            self.teacher = (torch.randn(M, k, generator=g) * 3 if teacher is None else teacher).to(TYPES[teacher_dtype][0])
+        self.dloss = torch.rand(M, generator=g) / M if given else None
+        # rows at a stride, behind some elements
+        self.flat = torch.full((M * (K + gap) + shift,), 7.0, dtype=t, device=gpu)
+        self.dev_x = self.flat[shift:].view(M, K + gap)[:, :K]
+        self.dev_x.copy_(self.x)
+        self.wflat = torch.full((V * K + shift,), 7.0, dtype=t, device=gpu)
+        self.dev_w = self.wflat[shift:].view(V, K)
+        self.dev_w.copy_(w)
+        self.d = L.OfVocabDesc(M=M, V=V, K=K, ldx=K + gap, dtype=kind, grad_dtype=TYPES[self.grads][1], topk=k,
+                               teacher_dtype=TYPES[teacher_dtype][1], softcap=cap, z_loss=z_loss, temperature=T)
+        self.param = L.OfParam(numel=V * K, **{"w" if dtype == "f32" else "w_bf16": self.dev_w.data_ptr()})
+        self.t = [ids.to(gpu)] + ([self.teacher.to(gpu)] if k else [])
+        self.dev_dloss = self.dloss.to(gpu) if given else None
+        new = lambda *s: torch.full(s, 7.0, device=gpu)  # noqa: E731
+        self.loss, self.lse, self.zt, self.mean = new(M), new(M), new(M, self.k), new(1)
+        gt = TYPES[self.grads][0]
+        self.dxflat = torch.full((M * (K + gap) + shift,), 7.0, dtype=gt, device=gpu)
+        self.dx = self.dxflat[shift:].view(M, K + gap)[:, :K]
+        self.dw = torch.full((V, K), 7.0, dtype=gt, device=gpu)
+        self.ws = {}
+        for op in (L.OF_VOCAB_FWD, L.OF_VOCAB_BWD):
+            size = L.of_vocab_workspace_size(self.d, op)
+            self.ws[op] = torch.full((size + 256,), 0xff, dtype=torch.uint8, device=gpu)   # NaN, whatever it is read as
+
+    def _ws(self, op):
+        return self.ws[op].data_ptr(), self.ws[op].numel() - 256
+
+    def _stream(self):
+        return torch.cuda.current_stream().cuda_stream
+
+    def _targets(self):
+        return [x.data_ptr() for x in self.t]
+
+    def fwd(self, mean=True):
+        f = L.of_vocab_distill_fwd if self.distill else L.of_vocab_xent_fwd
+        f(self.d, self.dev_x.data_ptr(), self.param, *self._targets(), self.loss.data_ptr(), self.lse.data_ptr(),
+          self.zt.data_ptr(), self.mean.data_ptr() if mean else None, *self._ws(L.OF_VOCAB_FWD), self._stream())
+
+    def bwd(self, dx=True, dw=True, accumulate=0):
+        f = L.of_vocab_distill_bwd if self.distill else L.of_vocab_xent_bwd
+        f(self.d, self.dev_x.data_ptr(), self.param, *self._targets(), self.lse.data_ptr(), self.zt.data_ptr(),
+          self.dev_dloss.data_ptr() if self.dev_dloss is not None else None, self.dx.data_ptr() if dx else None,
+          self.dw.data_ptr() if dw else None, accumulate, *self._ws(L.OF_VOCAB_BWD), self._stream())
+
+    def bwd_fused(self, opt, gW=None, dx=True):
+        f = L.of_vocab_distill_bwd_fused if self.distill else L.of_vocab_xent_bwd_fused
+        f(self.d, self.dev_x.data_ptr(), self.param, *self._targets(), self.lse.data_ptr(), self.zt.data_ptr(),
+          self.dev_dloss.data_ptr() if self.dev_dloss is not None else None, gW.data_ptr() if gW is not None else None, opt,
+          self.dx.data_ptr() if dx else None, *self._ws(L.OF_VOCAB_BWD), self._stream())
+
+    def reference(self, **kw):
+        a = dict(x=self.x, w=self.w, ids=self.ids, teacher=self.teacher, T=self.T, cap=self.cap, z_loss=self.z_loss,
+                 dloss=self.dloss, u=TYPES[self.dtype][2])
+        a.update(kw)
+        return Reference(**a)
+
+    def check_fwd(self, r=None, mean=True):
+        r = r or self.reference()
+        near("lse", self.lse, r.lse, r.e_lse)
+        near("zt", self.zt, r.zt, r.e_zt)
+        near("loss", self.loss, r.loss, r.e_loss)
+        if mean:
+            near("mean", self.mean[0], torch.tensor(r.mean, dtype=torch.float64), torch.tensor(r.e_mean, dtype=torch.float64))
+
+    def check_bwd(self, r=None, dx=True, dw=True):
+        r, half = r or self.reference(), TYPES[self.grads][2]
+        if dx:
+            near("dx", self.dx, r.dx, r.e_dx, half)
+        if dw:
+            near("dw", self.dw, r.dw, r.e_dw, half)
+
+    def untouched(self):
+        """What lies behind the rows, before shifted tensors and behind the workspaces."""
+        for flat, view in ((self.flat, self.dev_x), (self.dxflat, self.dx)):
+            rest = flat.clone()
+            rest[view.storage_offset():].view(self.M, -1)[:, :self.K] = 7.0
+            assert (rest == 7.0).all()
+        for w in self.ws.values():
+            assert (w[-256:] == 0xff).all()
+
+
+SIZES = [(1, 1, 1), (1, 5, 8), (2, 64, 32), (3, 63, 31), (31, 129, 40), (33, 257, 64), (64, 1000, 128), (127, 255, 33),
+         (129, 130, 257), (257, 520, 72), (300, 1031, 320), (8, 5003, 512), (130, 7, 100), (513, 300, 96), (40, 4100, 264)]
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,V,K", SIZES)
+def test_xent(gpu, M, V, K, dtype):
+    c = Call(gpu, M, V, K, dtype, given=M % 2 == 0)
+    c.fwd()
+    c.bwd()
+    c.check_fwd()
+    c.check_bwd()
+    c.untouched()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,V,K,k,T", [(1, 9, 8, 3, 1.0), (5, 64, 40, 64, 2.0), (33, 700, 64, 7, 1.5), (129, 260, 33, 100, 4.0),
+                                       (300, 1031, 128, 20, 1.0), (16, 5003, 72, 257, 0.5), (260, 130, 64, 1, 3.0),
+                                       (37, 1100, 64, 1024, 1.0)])
+def test_distill(gpu, M, V, K, k, T, dtype):
+    c = Call(gpu, M, V, K, dtype, k=k, T=T, given=M % 2 == 1, teacher_dtype="bf16" if k % 2 else "f32")
+    c.fwd()
+    c.bwd()
+    c.check_fwd()
+    c.check_bwd()
+    c.untouched()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("kw", [dict(cap=5.0), dict(cap=30.0, z_loss=1e-3), dict(z_loss=0.1), dict(cap=2.0 ** 20),
+                                dict(cap=0.5, k=9, T=2.0), dict(gap=8), dict(gap=3, given=True), dict(shift=1),
+                                dict(gap=5, shift=3, k=4), dict(gap=16, shift=8), dict(grads="f32"),
+                                dict(grads="f32", k=3, gap=1)])
+@pytest.mark.parametrize("M,V,K", [(35, 300, 64), (140, 600, 136)])
+def test_options(gpu, M, V, K, dtype, kw):
+    c = Call(gpu, M, V, K, dtype, **kw)
+    c.fwd()
+    c.bwd()
+    c.check_fwd()
+    c.check_bwd()
+    c.untouched()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("k", [0, 3])
+def test_rows_that_do_not_count(gpu, dtype, k):
+    """Rows without a target hold NaN and infinities: nothing of them reaches another row, dX or dW."""
+    M, V, K = 150, 333, 72
+    c = Call(gpu, M, V, K, dtype, k=k)
+    out = torch.arange(M) % 3 == 1
+    c.ids[out] = -1
+    if k:   # some by logits of -infinity instead, some with NaN in entries that are not there
+        low = torch.arange(M) % 6 == 1
+        c.ids[low] = 5
+        c.teacher[low] = -math.inf
+        c.teacher[torch.arange(M) % 6 == 4] = math.nan
+        c.t[1].copy_(c.teacher)
+    c.t[0].copy_(c.ids)
+    bad = torch.randn(M, K)
+    bad[::2], bad[1::2] = math.nan, math.inf
+    c.dev_x[out.to(gpu)] = bad[out].to(c.x.dtype).to(gpu)
+    c.fwd()
+    c.bwd()
+    r = c.reference()
+    assert (r.counts == ~out).all() or (r.counts[~out].sum() > 0 and not r.counts[out].any())
+    near("loss", c.loss, r.loss, r.e_loss)
+    keep = ~out
+    near("lse", c.lse[keep.to(gpu)], r.lse[keep], r.e_lse[keep])
+    near("mean", c.mean[0], torch.tensor(r.mean, dtype=torch.float64), torch.tensor(r.e_mean, dtype=torch.float64))
+    c.check_bwd(r)
+    assert (c.dx[out.to(gpu)] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("k", [0, 2])
+def test_no_row_counts(gpu, dtype, k):
+    c = Call(gpu, 9, 50, 24, dtype, k=k, ids=torch.full((9, max(k, 1)), -1))
+    c.fwd()
+    c.bwd()
+    assert (c.loss == 0).all() and (c.mean == 0).all() and (c.zt == 0).all()
+    assert (c.dx == 0).all() and (c.dw == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("k", [0, 3])
+def test_ids_past_the_vocabulary(gpu, dtype, k):
+    """Such a row's loss (and the mean) is NaN; it gets no gradient and counts in the mean's."""
+    c = Call(gpu, 20, 70, 40, dtype, k=k)
+    c.ids[:, 0] = torch.arange(20)
+    clean = c.ids.clone()
+    c.ids[4, 0], c.ids[11, -1] = 70, 1 << 40
+    c.t[0].copy_(c.ids)
+    c.fwd()
+    c.bwd()
+    bad = torch.zeros(20, dtype=torch.bool)
+    bad[4] = bad[11] = True
+    assert (c.loss.cpu().isnan() == bad).all() and c.mean.isnan().all()
+    clean[bad] = 0
+    r = c.reference(ids=clean)
+    near("loss", c.loss[~bad.to(gpu)], r.loss[~bad], r.e_loss[~bad])
+    g = torch.full((20,), 1 / 20)
+    g[bad] = 0
+    r = c.reference(ids=clean, dloss=g)
+    c.check_bwd(r, dx=True)
+    assert (c.dx[bad.to(gpu)] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_entries_that_repeat(gpu, dtype):
+    ids = torch.randint(0, 12, (70, 30), generator=torch.Generator().manual_seed(1))
+    ids[::7, 3:] = -1
+    ids[5] = 4
+    c = Call(gpu, 70, 300, 64, dtype, k=30, ids=ids, T=2.0)
+    c.fwd()
+    c.bwd()
+    c.check_fwd()
+    c.check_bwd()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_sharp_and_flat_rows(gpu, dtype):
+    """Logits far apart (most probabilities underflow) and all alike (X of zeros)."""
+    c = Call(gpu, 40, 400, 64, dtype, x_scale=60.0)
+    c.x[::2] = 0
+    c.dev_x.copy_(c.x)
+    c.fwd()
+    c.bwd()
+    c.check_fwd()
+    c.check_bwd()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_infinite_and_nan_logits(gpu, dtype):
+    """A logit of -infinity has probability 0; NaN makes its own row's lse and loss NaN and no other's."""
+    c = Call(gpu, 12, 90, 16, dtype, ids=torch.arange(12)[:, None])
+    c.w[:, 0] = 0
+    c.w[50, 0] = -math.inf     # with x[:, 0] > 0: -infinity, with 0: NaN
+    c.x[:, 0] = 1
+    c.x[3, 0] = 0
+    c.dev_x.copy_(c.x)
+    c.dev_w.copy_(c.w)
+    c.fwd(mean=False)
+    assert (c.lse.isnan().cpu() == (torch.arange(12) == 3)).all()
+    c.w[50, 0] = -3e4
+    r = c.reference()
+    keep = torch.arange(12) != 3
+    near("lse", c.lse[keep.to(gpu)], r.lse[keep], r.e_lse[keep])
+
+
+@pytest.mark.parametrize("dtype,grads", [("f32", "f32"), ("bf16", "bf16"), ("bf16", "f32")])
+@pytest.mark.parametrize("M,V,K", [(50, 200, 48), (260, 300, 129)])
+def test_parts_of_the_backward(gpu, M, V, K, dtype, grads):
+    """dX alone, dW alone, dW added to what is there, each the same bits as together."""
+    c = Call(gpu, M, V, K, dtype, grads=grads, given=True)
+    c.fwd()
+    c.bwd()
+    dx, dw = c.dx.clone(), c.dw.clone()
+    c.dx.fill_(7.0), c.dw.fill_(7.0)
+    c.bwd(dw=False)
+    assert torch.equal(c.dx, dx) and (c.dw == 7.0).all()
+    c.dx.fill_(7.0)
+    c.bwd(dx=False)
+    assert torch.equal(c.dw, dw) and (c.dx == 7.0).all()
+    old = torch.randn(V, K, generator=torch.Generator().manual_seed(3)).mul_(dw.float().abs().mean().item()).to(dw.dtype)
+    c.dw.copy_(old)
+    c.bwd(dx=False, accumulate=1)
+    r, half = c.reference(), TYPES[grads][2]
+    near("dw", c.dw, r.dw + old.double(), r.e_dw + 2.0 ** -24 * (r.dw.abs() + old.double().abs()), half)
+
+
+OPTS = [dict(kind="sgd", lr=0.1, momentum=0.9, weight_decay=0.01), dict(kind="adam", lr=1e-3, beta1=0.9, beta2=0.99, eps=1e-8),
+        dict(kind="adamw", lr=1e-3, beta1=0.9, beta2=0.99, eps=1e-8, weight_decay=0.1),
+        dict(kind="adagrad", lr=1e-2, eps=1e-8), dict(kind="rmsprop", lr=1e-3, alpha=0.9, eps=1e-6, momentum=0.5),
+        dict(kind="adadelta", lr=0.5, rho=0.9, eps=1e-6)]
+
+
+@pytest.mark.parametrize("hyper", OPTS, ids=[o["kind"] for o in OPTS])
+@pytest.mark.parametrize("dtype,M,V,K,k", [("f32", 40, 130, 64, 0), ("bf16", 40, 130, 64, 0), ("bf16", 150, 333, 41, 4),
+                                           ("f32", 150, 333, 41, 4), ("bf16", 300, 600, 128, 0)])
+def test_update(gpu, dtype, M, V, K, k, hyper):
+    """The update in dW's product is that of a stored fp32 dW, applied by the element-wise update; dX reads the old W."""
+    c = Call(gpu, M, V, K, dtype, k=k, grads="f32")
+    g = torch.Generator().manual_seed(5)
+    w = c.w.float().add(torch.randn(V, K, generator=g) * 1e-4).to(gpu) if dtype == "bf16" else c.dev_w
+    m, v = (torch.randn(V, K, generator=g) * 1e-3).to(gpu), (torch.rand(V, K, generator=g) * 1e-5).to(gpu)
+    if hyper["kind"] == "adadelta":
+        m.abs_()
+    extra = (torch.randn(V, K, generator=g) * 1e-4).to(gpu)
+    shadow = c.dev_w if dtype == "bf16" else None
+    c.fwd()
+    c.bwd()
+    dx, dw = c.dx.clone(), c.dw.clone()
+    ref = [t.clone() for t in (w, m, v)]
+    ref_shadow = shadow.clone() if shadow is not None else None
+    opt = L.make_opt(hyper, 3)
+    p = L.param_of(*ref, w_bf16=ref_shadow)
+    total = torch.empty_like(dw)
+    L.of_add(extra.data_ptr(), dw.data_ptr(), dw.numel(), total.data_ptr(), c._stream())
+    L.of_elementwise_fused_update(p, total.data_ptr(), 1, 0, opt, c._stream())
+    c.param = L.OfParam(w.data_ptr(), m.data_ptr(), v.data_ptr(), shadow.data_ptr() if shadow is not None else None, V * K)
+    c.dx.fill_(7.0)
+    c.bwd_fused(opt, extra)
+    torch.cuda.synchronize()
+    assert torch.equal(c.dx, dx)
+    for name, a, b in zip("wmv", (w, m, v), ref):
+        assert torch.equal(a, b), (name, float((a - b).abs().max()))
+    if shadow is not None:
+        assert torch.equal(shadow, ref_shadow)
+    # without dX and without an earlier gradient, from a step counter on the device
+    step = torch.tensor([4], device=gpu)
+    opt = L.make_opt(hyper, 0, step.data_ptr())
+    c.fwd()
+    c.bwd(dx=False)
+    dw = c.dw.clone()
+    ref = [t.clone() for t in (w, m, v)]
+    L.of_elementwise_fused_update(L.param_of(*ref), dw.data_ptr(), 1, 0, opt, c._stream())
+    c.dx.fill_(7.0)
+    c.bwd_fused(opt, dx=False)
+    for name, a, b in zip("wmv", (w, m, v), ref):
+        assert torch.equal(a, b), name
+    assert (c.dx == 7.0).all()
+
+
+@pytest.mark.parametrize("dtype,k", [("f32", 0), ("bf16", 0), ("f32", 5), ("bf16", 5)])
+def test_differences(gpu, dtype, k):
+    """dX and dW against differences of the mean loss.
+
+    Along D the mean's third derivative is at most 8 max |D w|^3 (cumulants of a softmax over values in
+    [-a, a]); the two losses are within e_mean of their float64 values."""
+    M, V, K = 24, 120, 32
+    c = Call(gpu, M, V, K, dtype, k=k, grads="f32", T=2.0 if k else 1.0)
+    c.fwd()
+    c.bwd()
+    r = c.reference()
+    for side, h in (("x", 2.0 ** -6), ("w", 2.0 ** -7)):
+        base = getattr(c, side).clone()
+        dev = c.dev_x if side == "x" else c.dev_w
+        d = torch.sign(r.dx if side == "x" else r.dw)   # uphill everywhere
+        hi, lo = (base.double() + h * d).to(base.dtype), (base.double() - h * d).to(base.dtype)
+        got = []
+        for v in (hi, lo):
+            dev.copy_(v)
+            c.fwd()
+            got.append(c.mean.double().item())
+        dev.copy_(base)
+        step = hi.double() - lo.double()        # what was moved, after rounding to the type
+        mid = (hi.double() + lo.double()) / 2 - base.double()
+        grad = c.dx if side == "x" else c.dw
+        want = (grad.detach().cpu().double() * step).sum().item()
+        other = c.w if side == "x" else c.x
+        a = (step.abs() @ other.double().abs().t()).max().item() if side == "x" else (other.double().abs() @ step.abs().t()).max().item()
+        b = (mid.abs() @ other.double().abs().t()).max().item() if side == "x" else (other.double().abs() @ mid.abs().t()).max().item()
+        e = (r.e_dx if side == "x" else r.e_dw)
+        # second order of the uneven part, third of the even one (T^2 (1/T)^n <= 1 for n >= 2), the gradient's own bound
+        bound = a * b + 8 * (a / 2 + b) ** 3 / 6 + 2 * r.e_mean * 2 + 1.01 * (e * step.abs()).sum().item() + 1e-6 * abs(want)
+        assert abs(got[0] - got[1] - want) <= bound, (side, got[0] - got[1], want, bound)
+        assert bound < 0.5 * abs(want) + 0.05, (bound, want)    # (it says something)
+
+
+@pytest.mark.parametrize("dtype,k", [("f32", 0), ("bf16", 0), ("bf16", 6)])
+def test_replays(gpu, dtype, k):
+    """Forward and backward captured once and replayed over new rows, with eager work on the same buffers between,
+    and another graph that shares the workspaces: the eager results each time."""
+    c = Call(gpu, 70, 900, 64, dtype, k=k)
+    other = Call(gpu, 33, 900, 64, dtype, k=k, seed=1)
+    for op in c.ws:   # shared, as large as the larger one
+        big = max(c.ws[op], other.ws[op], key=lambda t: t.numel())
+        c.ws[op] = other.ws[op] = big
+    graphs = []
+    s = torch.cuda.Stream()
+    for call in (c, other):
+        with torch.cuda.stream(s):
+            call.fwd(), call.bwd()
+        s.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            call.fwd()
+            call.bwd()
+        graphs.append(graph)
+    g = torch.Generator().manual_seed(2)
+    for turn in range(4):
+        for call, graph in zip((c, other), graphs):
+            call.dev_x.copy_(torch.randn(call.M, call.K, generator=g).to(call.x.dtype))
+            call.fwd(), call.bwd()
+            torch.cuda.synchronize()
+            want = [t.clone() for t in (call.loss, call.lse, call.zt, call.mean, call.dx, call.dw)]
+            for t in (call.loss, call.lse, call.zt, call.mean, call.dx, call.dw):
+                t.fill_(7.0)
+            graph.replay()
+            torch.cuda.synchronize()
+            for a, b in zip((call.loss, call.lse, call.zt, call.mean, call.dx, call.dw), want):
+                assert torch.equal(a, b), turn
+
+
+def test_two_streams(gpu):
+    """Two calls at once, each with its own workspace."""
+    a, b = Call(gpu, 200, 3000, 128, "bf16"), Call(gpu, 100, 2000, 64, "f32", k=5)
+    sa, sb = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(3):
+        with torch.cuda.stream(sa):
+            a.fwd(), a.bwd()
+        with torch.cuda.stream(sb):
+            b.fwd(), b.bwd()
+    torch.cuda.synchronize()
+    for c in (a, b):
+        c.check_fwd()
+        c.check_bwd()
+
+
+def test_repeats(gpu):
+    """The same bits every time."""
+    for kw in (dict(dtype="bf16"), dict(dtype="f32"), dict(dtype="bf16", k=20)):
+        c = Call(gpu, 400, 2500, 192, **kw)
+        c.fwd(), c.bwd()
+        want = [t.clone() for t in (c.loss, c.lse, c.zt, c.mean, c.dx, c.dw)]
+        for _ in range(3):
+            c.fwd(), c.bwd()
+            assert all(torch.equal(x, y) for x, y in zip((c.loss, c.lse, c.zt, c.mean, c.dx, c.dw), want))
