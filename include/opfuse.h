@@ -827,10 +827,11 @@ of_status of_attn_bwd(const of_attn_desc* d, const void* q, const void* k, const
  *
  * dtype is the type in memory of X and of the head that is read (OF_F32: W->w; OF_BF16: W->w_bf16,
  * uint16 bit patterns) and of the matrix-core operands; logits, statistics and sums are fp32 or wider.
- * Any alignment to the elements' size is accepted.
+ * Any alignment to the elements' size is accepted; rows of 16-byte pieces save a copy.  M * V < 2^37,
+ * V * K <= 2^36, M * K < 2^29, X < 2 GiB.
  */
 typedef struct of_vocab_desc {
-  int64_t M, V, K;        /* rows, vocabulary, width */
+  int64_t M, V, K;        /* rows (<= 2^22), vocabulary (<= 2^21), width (<= 2^20) */
   int64_t ldx;            /* row stride of X and dX; 0 means K; <= 2^21 */
   int32_t dtype;          /* of_dtype of X and W */
   int32_t grad_dtype;     /* backward: of_dtype of dX and dW (OF_BF16 only with dtype OF_BF16).  bf16 operands:

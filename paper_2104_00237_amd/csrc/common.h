@@ -508,5 +508,9 @@ struct VocabArgs {
 size_t vocab_ws_bytes(const VocabArgs& a, bool bwd);
 hipError_t vocab_fwd_launch(const VocabArgs& a, void* ws, hipStream_t stream);
 hipError_t vocab_bwd_launch(const VocabArgs& a, void* ws, hipStream_t stream);
+// Those of bf16 operands.
+size_t vocab_bf16_ws_bytes(const VocabArgs& a, bool bwd);
+hipError_t vocab_bf16_fwd(const VocabArgs& a, void* ws, hipStream_t stream);
+hipError_t vocab_bf16_bwd(const VocabArgs& a, void* ws, hipStream_t stream);
 
 }  // namespace opfuse

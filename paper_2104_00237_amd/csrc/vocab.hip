@@ -1,6 +1,6 @@
-// Vocabulary losses: softmax cross-entropy of an output head and distillation from a teacher's top
-// logits, forward and backward, in pieces of the vocabulary: the logits of a piece are the only ones
-// that ever exist.
+// Vocabulary losses on fp32 operands: softmax cross-entropy of an output head and distillation from a
+// teacher's top logits, forward and backward, in pieces of the vocabulary: the logits of a piece are the
+// only ones that ever exist.
 //
 // Per piece: its logits (the library's linear forward), then the rows' statistics (forward), or
 // their gradient in place and from it dX and dW, or the update of the piece's W (backward): dX reads a
@@ -169,29 +169,12 @@ __global__ __launch_bounds__(256) void vocab_grad_kernel(VocabArgs a, float* __r
 
 // X for the backward's products: rows that get no gradient are zeros there, so that nothing they hold
 // (a NaN times their zero gradient, too) reaches dW.
-template <typename T>
-__global__ __launch_bounds__(256) void vocab_rows_kernel(const T* x, int64_t ldx, const float2* coef, T* dst, int64_t M, int64_t K) {
+__global__ __launch_bounds__(256) void vocab_rows_kernel(const float* x, int64_t ldx, const float2* coef, float* dst, int64_t M,
+                                                         int64_t K) {
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < M * K; i += (int64_t)gridDim.x * 256) {
     const int64_t r = i / K;
     const float2 c = coef[r];
-    dst[i] = c.x == 0.f && c.y == 0.f ? (T)0 : x[r * ldx + (i - r * K)];
-  }
-}
-
-// dst (bf16 or fp32) = src, or += src; rows of n with strides ld.
-template <typename T>
-__global__ __launch_bounds__(256) void vocab_store_kernel(const float* src, int64_t lds, T* dst, int64_t ldd, int64_t rows,
-                                                          int64_t n, int accumulate) {
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * n; i += (int64_t)gridDim.x * 256) {
-    const int64_t r = i / n, c = i - r * n;
-    T* d = dst + r * ldd + c;
-    float v = src[r * lds + c];
-    if constexpr (sizeof(T) == 2) {
-      if (accumulate) v = __fadd_rn(__uint_as_float((uint32_t)*d << 16), v);
-      *d = f32_to_bf16(v);
-    } else {
-      *d = accumulate ? __fadd_rn(*d, v) : v;
-    }
+    dst[i] = c.x == 0.f && c.y == 0.f ? 0.f : x[r * ldx + (i - r * K)];
   }
 }
 
@@ -210,7 +193,7 @@ int64_t piece_of(const VocabArgs& a) {
 
 struct Plan {
   int64_t piece, ldz;
-  size_t z, stat, counts, coef, scale, x, dx, dw, gemm, total;   // offsets; total: bytes
+  size_t z, stat, counts, coef, scale, x, gemm, total;   // offsets; total: bytes
 };
 
 Plan plan_of(const VocabArgs& a, bool bwd) {
@@ -229,18 +212,14 @@ Plan plan_of(const VocabArgs& a, bool bwd) {
   p.counts = take((size_t)a.M * 4);
   p.scale = take(4);
   auto bytes = [&](int kind, int64_t P, int64_t Q, int64_t R) {
-    return a.bf16 ? gemm_bf16_workspace_bytes(kind, (int)P, (int)Q, (int)R) : gemm_workspace_bytes(kind, (int)P, (int)Q, (int)R);
+    return gemm_workspace_bytes(kind, (int)P, (int)Q, (int)R);
   };
   size_t g = 0;
   for (int64_t n : {p.piece, a.V % p.piece ? a.V % p.piece : p.piece}) {
     g = std::max(g, bytes(EPI_FWD, a.M, n, a.K));
     if (bwd) g = std::max({g, bytes(EPI_DGRAD, a.M, a.K, n), bytes(EPI_WGRAD, n, a.K, a.M)});
   }
-  if (bwd) p.x = take((size_t)a.M * a.K * (a.bf16 ? 2 : 4));
-  if (bwd && a.gbf) {
-    p.dx = take((size_t)a.M * a.K * 4);
-    p.dw = take((size_t)p.piece * a.K * 4);
-  }
+  if (bwd) p.x = take((size_t)a.M * a.K * 4);
   p.gemm = take(g);
   p.total = at;
   return p;
@@ -268,15 +247,12 @@ struct Pieces {
   char* ws;
   hipStream_t s;
   float* z() const { return (float*)(ws + p.z); }
-  hipError_t product(int kind, GemmProblem pr, const EpiArgs& ea) const {
-    return a.bf16 ? gemm_bf16_launch(kind, pr, ea, ws + p.gemm, s) : gemm_launch(kind, pr, ea, ws + p.gemm, s);
+  hipError_t product(int kind, const GemmProblem& pr, const EpiArgs& ea) const {
+    return gemm_launch(kind, pr, ea, ws + p.gemm, s);
   }
-  const float* w(int64_t v0) const {
-    return a.bf16 ? (const float*)(a.W.w_bf16 + v0 * a.K) : a.W.w + v0 * a.K;
-  }
-  hipError_t logits(const void* x, int64_t ldx, int64_t v0, int64_t n) const {
-    GemmProblem pr{(const float*)x, ldx, 1, w(v0), a.K, 1, (int)a.M, (int)n, (int)a.K};
-    pr.a_bf16 = pr.b_bf16 = a.bf16;
+  const float* w(int64_t v0) const { return a.W.w + v0 * a.K; }
+  hipError_t logits(const float* x, int64_t ldx, int64_t v0, int64_t n) const {
+    const GemmProblem pr{x, ldx, 1, w(v0), a.K, 1, (int)a.M, (int)n, (int)a.K};
     EpiArgs ea = no_epi();
     ea.out = z(), ea.ldo = p.ldz, ea.ldz = p.ldz, ea.ldr = p.ldz;
     return product(EPI_FWD, pr, ea);
@@ -291,15 +267,16 @@ struct Pieces {
 
 }  // namespace
 
-size_t vocab_ws_bytes(const VocabArgs& a, bool bwd) { return plan_of(a, bwd).total; }
+size_t vocab_ws_bytes(const VocabArgs& a, bool bwd) { return a.bf16 ? vocab_bf16_ws_bytes(a, bwd) : plan_of(a, bwd).total; }
 
 hipError_t vocab_fwd_launch(const VocabArgs& a, void* ws, hipStream_t s) {
+  if (a.bf16) return vocab_bf16_fwd(a, ws, s);
   const Pieces g{a, plan_of(a, false), (char*)ws, s};
   Stat* stat = (Stat*)(g.ws + g.p.stat);
   float* counts = (float*)(g.ws + g.p.counts);
   for (int64_t v0 = 0; v0 < a.V; v0 += g.p.piece) {
     const int64_t n = std::min(g.p.piece, a.V - v0);
-    TRY(g.logits(a.x, a.ldx, v0, n));
+    TRY(g.logits((const float*)a.x, a.ldx, v0, n));
     hipLaunchKernelGGL(vocab_stats_kernel, dim3((unsigned)a.M), dim3(256), 0, s, a, g.z(), g.p.ldz, v0, (int)n, stat);
     TRY(hipGetLastError());
   }
@@ -310,6 +287,7 @@ hipError_t vocab_fwd_launch(const VocabArgs& a, void* ws, hipStream_t s) {
 }
 
 hipError_t vocab_bwd_launch(const VocabArgs& a, void* ws, hipStream_t s) {
+  if (a.bf16) return vocab_bf16_bwd(a, ws, s);
   const Pieces g{a, plan_of(a, true), (char*)ws, s};
   const Plan& p = g.p;
   float2* coef = (float2*)(g.ws + p.coef);
@@ -319,31 +297,23 @@ hipError_t vocab_bwd_launch(const VocabArgs& a, void* ws, hipStream_t s) {
   TRY(hipGetLastError());
   if (scale) hipLaunchKernelGGL(vocab_scale_kernel, dim3(1), dim3(1024), 0, s, counts, a.M, scale);
   TRY(hipGetLastError());
-  void* x = g.ws + p.x;
-  if (a.bf16)
-    hipLaunchKernelGGL(vocab_rows_kernel<uint16_t>, dim3(store_grid(a.M * a.K)), dim3(256), 0, s, (const uint16_t*)a.x, a.ldx,
-                       coef, (uint16_t*)x, a.M, a.K);
-  else
-    hipLaunchKernelGGL(vocab_rows_kernel<float>, dim3(store_grid(a.M * a.K)), dim3(256), 0, s, (const float*)a.x, a.ldx, coef,
-                       (float*)x, a.M, a.K);
+  float* x = (float*)(g.ws + p.x);
+  hipLaunchKernelGGL(vocab_rows_kernel, dim3(store_grid(a.M * a.K)), dim3(256), 0, s, (const float*)a.x, a.ldx, coef, x, a.M, a.K);
   TRY(hipGetLastError());
-  float* dx = a.gbf ? (float*)(g.ws + p.dx) : (float*)a.dx;
-  const int64_t lddx = a.gbf ? a.K : a.ldx;
+  float* dx = (float*)a.dx;
   for (int64_t v0 = 0; v0 < a.V; v0 += p.piece) {
     const int64_t n = std::min(p.piece, a.V - v0);
     TRY(g.logits(x, a.K, v0, n));
     hipLaunchKernelGGL(vocab_grad_kernel, dim3((unsigned)a.M), dim3(256), 0, s, a, g.z(), p.ldz, v0, (int)n, coef, scale);
     TRY(hipGetLastError());
     if (a.dx) {
-      GemmProblem pr{g.z(), p.ldz, 1, g.w(v0), 1, a.K, (int)a.M, (int)a.K, (int)n};
-      pr.b_bf16 = a.bf16;
+      const GemmProblem pr{g.z(), p.ldz, 1, g.w(v0), 1, a.K, (int)a.M, (int)a.K, (int)n};
       EpiArgs ea = no_epi();
-      ea.out = dx, ea.ldo = ea.ldp = ea.ldr = lddx;
+      ea.out = dx, ea.ldo = ea.ldp = ea.ldr = a.ldx;
       ea.res = v0 ? dx : nullptr;
       TRY(g.product(EPI_DGRAD, pr, ea));
     }
-    GemmProblem pr{g.z(), 1, p.ldz, (const float*)x, 1, a.K, (int)n, (int)a.K, (int)a.M};
-    pr.b_bf16 = a.bf16;
+    const GemmProblem pr{g.z(), 1, p.ldz, x, 1, a.K, (int)n, (int)a.K, (int)a.M};
     EpiArgs ea = no_epi();
     ea.ldo = a.K;
     if (a.fused) {
@@ -351,22 +321,13 @@ hipError_t vocab_bwd_launch(const VocabArgs& a, void* ws, hipStream_t s) {
       ea.gW = a.gW ? a.gW + v0 * a.K : nullptr;
       ea.opt = a.opt;
       TRY(g.product(EPI_WGRAD_BF, pr, ea));
-    } else if (a.dw && !a.gbf) {
+    } else if (a.dw) {
       ea.out = (float*)a.dw + v0 * a.K;
       ea.accumulate = a.accumulate;
       TRY(g.product(EPI_WGRAD, pr, ea));
-    } else if (a.dw) {
-      ea.out = (float*)(g.ws + p.dw);
-      TRY(g.product(EPI_WGRAD, pr, ea));
-      hipLaunchKernelGGL(vocab_store_kernel<uint16_t>, dim3(store_grid(n * a.K)), dim3(256), 0, s, ea.out, a.K,
-                         (uint16_t*)a.dw + v0 * a.K, a.K, n, a.K, a.accumulate);
-      TRY(hipGetLastError());
     }
   }
-  if (a.dx && a.gbf)
-    hipLaunchKernelGGL(vocab_store_kernel<uint16_t>, dim3(store_grid(a.M * a.K)), dim3(256), 0, s, dx, a.K,
-                       (uint16_t*)a.dx, a.ldx, a.M, a.K, 0);
-  return hipGetLastError();
+  return hipSuccess;
 }
 
 }  // namespace opfuse

@@ -56,7 +56,8 @@ BAD = [(L.OF_EINVAL, dict(M=0)), (L.OF_EINVAL, dict(V=0)), (L.OF_EINVAL, dict(K=
        (L.OF_EINVAL, dict(softcap=float("nan"))), (L.OF_EUNSUPPORTED, dict(softcap=2.0 ** 41)),
        (L.OF_EINVAL, dict(z_loss=-1e-4)), (L.OF_EINVAL, dict(z_loss=float("inf"))), (L.OF_EINVAL, dict(temperature=-1.0)),
        (L.OF_EUNSUPPORTED, dict(temperature=2.0 ** -41)), (L.OF_EUNSUPPORTED, dict(M=(1 << 22) + 1)),
-       (L.OF_EUNSUPPORTED, dict(V=(1 << 22) + 1)), (L.OF_EUNSUPPORTED, dict(K=(1 << 20) + 1)),
+       (L.OF_EUNSUPPORTED, dict(V=(1 << 21) + 1)), (L.OF_EUNSUPPORTED, dict(K=(1 << 20) + 1)),
+       (L.OF_EUNSUPPORTED, dict(M=1 << 20, V=1 << 17)), (L.OF_EUNSUPPORTED, dict(V=1 << 21, K=(1 << 15) + 1)),
        (L.OF_EUNSUPPORTED, dict(ldx=(1 << 21) + 1)), (L.OF_EUNSUPPORTED, dict(M=1 << 20, ldx=1 << 10)),
        (L.OF_EUNSUPPORTED, dict(M=1 << 21, topk=1024))]
 
