@@ -494,7 +494,7 @@ struct VocabArgs {
   const void* teacher;             // [M, k] logits
   bool tbf;                        // the teacher's logits are bf16
   int k;
-  float cap, z_loss, T;            // cap 0: none
+  float cap, rcap, z_loss, T;      // cap 0: none; rcap = 1 / cap
   float *loss, *lse, *zt, *mean;   // forward: [M], [M], [M, k], [1] or NULL
   // backward
   const float* dloss;              // [M] or NULL: the mean's
@@ -508,9 +508,10 @@ struct VocabArgs {
 size_t vocab_ws_bytes(const VocabArgs& a, bool bwd);
 hipError_t vocab_fwd_launch(const VocabArgs& a, void* ws, hipStream_t stream);
 hipError_t vocab_bwd_launch(const VocabArgs& a, void* ws, hipStream_t stream);
-// Those of bf16 operands.
-size_t vocab_bf16_ws_bytes(const VocabArgs& a, bool bwd);
-hipError_t vocab_bf16_fwd(const VocabArgs& a, void* ws, hipStream_t stream);
-hipError_t vocab_bf16_bwd(const VocabArgs& a, void* ws, hipStream_t stream);
+// Those of bf16 operands, and of fp32 operands of more than a few rows: logits in accumulators only.
+bool vocab_tiles_ok(const VocabArgs& a);
+size_t vocab_tiles_ws_bytes(const VocabArgs& a, bool bwd);
+hipError_t vocab_tiles_fwd(const VocabArgs& a, void* ws, hipStream_t stream);
+hipError_t vocab_tiles_bwd(const VocabArgs& a, void* ws, hipStream_t stream);
 
 }  // namespace opfuse

@@ -1427,6 +1427,7 @@ of_status check_vocab(const of_vocab_desc* d, bool bwd, VocabArgs* a) {
   a->tbf = d->teacher_dtype == OF_BF16;
   a->k = std::max<int32_t>(d->topk, 1);
   a->cap = d->softcap;
+  a->rcap = a->cap ? 1.f / a->cap : 0.f;
   a->z_loss = d->z_loss;
   a->T = d->temperature ? d->temperature : 1.f;
   return OF_OK;

@@ -32,7 +32,22 @@ __device__ __forceinline__ float wave_max(float v) {
   return v;
 }
 
-__device__ __forceinline__ float vocab_cap(float s, float cap) { return cap > 0.f ? cap * tanhf(s / cap) : s; }
+// tanh(x) as x P(x^2) / Q(x^2), fitted in float64 for the least relative error on (0, 9] (2.1e-8; with fp32
+// rounding at most 3.2e-7, rms 5.3e-8, near 0 too, where 1 - 2 / (e^2x + 1) has nothing left); beyond 9 it
+// is 1 within half a step.  A third of tanhf's instructions: a capped tile of logits takes 65536 of them.
+__device__ __forceinline__ float vocab_tanh(float x) {
+  x = fabsf(x) > 9.f ? copysignf(9.f, x) : x;   // (a NaN stays)
+  const float u = __fmul_rn(x, x);
+  float p = 1.33548417e-08f, q = 7.77663388e-07f;
+  p = __fmaf_rn(p, u, 2.06092191e-05f), q = __fmaf_rn(q, u, 3.28564871e-04f);
+  p = __fmaf_rn(p, u, 3.49559658e-03f), q = __fmaf_rn(q, u, 2.58770157e-02f);
+  p = __fmaf_rn(p, u, 1.33810326e-01f), q = __fmaf_rn(q, u, 4.67143476e-01f);
+  p = __fmaf_rn(p, u, 1.f), q = __fmaf_rn(q, u, 1.f);
+  return __fmul_rn(__fmul_rn(x, p), __builtin_amdgcn_rcpf(q));
+}
+__device__ __forceinline__ float vocab_cap(float s, float cap, float rcap) {
+  return cap > 0.f ? __fmul_rn(cap, vocab_tanh(__fmul_rn(s, rcap))) : s;
+}
 
 // A row's target as a wavefront sees it: entry j has weight exp(t_j / T - top) / total.
 // Entries with a negative id are left out whatever their logit; a row none of whose entries has a

@@ -1,4 +1,4 @@
-// Vocabulary losses on fp32 operands: softmax cross-entropy of an output head and distillation from a
+// Vocabulary losses of few fp32 rows: softmax cross-entropy of an output head and distillation from a
 // teacher's top logits, forward and backward, in pieces of the vocabulary: the logits of a piece are the
 // only ones that ever exist.
 //
@@ -37,16 +37,16 @@ __global__ __launch_bounds__(256) void vocab_stats_kernel(VocabArgs a, const flo
   const int64_t row = blockIdx.x;
   const float* s = z + row * ldz;
   float m = -INFINITY;
-  for (int v = threadIdx.x; v < n; v += 256) m = fmaxf(m, __fdiv_rn(vocab_cap(s[v], a.cap), a.T));
+  for (int v = threadIdx.x; v < n; v += 256) m = fmaxf(m, __fdiv_rn(vocab_cap(s[v], a.cap, a.rcap), a.T));
   const float shift = stat_shift(m);
   float sum = 0.f;
   for (int v = threadIdx.x; v < n; v += 256)
-    sum = __fadd_rn(sum, expf(__fdiv_rn(vocab_cap(s[v], a.cap), a.T) - shift));
+    sum = __fadd_rn(sum, expf(__fdiv_rn(vocab_cap(s[v], a.cap, a.rcap), a.T) - shift));
   const Stat mine = block_stat(Stat{m, sum}, sh);
   if (threadIdx.x == 0) stat[row] = v0 == 0 ? mine : stat_join(stat[row], mine);
   for (int j = threadIdx.x; j < a.k; j += 256) {
     const int64_t i = row * a.k + j, id = a.ids[i];
-    if (id >= v0 && id < v0 + n) a.zt[i] = vocab_cap(s[id - v0], a.cap);
+    if (id >= v0 && id < v0 + n) a.zt[i] = vocab_cap(s[id - v0], a.cap, a.rcap);
     else if (v0 == 0 && (id < 0 || id >= a.V)) a.zt[i] = 0.f;
   }
 }
@@ -126,11 +126,11 @@ __global__ __launch_bounds__(256) void vocab_grad_kernel(VocabArgs a, float* __r
   const float g = scale ? *scale : 1.f, lse = a.lse[row];
   const float ct = __fmul_rn(c.x, g), cp = __fmul_rn(c.y, g);
   auto grad = [&](float logit, float q) {
-    const float zc = vocab_cap(logit, a.cap);
+    const float zc = vocab_cap(logit, a.cap, a.rcap);
     const float p = expf(__fdiv_rn(zc, a.T) - lse);
     float d = __fmaf_rn(cp, p, -__fmul_rn(ct, q));
     if (a.cap > 0.f) {
-      const float r = zc / a.cap;
+      const float r = __fmul_rn(zc, a.rcap);
       d = __fmul_rn(d, __fmaf_rn(-r, r, 1.f));
     }
     return d;
@@ -267,10 +267,12 @@ struct Pieces {
 
 }  // namespace
 
-size_t vocab_ws_bytes(const VocabArgs& a, bool bwd) { return a.bf16 ? vocab_bf16_ws_bytes(a, bwd) : plan_of(a, bwd).total; }
+size_t vocab_ws_bytes(const VocabArgs& a, bool bwd) {
+  return vocab_tiles_ok(a) ? vocab_tiles_ws_bytes(a, bwd) : plan_of(a, bwd).total;
+}
 
 hipError_t vocab_fwd_launch(const VocabArgs& a, void* ws, hipStream_t s) {
-  if (a.bf16) return vocab_bf16_fwd(a, ws, s);
+  if (vocab_tiles_ok(a)) return vocab_tiles_fwd(a, ws, s);
   const Pieces g{a, plan_of(a, false), (char*)ws, s};
   Stat* stat = (Stat*)(g.ws + g.p.stat);
   float* counts = (float*)(g.ws + g.p.counts);
@@ -287,7 +289,7 @@ hipError_t vocab_fwd_launch(const VocabArgs& a, void* ws, hipStream_t s) {
 }
 
 hipError_t vocab_bwd_launch(const VocabArgs& a, void* ws, hipStream_t s) {
-  if (a.bf16) return vocab_bf16_bwd(a, ws, s);
+  if (vocab_tiles_ok(a)) return vocab_tiles_bwd(a, ws, s);
   const Pieces g{a, plan_of(a, true), (char*)ws, s};
   const Plan& p = g.p;
   float2* coef = (float2*)(g.ws + p.coef);

@@ -14,6 +14,12 @@
 // banks; the others as rows [r][BX] with 64-byte blocks swizzled by r % 4, read with ds_read_b64_tr_b16.
 // A load to LDS writes lane i at base + 16 i, so the swizzle is applied to the address each lane loads.
 // Rows are whole 16-byte pieces at 16-byte boundaries; r past R and x past the operand read as zeros.
+//
+// fp32 operands (PL = 3) come as three bf16 planes each, x = high + middle + low with every part the
+// nearest bf16 to what the ones before leave (the splitting of Henry, Tang and Heinecke, Leveraging the
+// bfloat16 Artificial Intelligence Datatype For Higher-Precision Computations, ARITH 2019).  Parts shrink
+// by 2^-9, so three hold all 24 bits, and of the nine partial products the three below 2^-26 of the
+// whole are left out: six are summed in one accumulator.
 #pragma once
 
 #include <type_traits>
@@ -107,6 +113,7 @@ struct TileProblem {
   int P, Q, R;
   const int* rows;
   int gp, gq, S;        // tiles, and parts of the reduction
+  int64_t pa, pb;       // PL = 3: elements from one plane to the next
 };
 enum TileRows { ROWS_NONE = 0, ROWS_P = 1, ROWS_Q = 2, ROWS_R = 3 };
 
@@ -137,7 +144,7 @@ __device__ __forceinline__ bool tile_place(const TileProblem& pr, int rows_dim, 
 }
 
 // The main loop.  e(place, acc, lds, lane, wave, wp, wq): the finished tile; lds: the ring, free.
-template <class T, bool A_RC, bool B_RC, class Epi>
+template <class T, int PL, bool A_RC, bool B_RC, class Epi>
 __global__ __launch_bounds__(T::NT, T::OCC) void tile_kernel(TileProblem pr, Epi e) {
   constexpr int IP = T::IP, IQ = T::IQ, NK = T::NK, NL = T::NL, STAGE = T::ABYTES + T::BBYTES;
   __shared__ __attribute__((aligned(1024))) char s0[STAGE], s1[STAGE], s2[STAGE], s3[STAGE];
@@ -165,11 +172,15 @@ __global__ __launch_bounds__(T::NT, T::OCC) void tile_kernel(TileProblem pr, Epi
   };
   Frags f[2];
 
-  // loads [from, to) of stage c
-  auto request = [&](char* s, int c, int from, int to) {
-    const int nr = c < nst ? t.rend - t.rbeg - c * T::BK : 0;   // 0 past the end: zeros
-    const int64_t at = c < nst ? c : 0;
-    const rsrc_t ra = make_rsrc(A + at * da), rb = make_rsrc(B + at * db);
+  // loads [from, to) of stage c.  Planes: a stage for each of the products high high, high middle, high
+  // low, middle high, middle middle, low high of the same reduction elements
+  auto request = [&](char* s, int c, int from, int to) __attribute__((always_inline)) {
+    const int k = PL == 1 ? c : c / 6, pi = PL == 1 ? 0 : (c - k * 6) * 4;
+    const int nr = k < nst ? t.rend - t.rbeg - k * T::BK : 0;   // 0 past the end: zeros
+    const int64_t at = k < nst ? k : 0;
+    const char *a = A + at * da, *b = B + at * db;
+    if constexpr (PL == 3) a += (0x211000 >> pi & 3) * pr.pa * 2, b += (0x010210 >> pi & 3) * pr.pb * 2;
+    const rsrc_t ra = make_rsrc(a), rb = make_rsrc(b);
 #pragma unroll
     for (int i = 0; i < NL; ++i) {
       if (i < from || i >= to) continue;
@@ -181,13 +192,13 @@ __global__ __launch_bounds__(T::NT, T::OCC) void tile_kernel(TileProblem pr, Epi
       }
     }
   };
-  auto read = [&](Frags& d, const char* s, int k) {
+  auto read = [&](Frags& d, const char* s, int k) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < IP; ++i) d.a[i] = stage_frag<A_RC, T::BP, T::BK>(s, (wp * IP + i) * 32, k, lane);
 #pragma unroll
     for (int j = 0; j < IQ; ++j) d.b[j] = stage_frag<B_RC, T::BQ, T::BK>(s + T::ABYTES, (wq * IQ + j) * 32, k, lane);
   };
-  auto mfma = [&](const Frags& d) {
+  auto mfma = [&](const Frags& d) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < IP; ++i)
 #pragma unroll
@@ -195,7 +206,7 @@ __global__ __launch_bounds__(T::NT, T::OCC) void tile_kernel(TileProblem pr, Epi
   };
   // MFMAs with a share of the LDS reads and of the loads behind each
   constexpr int READS = (A_RC ? 1 : 2) * IP + (B_RC ? 1 : 2) * IQ, MF = IP * IQ;
-  auto sched = [&](auto N) {
+  auto sched = [&](auto N) __attribute__((always_inline)) {
     constexpr int n = decltype(N)::value;
 #pragma unroll
     for (int g = 0; g < MF; ++g) {
@@ -213,7 +224,7 @@ __global__ __launch_bounds__(T::NT, T::OCC) void tile_kernel(TileProblem pr, Epi
   constexpr int L1 = (NL + NK - 1) / NK;
 
   // Stage c is in s, stage c + 1 lands in sn, stage c + 3 is asked for in s3n.
-  auto stage = [&](char* s, char* sn, char* s3n, int c) {
+  auto stage = [&](char* s, char* sn, char* s3n, int c) __attribute__((always_inline)) {
     each(std::make_integer_sequence<int, NK - 1>{}, [&](auto K_) {
       constexpr int k = decltype(K_)::value;
       read(f[(k + 1) & 1], s, k + 1);
@@ -239,7 +250,7 @@ __global__ __launch_bounds__(T::NT, T::OCC) void tile_kernel(TileProblem pr, Epi
   __builtin_amdgcn_sched_barrier(0);
   // (stages past the end are zeros: a branch around them makes the compiler move accumulators
   // between register files)
-  for (int c = 0; c < nst; c += 4) {
+  for (int c = 0; c < (PL == 1 ? nst : 6 * nst); c += 4) {
     stage(s0, s1, s3, c);
     stage(s1, s2, s0, c + 1);
     stage(s2, s3, s1, c + 2);

@@ -1,0 +1,1032 @@
+// Vocabulary losses on the bf16 matrix cores: the logits' product ends in the rows' statistics (forward)
+// or in the logits' gradient (backward), so that logits exist in accumulators only.
+//
+// Forward, three launches: the rows' entries sorted by the tile of logits that holds them; the logits'
+// product, whose tiles leave a maximum and a sum of exponentials a row and the entries' logits; the
+// statistics joined, losses and their mean.
+// Backward: the rows that get a gradient, gathered (what others hold is never read, and they cost no
+// work); then per piece of the vocabulary the logits' product again, stored as their gradient in bf16,
+// dX summed over the pieces in fp32, dW (or the update) of the piece's rows; at the end dX rounded and
+// put back to its rows.  A common factor (T over the rows that count) is left out of the stored gradient
+// and applied to the sums: p - 1 near -1 then rounds to itself.
+// Six products' worth of flops for M V K instead of the four that stored logits would need.
+//
+// fp32 operands take the same way as three bf16 planes each (vocab_tile.h), made beforehand: X once, W
+// and the logits' gradient a piece at a time.
+
+#include <algorithm>
+#include <cstring>
+
+#include "vocab_tile.h"
+
+namespace opfuse {
+
+namespace {
+
+// Tiles (rows x columns, in wavefronts of 4x2, 2x2 and 1x1 blocks): a 256x256 tile a CU with two
+// wavefronts a SIMD, 128x128 where those would not fill the chip, 32 wide for few rows.
+using Big = TileShape<4, 2, 2, 4, 32, 2>;
+using Mid = TileShape<2, 2, 2, 2, 32, 2>;
+using FewQ = TileShape<1, 1, 4, 1, 64, 2>;   // 128 x 32
+using FewP = TileShape<1, 1, 1, 4, 64, 2>;   // 32 x 128
+
+constexpr int kFew = 32;                     // rows up to which a product's tiles are 32 wide
+
+int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
+int64_t per(int64_t n, int64_t each) { return (n + each - 1) / each; }
+bool odd_rows(const void* p, int64_t ld, int64_t K) { return !aligned16(p) || ld % 8 != 0 || K % 8 != 0; }
+
+// A wavefront's own part of the ring once the main loop is done: BYTES each.
+template <class T, int BYTES>
+__device__ __forceinline__ char* own_lds(char* const (&ring)[4], int wave) {
+  constexpr int EACH = (T::ABYTES + T::BBYTES) / BYTES;
+  static_assert(EACH * 4 >= T::NW, "room for every wavefront");
+  const int r = wave / EACH;
+  return (r == 0 ? ring[0] : r == 1 ? ring[1] : r == 2 ? ring[2] : ring[3]) + (wave % EACH) * BYTES;
+}
+// The nearest bf16s of two values, which keep what that leaves.  Infinity (and what would round to it)
+// counts as the largest bf16: with an infinite high part, the other operand's low parts of 0 would make a NaN.
+__device__ __forceinline__ uint32_t take_part(float& x, float& y) {
+  constexpr float most = 3.38953139e38f;
+  x = fabsf(x) > most ? copysignf(most, x) : x;   // (a NaN stays)
+  y = fabsf(y) > most ? copysignf(most, y) : y;
+  const uint32_t w = pack2(x, y);
+  x = __fsub_rn(x, __uint_as_float(w << 16));
+  y = __fsub_rn(y, __uint_as_float(w & 0xffff0000u));
+  return w;
+}
+
+// This wavefront's LDS writes are there for all its lanes.
+__device__ __forceinline__ void wave_lds_sync() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// ---------------------------------------------------------------------- forward
+// A row's entries by tile: off[row tile][vocabulary tile] .. of list[row tile], each entry its row and
+// its column in the tile and its number in the row.
+struct Entries {
+  int* off;            // [row tiles][vtiles + 1]
+  uint32_t* list;      // [row tiles][BQ * k]
+  int vtiles;
+};
+
+template <int BP, int BQ>
+__global__ __launch_bounds__(1024) void vocab_sort_kernel(VocabArgs a, Entries en, int* done) {
+  extern __shared__ int bins[];   // [vtiles]
+  __shared__ int part[1024];
+  const int t = threadIdx.x;
+  const int64_t row0 = (int64_t)blockIdx.x * BQ;
+  const int n = (int)min((int64_t)BQ, a.M - row0) * a.k;
+  const int64_t* ids = a.ids + row0 * a.k;
+  if (blockIdx.x == 0 && t == 0) *done = 0;
+  for (int i = t; i < en.vtiles; i += 1024) bins[i] = 0;
+  __syncthreads();
+  constexpr int U = 8;   // loads in flight
+  for (int i0 = t; i0 < n; i0 += 1024 * U) {
+    int64_t id[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) id[u] = i0 + u * 1024 < n ? ids[i0 + u * 1024] : 0;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = i0 + u * 1024;
+      if (i >= n) continue;
+      if (id[u] >= 0 && id[u] < a.V) atomicAdd(&bins[(int)id[u] / BP], 1);
+      else a.zt[row0 * a.k + i] = 0.f;
+    }
+  }
+  __syncthreads();
+  // exclusive sums: a run of bins each thread, the runs' totals in steps of doubling
+  const int run = (en.vtiles + 1023) / 1024, b0 = min(en.vtiles, t * run), b1 = min(en.vtiles, b0 + run);
+  int sum = 0;
+  for (int b = b0; b < b1; ++b) sum += bins[b];
+  part[t] = sum;
+  __syncthreads();
+  for (int d = 1; d < 1024; d <<= 1) {
+    const int v = t >= d ? part[t - d] : 0;
+    __syncthreads();
+    part[t] += v;
+    __syncthreads();
+  }
+  int at = part[t] - sum;
+  int* off = en.off + (int64_t)blockIdx.x * (en.vtiles + 1);
+  for (int b = b0; b < b1; ++b) {
+    const int c = bins[b];
+    off[b] = at;
+    bins[b] = at;
+    at += c;
+  }
+  if (t == 1023) off[en.vtiles] = part[1023];
+  __syncthreads();
+  // (the order of a tile's entries may differ from run to run: each goes to a place of its own)
+  uint32_t* list = en.list + (int64_t)blockIdx.x * BQ * a.k;
+  for (int i0 = t; i0 < n; i0 += 1024 * U) {
+    int64_t id[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) id[u] = i0 + u * 1024 < n ? ids[i0 + u * 1024] : -1;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (id[u] < 0 || id[u] >= a.V) continue;
+      const int i = i0 + u * 1024, tile = (int)id[u] / BP, row = i / a.k;
+      list[atomicAdd(&bins[tile], 1)] = (uint32_t)row | (uint32_t)((int)id[u] - tile * BP) << 8 | (uint32_t)(i - row * a.k) << 16;
+    }
+  }
+}
+
+// Two statistics in units of log2.
+__device__ __forceinline__ float2 stat2_join(float2 x, float2 y) {
+  const float m = fmaxf(x.x, y.x), s = stat_shift(m);
+  return make_float2(m, __fadd_rn(__fmul_rn(x.y, __builtin_amdgcn_exp2f(x.x - s)), __fmul_rn(y.y, __builtin_amdgcn_exp2f(y.x - s))));
+}
+
+// A = W, B = X: a lane's accumulators are one row's logits, for statistics within the lane.
+template <class T>
+struct StatEpi {
+  static constexpr int ROWS = ROWS_NONE;
+  float2* part;        // [vtiles][M]: maximum (in units of log2) and sum
+  float* zt;
+  Entries en;
+  int tile0;           // the piece's first vocabulary tile
+  int64_t M;
+  int k;
+  float cap, rcap, c;  // c = log2(e) / T
+  template <class Acc>
+  __device__ __forceinline__ void operator()(const TilePlace& t, Acc& acc, char* const (&ring)[4], int lane, int wave, int wp,
+                                             int wq) const {
+    constexpr int IP = T::IP, IQ = T::IQ;
+    const int h4 = (lane >> 5) * 4, l32 = lane & 31;
+    const int np = t.np - wp * IP * 32;   // vocabulary entries from this wavefront's first
+    if (cap > 0.f) {
+#pragma unroll
+      for (int i = 0; i < IP; ++i)
+#pragma unroll
+        for (int j = 0; j < IQ; ++j)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) acc[i][j][r] = vocab_cap(acc[i][j][r], cap, rcap);
+    }
+    const int tile = tile0 + t.p0 / T::BP, rt = t.q0 / T::BQ;
+    const int* off = en.off + (int64_t)rt * (en.vtiles + 1) + tile;
+    const int e0 = off[0], e1 = off[1];
+    if (e1 > e0) {
+      const uint32_t* list = en.list + (int64_t)rt * T::BQ * k;
+      float* lds = (float*)own_lds<T, (IP * IQ * 2048 > 4096 ? IP * IQ * 2048 : 4096)>(ring, wave);
+      constexpr int U = 4;   // entries of a lane at a time
+      for (int b = e0; b < e1; b += 64 * U) {
+        uint32_t x[U];
+        int block[U];          // that of this wavefront's which holds the entry
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          const int e = b + u * 64 + lane;
+          x[u] = e < e1 ? list[e] : 0;
+          const int i = ((x[u] >> 13) & 7) - wp * IP, j = ((x[u] >> 5) & 7) - wq * IQ;
+          block[u] = e < e1 && i >= 0 && i < IP && j >= 0 && j < IQ ? i * IQ + j : -1;
+        }
+#pragma unroll
+        for (int i = 0; i < IP; ++i)
+#pragma unroll
+          for (int j = 0; j < IQ; ++j) {
+            bool mine = false;
+#pragma unroll
+            for (int u = 0; u < U; ++u) mine |= block[u] == i * IQ + j;
+            if (!__any(mine)) continue;
+#pragma unroll
+            for (int r = 0; r < 16; ++r) lds[(8 * (r >> 2) + h4 + (r & 3)) * 32 + l32] = acc[i][j][r];
+            wave_lds_sync();
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+              if (block[u] == i * IQ + j)
+                zt[((int64_t)t.q0 + (x[u] & 255)) * k + (x[u] >> 16)] = lds[((x[u] >> 8) & 31) * 32 + (x[u] & 31)];
+            wave_lds_sync();
+          }
+      }
+    }
+    float m[IQ], s[IQ];
+    auto in = [&](int i, int r) { return i * 32 + 8 * (r >> 2) + h4 + (r & 3) < np; };
+    if (np < IP * 32) {   // the last tile: what lies past the vocabulary has no probability
+#pragma unroll
+      for (int i = 0; i < IP; ++i)
+#pragma unroll
+        for (int j = 0; j < IQ; ++j)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) acc[i][j][r] = in(i, r) ? acc[i][j][r] : -INFINITY;
+    }
+#pragma unroll
+    for (int j = 0; j < IQ; ++j) {
+      m[j] = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < IP; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) m[j] = fmaxf(m[j], acc[i][j][r]);
+      m[j] = fmaxf(m[j], __shfl_xor(m[j], 32));
+      const float shift = __fmul_rn(stat_shift(m[j]), c);
+      s[j] = 0.f;
+#pragma unroll
+      for (int i = 0; i < IP; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[j] = __fadd_rn(s[j], __builtin_amdgcn_exp2f(__fmaf_rn(acc[i][j][r], c, -shift)));
+      s[j] = __fadd_rn(s[j], __shfl_xor(s[j], 32));
+      m[j] = m[j] == -INFINITY ? m[j] : shift;
+    }
+    // the wavefronts of a row's vocabulary entries join in LDS
+    float2* sh = (float2*)ring[0];   // [WP][BQ]
+    __syncthreads();
+    if (lane < 32) {
+#pragma unroll
+      for (int j = 0; j < IQ; ++j) sh[wp * T::BQ + (wq * IQ + j) * 32 + l32] = make_float2(m[j], s[j]);
+    }
+    __syncthreads();
+    const int q = wave * 64 + lane;
+    if (q < T::BQ && q < t.nq) {
+      float2 v = sh[q];
+#pragma unroll
+      for (int w = 1; w < T::WP; ++w) v = stat2_join(v, sh[w * T::BQ + q]);
+      part[(int64_t)tile * M + t.q0 + q] = v;
+    }
+  }
+};
+
+// Rows' statistics joined, RB rows a workgroup; their losses; the last workgroup takes the mean from
+// the workgroups' sums, in their order.
+constexpr int kJoinRows = 8, kJoinFew = 256;   // one row a workgroup up to kJoinFew rows
+template <int RB>
+__global__ __launch_bounds__(256) void vocab_join_kernel(VocabArgs a, const float2* part, int parts, double2* sums, int* done) {
+  __shared__ float2 sh[256];
+  __shared__ float ll[RB], cc[RB];
+  __shared__ int last;
+  const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
+  const int64_t row0 = (int64_t)blockIdx.x * RB, row = row0 + t % RB;
+  float2 v = make_float2(-INFINITY, 0.f);
+  constexpr int U = 8, STEP = 256 / RB;
+  for (int p = t / RB; p < parts; p += STEP * U) {
+    float2 x[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      x[u] = p + u * STEP < parts && row < a.M ? part[(int64_t)(p + u * STEP) * a.M + row] : make_float2(-INFINITY, 0.f);
+    // (one maximum for the eight: a chain of joins would be two exponentials long each)
+    float m = v.x;
+#pragma unroll
+    for (int u = 0; u < U; ++u) m = fmaxf(m, x[u].x);
+    const float shift = stat_shift(m);
+    float s = __fmul_rn(v.y, __builtin_amdgcn_exp2f(v.x - shift));
+#pragma unroll
+    for (int u = 0; u < U; ++u) s = __fmaf_rn(x[u].y, __builtin_amdgcn_exp2f(x[u].x - shift), s);
+    v = make_float2(m, s);
+  }
+  sh[t] = v;
+  __syncthreads();
+  for (int d = 128; d >= RB; d >>= 1) {
+    if (t < d) sh[t] = stat2_join(sh[t], sh[t + d]);
+    __syncthreads();
+  }
+  auto lse_of = [&](int r) { return __fmul_rn(__fadd_rn(sh[r].x, log2f(sh[r].y)), 0.693147180559945309f); };
+  if (a.teacher == nullptr) {   // a row's loss by one lane
+    if (t < RB) {
+      float loss = 0.f;
+      bool counts = false;
+      if (row < a.M) {
+        const float lse = lse_of(t);
+        const int64_t y = a.ids[row];
+        counts = y >= 0;
+        if (counts) loss = y >= a.V ? NAN : __fmaf_rn(__fmul_rn(a.z_loss, lse), lse, __fsub_rn(lse, a.zt[row]));
+        a.lse[row] = lse;
+        a.loss[row] = loss;
+      }
+      ll[t] = loss;
+      cc[t] = counts ? 1.f : 0.f;
+    }
+  } else {
+    for (int r = wave; r < RB; r += 4) {
+      float loss = 0.f;
+      bool counts = false;
+      if (row0 + r < a.M) {
+        const float lse = lse_of(r);
+        loss = row_loss(a, row0 + r, lse, lane, &counts);
+        if (lane == 0) {
+          a.lse[row0 + r] = lse;
+          a.loss[row0 + r] = loss;
+        }
+      }
+      if (lane == 0) {
+        ll[r] = loss;
+        cc[r] = counts ? 1.f : 0.f;
+      }
+    }
+  }
+  if (a.mean == nullptr) return;
+  __syncthreads();
+  if (t == 0) {
+    double l = 0.0, c = 0.0;
+    for (int r = 0; r < RB; ++r) l += (double)ll[r], c += (double)cc[r];
+    sums[blockIdx.x] = make_double2(l, c);
+    __threadfence();
+    last = atomicAdd(done, 1) == (int)gridDim.x - 1;
+  }
+  __syncthreads();
+  if (!last) return;
+  __threadfence();
+  __shared__ double2 tot[256];
+  double l = 0.0, c = 0.0;
+  for (int i = t; i < (int)gridDim.x; i += 256) l += sums[i].x, c += sums[i].y;
+  tot[t] = make_double2(l, c);
+  __syncthreads();
+  for (int d = 128; d > 0; d >>= 1) {
+    if (t < d) tot[t].x += tot[t + d].x, tot[t].y += tot[t + d].y;
+    __syncthreads();
+  }
+  if (t == 0) *a.mean = (float)(tot[0].x / fmax(tot[0].y, 1.0));
+}
+
+// --------------------------------------------------------------------- backward
+// Which rows have a gradient (2), or count without one (1); distillation: the weights' shift and sum.
+__global__ __launch_bounds__(256) void vocab_flag_kernel(VocabArgs a, uint8_t* flag, float2* weight) {
+  const int lane = threadIdx.x & 63;
+  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (row >= a.M) return;
+  const RowTarget r = row_target(a, row, lane);
+  if (lane) return;
+  flag[row] = r.counts ? r.bad ? 1 : 2 : 0;
+  weight[row] = make_float2(r.top, r.total);
+}
+
+// The rows with a gradient in order: at[i] is the i-th, place[row] its number or -1, n[0] how many;
+// scale: what the stored gradient leaves out.  rows[i]: lse in units of log2, the factors of the
+// probabilities and of the targets, the label.
+struct RowCoef {
+  float lse2, cp, ct;
+  int label;           // cross-entropy; distillation: -1
+};
+__global__ __launch_bounds__(1024) void vocab_index_kernel(VocabArgs a, const uint8_t* flag, int* at, int* place, int* n,
+                                                           float* scale, RowCoef* rows) {
+  __shared__ int waves[16], counted[16], base;
+  const int t = threadIdx.x, lane = t & 63, w = t >> 6;
+  if (t == 0) base = 0;
+  int counts = 0;
+  for (int64_t r0 = 0; r0 < a.M; r0 += 1024) {
+    const int64_t row = r0 + t;
+    int f = 0;
+    if (row < a.M) {
+      if (a.teacher) {
+        f = flag[row];
+      } else {
+        const int64_t y = a.ids[row];
+        f = y < 0 ? 0 : y >= a.V ? 1 : 2;
+      }
+    }
+    counts += f != 0;
+    const uint64_t b = __ballot(f == 2);
+    if (lane == 0) waves[w] = __popcll(b);
+    __syncthreads();
+    int before = base, all = base;
+    for (int i = 0; i < 16; ++i) {
+      if (i < w) before += waves[i];
+      all += waves[i];
+    }
+    before += __popcll(b & ((1ull << lane) - 1));
+    if (row < a.M) place[row] = f == 2 ? before : -1;
+    if (f == 2) {
+      at[before] = (int)row;
+      const float ct = a.dloss ? __fmul_rn(a.dloss[row], a.T) : 1.f;
+      rows[before] = RowCoef{__fmul_rn(a.lse[row], 1.44269504088896341f), __fmul_rn(ct, __fmaf_rn(2.f * a.z_loss, a.lse[row], 1.f)), ct,
+                             a.teacher ? -1 : (int)a.ids[row]};
+    }
+    __syncthreads();
+    if (t == 0) base = all;
+    __syncthreads();
+  }
+  for (int d = 32; d > 0; d >>= 1) counts += __shfl_xor(counts, d);
+  if (lane == 0) counted[w] = counts;
+  __syncthreads();
+  if (t) return;
+  int c = 0;
+  for (int i = 0; i < 16; ++i) c += counted[i];
+  *n = base;
+  *scale = a.dloss ? 1.f : (float)((double)a.T / (double)max(c, 1));
+}
+
+// dst[i] = rows at[i] of src (at NULL: row i), n of them, widened to ldd with zeros; fp32 rows as three
+// planes, `plane` elements apart.
+template <int PL>
+__global__ __launch_bounds__(256) void vocab_gather_kernel(const void* srcp, int64_t lds, const int* at, const int* n,
+                                                           int64_t rows, int64_t K, uint16_t* dst, int64_t ldd, int64_t plane,
+                                                           int vec) {
+  const int64_t count = n ? *n : rows, each = ldd / 8;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < count * each; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / each, c = (i - r * each) * 8, from = (at ? at[r] : r) * lds + c;
+    uint16_t* d = dst + r * ldd + c;
+    if constexpr (PL == 1) {
+      const uint16_t* s = (const uint16_t*)srcp + from;
+      uint4 v;
+      if (vec) {
+        v = *reinterpret_cast<const uint4*>(s);
+      } else {
+        uint32_t w[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[e] = c + e < K ? s[e] : 0;
+        v = make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16);
+      }
+      *reinterpret_cast<uint4*>(d) = v;
+    } else {
+      const float* s = (const float*)srcp + from;
+      float x[8];
+      if (vec) {
+        const float4 a = ld4(s), b = ld4(s + 4);
+        x[0] = a.x, x[1] = a.y, x[2] = a.z, x[3] = a.w, x[4] = b.x, x[5] = b.y, x[6] = b.z, x[7] = b.w;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = c + e < K ? s[e] : 0.f;
+      }
+#pragma unroll
+      for (int p = 0; p < 3; ++p) {
+        uint32_t w[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w[e] = take_part(x[2 * e], x[2 * e + 1]);
+        *reinterpret_cast<uint4*>(d + p * plane) = make_uint4(w[0], w[1], w[2], w[3]);
+      }
+    }
+  }
+}
+
+// A = W, B = X again: the gradient of a row's logits (distillation: but for its entries), rounded to bf16 or
+// in three planes, stored [row][vocabulary] through the ring, in 16-byte pieces of whole rows.
+template <class T, int PL>
+struct GradEpi {
+  static constexpr int ROWS = ROWS_Q;
+  const RowCoef* rows;
+  uint16_t* dz;
+  int64_t ldz, plane;
+  float cap, rcap, c;
+  int v0;              // the piece's first vocabulary entry
+  template <class Acc>
+  __device__ __forceinline__ void operator()(const TilePlace& t, Acc& acc, char* const (&ring)[4], int lane, int wave, int wp,
+                                             int wq) const {
+    constexpr int IP = T::IP, IQ = T::IQ, SLOTS = IP * 4;   // 16-byte pieces of a row in LDS
+    const int h = lane >> 5, l32 = lane & 31;
+    const int np = t.np - wp * IP * 32, nq = t.nq - wq * IQ * 32;
+    char* lds = own_lds<T, (IP * IQ * 2048 > 4096 ? IP * IQ * 2048 : 4096)>(ring, wave);
+    auto fill = [&](auto Capped) {
+#pragma unroll
+      for (int j = 0; j < IQ; ++j) {
+        const int q = j * 32 + l32;
+        RowCoef rc{0.f, 0.f, 0.f, -1};
+        if (q < nq) rc = rows[t.q0 + wq * IQ * 32 + q];
+        const int label = rc.label < 0 ? -1 : rc.label - v0 - t.p0 - wp * IP * 32;   // among this wavefront's entries
+#pragma unroll
+        for (int i = 0; i < IP; ++i) {
+          const bool here = __any(label >= i * 32 && label < i * 32 + 32);
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int v = i * 32 + 8 * (r >> 2) + h * 4 + (r & 3);
+            const float z = vocab_cap(acc[i][j][r], decltype(Capped)::value ? cap : 0.f, rcap);
+            float d = __fmul_rn(__builtin_amdgcn_exp2f(__fmaf_rn(z, c, -rc.lse2)), rc.cp);
+            if (here) d = v == label ? __fsub_rn(d, rc.ct) : d;
+            if constexpr (decltype(Capped)::value) {
+              const float x = __fmul_rn(z, rcap);
+              d = __fmul_rn(d, __fmaf_rn(-x, x, 1.f));
+            }
+            acc[i][j][r] = v < np ? d : 0.f;
+          }
+        }
+      }
+    };
+    if (cap > 0.f) fill(std::true_type{});
+    else fill(std::false_type{});
+#pragma unroll
+    for (int p = 0; p < PL; ++p) {
+      if (p) wave_lds_sync();
+#pragma unroll
+      for (int j = 0; j < IQ; ++j)
+#pragma unroll
+        for (int i = 0; i < IP; ++i)
+#pragma unroll
+          for (int g = 0; g < 4; ++g) {
+            const int q = j * 32 + l32, slot = (i * 4 + g) ^ (q & (SLOTS - 1));
+            uint2 w;
+            if constexpr (PL == 1) {
+              w = make_uint2(pack2(acc[i][j][4 * g], acc[i][j][4 * g + 1]), pack2(acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]));
+            } else {
+              float x[4];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) x[e] = acc[i][j][4 * g + e];
+              w.x = take_part(x[0], x[1]);
+              w.y = take_part(x[2], x[3]);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) acc[i][j][4 * g + e] = x[e];
+            }
+            *reinterpret_cast<uint2*>(lds + q * (IP * 64) + slot * 16 + h * 8) = w;
+          }
+      wave_lds_sync();
+      uint16_t* out = dz + p * plane + ((int64_t)t.q0 + wq * IQ * 32) * ldz + t.p0 + wp * IP * 32;
+#pragma unroll
+      for (int u = 0; u < IQ * 32 * SLOTS / 64; ++u) {
+        const int x = u * 64 + lane, q = x / SLOTS, s = x % SLOTS;
+        const uint4 v = *reinterpret_cast<const uint4*>(lds + q * (IP * 64) + (s ^ (q & (SLOTS - 1))) * 16);
+        if (q < nq && s * 8 < np) *reinterpret_cast<uint4*>(out + q * ldz + s * 8) = v;
+      }
+    }
+  }
+};
+
+// Distillation, the entries' places in a piece: p less the weights of all the row's entries that name it, by
+// the first of them, from the logit that the forward kept.
+__device__ __forceinline__ float entry_grad(const VocabArgs& a, const RowCoef& rc, float z, float q) {
+  const float p = __builtin_amdgcn_exp2f(__fmaf_rn(z, 1.44269504088896341f / a.T, -rc.lse2));
+  float d = __fmaf_rn(rc.cp, p, -__fmul_rn(rc.ct, q));
+  if (a.cap > 0.f) {
+    const float x = __fmul_rn(z, a.rcap);
+    d = __fmul_rn(d, __fmaf_rn(-x, x, 1.f));
+  }
+  return d;
+}
+template <int PL>
+__global__ __launch_bounds__(256) void vocab_entry_kernel(VocabArgs a, const int* at, const int* n, const RowCoef* rows,
+                                                          const float2* weight, int64_t v0, int64_t nv, uint16_t* dz,
+                                                          int64_t ldz, int64_t plane) {
+  __shared__ int64_t ids[4][kTopMax];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  const int i = blockIdx.x * 4 + w;
+  if (i >= *n) return;
+  const int64_t row = at[i], first = row * a.k;
+  for (int j = lane; j < a.k; j += 64) ids[w][j] = a.ids[first + j];
+  wave_lds_sync();
+  const RowTarget r{weight[row].x, weight[row].y, true, false};
+  const RowCoef rc = rows[i];
+  for (int j = lane; j < a.k; j += 64) {
+    const int64_t id = ids[w][j];
+    if (id < v0 || id >= v0 + nv) continue;
+    float q = 0.f;
+    bool lead = true;
+    for (int e = 0; e < a.k; ++e) {
+      if (ids[w][e] != id) continue;
+      lead &= e >= j;
+      q = __fadd_rn(q, r.weight(teacher_logit(a, first + e)));
+    }
+    if (!lead) continue;
+    uint16_t* d = dz + (int64_t)i * ldz + (id - v0);
+    float x = entry_grad(a, rc, a.zt[first + j], q), y = 0.f;
+#pragma unroll
+    for (int p = 0; p < PL; ++p) d[p * plane] = (uint16_t)take_part(x, y);
+  }
+}
+
+// Sums of a part of the reduction: stored, or added to those of the pieces before.
+template <class T, int ROWS_DIM>
+struct PartEpi {
+  static constexpr int ROWS = ROWS_DIM;
+  float* out;          // [S][rows][ld]
+  int64_t rows, ld;
+  int add;
+  template <class Acc>
+  __device__ __forceinline__ void operator()(const TilePlace& t, Acc& acc, char* const (&)[4], int lane, int, int wp, int wq) const {
+    const int np = t.np - wp * T::IP * 32, nq = t.nq - wq * T::IQ * 32, h4 = (lane >> 5) * 4, l32 = lane & 31;
+    float* o = out + ((int64_t)t.split * rows + t.p0 + wp * T::IP * 32) * ld + t.q0 + wq * T::IQ * 32;
+#pragma unroll
+    for (int i = 0; i < T::IP; ++i)
+#pragma unroll
+      for (int j = 0; j < T::IQ; ++j) {
+        const bool in = j * 32 + l32 < nq;
+        float v[16];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int p = i * 32 + 8 * (r >> 2) + h4 + (r & 3);
+          v[r] = add && in && p < np ? o[p * ld + j * 32 + l32] : 0.f;
+        }
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int p = i * 32 + 8 * (r >> 2) + h4 + (r & 3);
+          if (in && p < np) o[p * ld + j * 32 + l32] = __fadd_rn(v[r], acc[i][j][r]);
+        }
+      }
+  }
+};
+
+// dW of a piece's rows: a gradient stored (or added), or the update.
+struct HeadGrad {
+  const float* scale;
+  void* dw;            // NULL: update
+  int gbf, accumulate;
+  int64_t K;
+  of_param W;
+  const float* gW;
+  OptK opt;
+  __device__ __forceinline__ void store(int64_t i, float g) const {
+    if (gbf) {
+      uint16_t* d = (uint16_t*)dw + i;
+      *d = f32_to_bf16(accumulate ? __fadd_rn(__uint_as_float((uint32_t)*d << 16), g) : g);
+    } else {
+      float* d = (float*)dw + i;
+      *d = accumulate ? __fadd_rn(*d, g) : g;
+    }
+  }
+};
+
+template <class T, bool UPDATE>
+struct HeadEpi {
+  static constexpr int ROWS = ROWS_R;
+  HeadGrad g;
+  template <class Acc>
+  __device__ __forceinline__ void operator()(const TilePlace& t, Acc& acc, char* const (&)[4], int lane, int, int wp, int wq) const {
+    const int np = t.np - wp * T::IP * 32, nq = (int)min((int64_t)t.nq, g.K - t.q0) - wq * T::IQ * 32;
+    const int h4 = (lane >> 5) * 4, l32 = lane & 31;
+    const int64_t org = (int64_t)(t.p0 + wp * T::IP * 32) * g.K + t.q0 + wq * T::IQ * 32;
+    const float scale = *g.scale;
+    OptK o = g.opt;
+    if constexpr (UPDATE) opt_prepare(o);
+    // bf16: lanes 2l and 2l + 1 trade a value so that each stores two columns of a row
+    const bool pair = !UPDATE && g.gbf && !g.accumulate && g.K % 2 == 0 && ((uintptr_t)g.dw & 3u) == 0;
+    auto at = [&](int r) { return 8 * (r >> 2) + h4 + (r & 3); };
+    each(std::make_integer_sequence<int, T::IP * T::IQ>{}, [&](auto B_) __attribute__((always_inline)) {
+      constexpr int i = decltype(B_)::value / T::IQ, j = decltype(B_)::value % T::IQ;
+      const int q = j * 32 + l32, n = np - i * 32;
+      const int64_t o0 = org + (int64_t)i * 32 * g.K + q;
+      if constexpr (UPDATE) {
+        constexpr int N = 8;   // elements at a time: their states' loads are in flight together
+        each(std::make_integer_sequence<int, 16 / N>{}, [&](auto R_) __attribute__((always_inline)) {
+          constexpr int r0 = decltype(R_)::value * N;
+          OptState1 st[N];
+          float e[N];
+#pragma unroll
+          for (int r = 0; r < N; ++r) {
+            if (q >= nq || at(r0 + r) >= n) continue;
+            st[r] = opt_load1(o, g.W, o0 + at(r0 + r) * g.K);
+            e[r] = g.gW ? g.gW[o0 + at(r0 + r) * g.K] : 0.f;
+          }
+#pragma unroll
+          for (int r = 0; r < N; ++r) {
+            if (q >= nq || at(r0 + r) >= n) continue;
+            const float d = __fmul_rn(acc[i][j][r0 + r], scale);
+            opt_apply1(o, g.W, st[r], g.gW ? __fadd_rn(e[r], d) : d, o0 + at(r0 + r) * g.K);
+          }
+        });
+      } else if (pair) {
+        const bool odd = lane & 1;
+#pragma unroll
+        for (int r = 0; r < 16; r += 2) {
+          const float x = __fmul_rn(acc[i][j][r], scale), y = __fmul_rn(acc[i][j][r + 1], scale);
+          const float mine = odd ? y : x, give = odd ? x : y;
+          const float got = __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(give), 0xb1, 0xf, 0xf, true));   // lane ^ 1
+          const int p = at(r) + (odd ? 1 : 0);
+          if (q < nq && p < n)
+            *reinterpret_cast<uint32_t*>((uint16_t*)g.dw + (o0 - (odd ? 1 : 0) + p * g.K)) = odd ? pack2(got, mine) : pack2(mine, got);
+        }
+      } else {
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+          if (q < nq && at(r) < n) g.store(o0 + at(r) * g.K, __fmul_rn(acc[i][j][r], scale));
+      }
+    });
+  }
+};
+
+// The same from parts [S][rows][ld], summed in order.
+__global__ __launch_bounds__(256) void vocab_head_kernel(HeadGrad g, const float* part, int S, int64_t rows, int64_t ld) {
+  const float scale = *g.scale;
+  OptK o = g.opt;
+  if (!g.dw) opt_prepare(o);
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * g.K; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / g.K, c = i - r * g.K;
+    const float* p = part + r * ld + c;
+    float v = p[0];
+    for (int s = 1; s < S; ++s) v = __fadd_rn(v, p[s * rows * ld]);
+    v = __fmul_rn(v, scale);
+    if (g.dw) g.store(i, v);
+    else update1(o, g.W, g.gW ? __fadd_rn(g.gW[i], v) : v, i);
+  }
+}
+
+// dX from its parts [S][M][ld]: their sum in order, scaled, at its row; zeros where a row has none.
+template <int V>
+__global__ __launch_bounds__(256) void vocab_dx_kernel(const float* part, int S, int64_t M, int64_t ld, const int* place,
+                                                       const float* scale, int64_t K, void* dx, int64_t ldx, int gbf) {
+  const float f = *scale;
+  const int64_t each = K / V;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < M * each; i += (int64_t)gridDim.x * 256) {
+    const int64_t row = i / each, c = (i - row * each) * V;
+    const int r = place[row];
+    float v[V];
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] = 0.f;
+    if (r >= 0) {
+      for (int s = 0; s < S; ++s) {
+        const float* p = part + ((int64_t)s * M + r) * ld + c;
+        if constexpr (V == 4) {
+          const float4 x = ld4(p);
+          v[0] = __fadd_rn(v[0], x.x), v[1] = __fadd_rn(v[1], x.y), v[2] = __fadd_rn(v[2], x.z), v[3] = __fadd_rn(v[3], x.w);
+        } else {
+          v[0] = __fadd_rn(v[0], *p);
+        }
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] = __fmul_rn(v[e], f);
+    if constexpr (V == 4) {
+      if (gbf) *reinterpret_cast<uint2*>((uint16_t*)dx + row * ldx + c) = make_uint2(pack2(v[0], v[1]), pack2(v[2], v[3]));
+      else st4((float*)dx + row * ldx + c, make_float4(v[0], v[1], v[2], v[3]));
+    } else {
+      if (gbf) ((uint16_t*)dx)[row * ldx + c] = f32_to_bf16(v[0]);
+      else ((float*)dx)[row * ldx + c] = v[0];
+    }
+  }
+}
+
+// ------------------------------------------------------------------------ plans
+enum Shape { BIG = 0, MID = 1, FEW = 2 };
+struct Choice {
+  Shape shape;
+  int S;               // parts of the reduction
+};
+
+// Time of a product of P x Q tiles over R: rounds of workgroups, each its stages of 32 elements and an
+// epilogue; parts are written and read again.  us, fitted to products of 512 to 32768 rows and columns.
+Choice choose(int64_t P, int64_t Q, int64_t R, int planes, bool split) {
+  Choice best{MID, 1};
+  double least = 1e300;
+  for (const Shape s : {BIG, MID}) {
+    const int64_t b = s == BIG ? 256 : 128, tiles = per(P, b) * per(Q, b);
+    for (int S = 1; S <= (split ? 64 : 1); S += S < 4 ? 1 : S / 2) {
+      if (S > 1 && R / S < 128) break;
+      const int64_t wg = tiles * S;
+      const double stages = (double)up(per(per(R, 32), S) * (planes == 3 ? 6 : 1), 4);
+      const double one = s == BIG ? stages * 0.85 + 8 : stages * (wg > 256 ? 0.58 : 0.36) + 4;
+      const double time = per(wg, s == BIG ? 256 : 512) * one + (S > 1 ? 2 + (double)P * Q * S * 8 / 4e6 : 0);
+      if (time < least) least = time, best = Choice{s, S};
+    }
+  }
+  return best;
+}
+
+// Parts of dX's reduction for few rows: enough workgroups for the chip, at least 256 entries each.
+int few_parts(int64_t K, int64_t V) {
+  return (int)std::max<int64_t>(1, std::min<int64_t>({64, per(512, per(K, 128)), V / 256}));
+}
+
+struct TilesPlan {
+  int PL;                           // planes of an operand
+  int64_t Kp, piece, copied, ldz;   // widened rows; vocabulary entries of a piece, and of one whose W is copied
+  Choice logits, dx, dw;
+  int BP, BQ;                       // the logits' tiles
+  int64_t vtiles, rtiles;
+  int64_t px, pw, pz;               // elements of a plane of X, W and the gradient
+  size_t x, w, off, list, part, sums, done;
+  size_t flag, weight, at, place, n, scale, rows, dz, pdx, pdw, total;
+};
+
+TilesPlan tiles_plan(const VocabArgs& a, bool bwd) {
+  TilesPlan p{};
+  p.PL = a.bf16 ? 1 : 3;
+  p.Kp = up(a.K, 8);
+  size_t here = 0;
+  auto take = [&](int64_t bytes) {
+    const size_t at = here;
+    here += (size_t)up(bytes, 256);
+    return at;
+  };
+  p.logits = a.M <= kFew && a.bf16 ? Choice{FEW, 1} : choose(a.V, a.M, a.K, p.PL, false);
+  p.BP = p.logits.shape == BIG ? 256 : 128;
+  p.BQ = p.logits.shape == BIG ? 256 : p.logits.shape == MID ? 128 : 32;
+  p.vtiles = per(a.V, p.BP), p.rtiles = per(a.M, p.BQ);
+  // fp32 W, and W whose rows are not whole 16-byte pieces, is copied: up to 512 MB at a time, in copies of
+  // one size
+  const int64_t room = std::max<int64_t>(256, (1LL << 28) / (p.Kp * p.PL) / 256 * 256);
+  p.copied = std::min(up(per(a.V, per(a.V, room)), 256), up(a.V, 8));
+  p.px = a.M * p.Kp;
+  p.x = take(p.px * p.PL * 2);
+  if (!bwd) {
+    p.pw = p.copied * p.Kp;
+    p.w = take(p.pw * p.PL * 2);
+    p.off = take(p.rtiles * (p.vtiles + 1) * 4);
+    p.list = take(p.rtiles * p.BQ * a.k * 4);
+    p.part = take(p.vtiles * a.M * 8);
+    p.sums = take(per(a.M, a.M <= kJoinFew ? 1 : kJoinRows) * 16);
+    p.done = take(4);
+    p.total = here;
+    return p;
+  }
+  // a piece's gradient takes up to 512 MB; pieces of one size
+  const int64_t most = std::max<int64_t>(256, (1LL << 28) / (a.M * p.PL) / 256 * 256);
+  p.piece = std::min(up(per(a.V, per(a.V, most)), 256), up(a.V, 8));
+  p.copied = std::min(p.copied, p.piece);
+  p.pw = p.copied * p.Kp;
+  p.w = take(p.pw * p.PL * 2);
+  p.ldz = p.piece;
+  p.pz = a.M * p.ldz;
+  p.dx = a.M <= kFew && a.bf16 ? Choice{FEW, few_parts(a.K, p.piece)} : choose(a.M, a.K, p.piece, p.PL, true);
+  p.dw = choose(p.piece, a.K, a.M, p.PL, true);
+  p.flag = take(a.M);
+  p.weight = take(a.M * 8);
+  p.at = take(a.M * 4);
+  p.place = take(a.M * 4);
+  p.n = take(4);
+  p.scale = take(4);
+  p.rows = take(a.M * (int64_t)sizeof(RowCoef));
+  p.dz = take(p.pz * p.PL * 2);
+  p.pdx = take((int64_t)p.dx.S * a.M * p.Kp * 4);
+  p.pdw = take(p.dw.S > 1 ? (int64_t)p.dw.S * p.piece * p.Kp * 4 : 0);
+  p.total = here;
+  return p;
+}
+
+// An operand: its first plane, row stride and planes' distance.
+struct Operand {
+  const uint16_t* p;
+  int64_t ld, plane;
+};
+
+template <class T, int PL, bool A, bool B, class Epi>
+hipError_t product(const Operand& a, const Operand& b, int64_t P, int64_t Q, int64_t R, const int* rows, int S, const Epi& e,
+                   hipStream_t s) {
+  const TileProblem pr{a.p, b.p, a.ld, b.ld, (int)P, (int)Q, (int)R, rows, (int)per(P, T::BP), (int)per(Q, T::BQ), S,
+                       a.plane, b.plane};
+  hipLaunchKernelGGL((tile_kernel<T, PL, A, B, Epi>), dim3((unsigned)(pr.gp * pr.gq * S)), dim3(T::NT), 0, s, pr, e);
+  return hipGetLastError();
+}
+
+#define TRY(x)                                    \
+  do {                                            \
+    const hipError_t e_ = (x);                    \
+    if (e_ != hipSuccess) return e_;              \
+  } while (0)
+
+int grid_of(int64_t n) { return (int)std::min<int64_t>(8192, std::max<int64_t>(1, per(n, 256))); }
+
+// A call's plan, workspace and stream.
+template <int PL>
+struct Tiles {
+  const VocabArgs& a;
+  TilesPlan p;
+  char* ws;
+  hipStream_t s;
+
+  template <class U>
+  U* at(size_t off) const { return (U*)(ws + off); }
+
+  hipError_t gather(const void* src, int64_t lds, const int* rows_at, const int* n, int64_t rows, uint16_t* dst, int64_t plane) const {
+    const int vec = PL == 1 ? !odd_rows(src, lds, a.K) : aligned16(src) && lds % 4 == 0 && a.K % 8 == 0;
+    hipLaunchKernelGGL(vocab_gather_kernel<PL>, dim3(grid_of(rows * p.Kp / 8)), dim3(256), 0, s, src, lds, rows_at, n, rows, a.K,
+                       dst, p.Kp, plane, vec);
+    return hipGetLastError();
+  }
+  bool copies_w() const { return PL == 3 || odd_rows(a.W.w_bf16, a.K, a.K); }
+  hipError_t head(int64_t v0, int64_t n, Operand* w) const {   // W's rows [v0, v0 + n)
+    if (!copies_w()) {
+      *w = Operand{a.W.w_bf16 + v0 * a.K, a.K, 0};
+      return hipSuccess;
+    }
+    *w = Operand{at<uint16_t>(p.w), p.Kp, p.pw};
+    const void* src = PL == 1 ? (const void*)(a.W.w_bf16 + v0 * a.K) : (const void*)(a.W.w + v0 * a.K);
+    return gather(src, a.K, nullptr, nullptr, n, at<uint16_t>(p.w), p.pw);
+  }
+
+  template <class T>
+  hipError_t sort_entries() const {
+    const Entries en{at<int>(p.off), at<uint32_t>(p.list), (int)p.vtiles};
+    hipLaunchKernelGGL((vocab_sort_kernel<T::BP, T::BQ>), dim3((unsigned)p.rtiles), dim3(1024), (size_t)p.vtiles * 4, s, a, en,
+                       at<int>(p.done));
+    return hipGetLastError();
+  }
+  template <class T>
+  hipError_t stats(const Operand& x, const Operand& w, int64_t v0, int64_t n) const {
+    const Entries en{at<int>(p.off), at<uint32_t>(p.list), (int)p.vtiles};
+    const StatEpi<T> e{at<float2>(p.part), a.zt, en, (int)(v0 / T::BP), a.M, a.k, a.cap, a.rcap, 1.44269504088896341f / a.T};
+    return product<T, PL, true, true>(w, x, n, a.M, a.K, nullptr, 1, e, s);
+  }
+  template <class T>
+  hipError_t grads(const Operand& w, int64_t v0, int64_t n) const {
+    const GradEpi<T, PL> e{at<RowCoef>(p.rows), at<uint16_t>(p.dz), p.ldz, p.pz, a.cap, a.rcap, 1.44269504088896341f / a.T, (int)v0};
+    return product<T, PL, true, true>(w, Operand{at<uint16_t>(p.x), p.Kp, p.px}, n, a.M, a.K, at<int>(p.n), 1, e, s);
+  }
+  template <class T>
+  hipError_t data_grad(const Operand& w, int64_t n, bool first) const {
+    const PartEpi<T, ROWS_P> e{at<float>(p.pdx), a.M, p.Kp, first ? 0 : 1};
+    return product<T, PL, true, false>(Operand{at<uint16_t>(p.dz), p.ldz, p.pz}, w, a.M, p.Kp, n, at<int>(p.n), p.dx.S, e, s);
+  }
+  template <class T>
+  hipError_t head_grad(const HeadGrad& g, int64_t n) const {
+    const Operand dz{at<uint16_t>(p.dz), p.ldz, p.pz}, x{at<uint16_t>(p.x), p.Kp, p.px};
+    const int* rows = at<int>(p.n);
+    if (p.dw.S > 1) {
+      const PartEpi<T, ROWS_R> e{at<float>(p.pdw), n, p.Kp, 0};
+      TRY((product<T, PL, false, false>(dz, x, n, p.Kp, a.M, rows, p.dw.S, e, s)));
+      hipLaunchKernelGGL(vocab_head_kernel, dim3(grid_of(n * a.K)), dim3(256), 0, s, g, at<const float>(p.pdw), p.dw.S, n, p.Kp);
+      return hipGetLastError();
+    }
+    if (g.dw) return product<T, PL, false, false>(dz, x, n, p.Kp, a.M, rows, 1, HeadEpi<T, false>{g}, s);
+    return product<T, PL, false, false>(dz, x, n, p.Kp, a.M, rows, 1, HeadEpi<T, true>{g}, s);
+  }
+
+  hipError_t fwd() const {
+    Operand x{(const uint16_t*)a.x, a.ldx, 0};
+    if (PL == 3 || odd_rows(a.x, a.ldx, a.K)) {
+      TRY(gather(a.x, a.ldx, nullptr, nullptr, a.M, at<uint16_t>(p.x), p.px));
+      x = Operand{at<uint16_t>(p.x), p.Kp, p.px};
+    }
+    switch (p.logits.shape) {
+      case BIG: TRY(sort_entries<Big>()); break;
+      case MID: TRY(sort_entries<Mid>()); break;
+      default: TRY(sort_entries<FewQ>()); break;
+    }
+    const int64_t piece = copies_w() ? p.copied : a.V;
+    for (int64_t v0 = 0; v0 < a.V; v0 += piece) {
+      const int64_t n = std::min(piece, a.V - v0);
+      Operand w;
+      TRY(head(v0, n, &w));
+      switch (p.logits.shape) {
+        case BIG: TRY(stats<Big>(x, w, v0, n)); break;
+        case MID: TRY(stats<Mid>(x, w, v0, n)); break;
+        default:
+          if constexpr (PL == 1) TRY(stats<FewQ>(x, w, v0, n));
+      }
+    }
+    if (a.M <= kJoinFew)
+      hipLaunchKernelGGL(vocab_join_kernel<1>, dim3((unsigned)a.M), dim3(256), 0, s, a, at<const float2>(p.part), (int)p.vtiles,
+                         at<double2>(p.sums), at<int>(p.done));
+    else
+      hipLaunchKernelGGL(vocab_join_kernel<kJoinRows>, dim3((unsigned)per(a.M, kJoinRows)), dim3(256), 0, s, a,
+                         at<const float2>(p.part), (int)p.vtiles, at<double2>(p.sums), at<int>(p.done));
+    return hipGetLastError();
+  }
+
+  hipError_t bwd() const {
+    int *rows_at = at<int>(p.at), *place = at<int>(p.place), *n = at<int>(p.n);
+    float* scale = at<float>(p.scale);
+    if (a.teacher) {
+      hipLaunchKernelGGL(vocab_flag_kernel, dim3((unsigned)per(a.M, 4)), dim3(256), 0, s, a, at<uint8_t>(p.flag), at<float2>(p.weight));
+      TRY(hipGetLastError());
+    }
+    hipLaunchKernelGGL(vocab_index_kernel, dim3(1), dim3(1024), 0, s, a, at<const uint8_t>(p.flag), rows_at, place, n, scale,
+                       at<RowCoef>(p.rows));
+    TRY(hipGetLastError());
+    TRY(gather(a.x, a.ldx, rows_at, n, a.M, at<uint16_t>(p.x), p.px));
+    const int64_t piece = copies_w() ? p.copied : p.piece;
+    for (int64_t v0 = 0; v0 < a.V; v0 += piece) {
+      const int64_t nv = std::min(piece, a.V - v0);
+      Operand w;
+      TRY(head(v0, nv, &w));
+      switch (p.logits.shape) {
+        case BIG: TRY(grads<Big>(w, v0, nv)); break;
+        case MID: TRY(grads<Mid>(w, v0, nv)); break;
+        default:
+          if constexpr (PL == 1) TRY(grads<FewQ>(w, v0, nv));
+      }
+      if (a.teacher) {
+        hipLaunchKernelGGL(vocab_entry_kernel<PL>, dim3((unsigned)per(a.M, 4)), dim3(256), 0, s, a, rows_at, n, at<RowCoef>(p.rows),
+                           at<const float2>(p.weight), v0, nv, at<uint16_t>(p.dz), p.ldz, p.pz);
+        TRY(hipGetLastError());
+      }
+      if (a.dx) {
+        switch (p.dx.shape) {
+          case BIG: TRY(data_grad<Big>(w, nv, v0 == 0)); break;
+          case MID: TRY(data_grad<Mid>(w, nv, v0 == 0)); break;
+          default:
+            if constexpr (PL == 1) TRY(data_grad<FewP>(w, nv, v0 == 0));
+        }
+      }
+      if (!a.fused && !a.dw) continue;
+      HeadGrad g{};
+      g.scale = scale;
+      g.K = a.K;
+      g.gbf = a.gbf;
+      g.accumulate = a.accumulate;
+      const int64_t o = v0 * a.K;
+      if (a.fused) {
+        g.W = a.W;
+        g.W.w += o;
+        if (g.W.m) g.W.m += o;
+        if (g.W.v) g.W.v += o;
+        if (g.W.w_bf16) g.W.w_bf16 += o;
+        g.gW = a.gW ? a.gW + o : nullptr;
+        g.opt = a.opt;
+      } else {
+        g.dw = a.gbf ? (void*)((uint16_t*)a.dw + o) : (void*)((float*)a.dw + o);
+      }
+      TRY(p.dw.shape == BIG ? head_grad<Big>(g, nv) : head_grad<Mid>(g, nv));
+    }
+    if (!a.dx) return hipSuccess;
+    const bool vec = a.K % 4 == 0 && a.ldx % 4 == 0 && ((uintptr_t)a.dx) % (a.gbf ? 8 : 16) == 0;
+    const float* part = at<const float>(p.pdx);
+    if (vec)
+      hipLaunchKernelGGL(vocab_dx_kernel<4>, dim3(grid_of(a.M * a.K / 4)), dim3(256), 0, s, part, p.dx.S, a.M, p.Kp, place, scale,
+                         a.K, a.dx, a.ldx, a.gbf ? 1 : 0);
+    else
+      hipLaunchKernelGGL(vocab_dx_kernel<1>, dim3(grid_of(a.M * a.K)), dim3(256), 0, s, part, p.dx.S, a.M, p.Kp, place, scale,
+                         a.K, a.dx, a.ldx, a.gbf ? 1 : 0);
+    return hipGetLastError();
+  }
+};
+
+}  // namespace
+
+bool vocab_tiles_ok(const VocabArgs& a) { return a.bf16 || a.M > 2 * kFew; }
+
+size_t vocab_tiles_ws_bytes(const VocabArgs& a, bool bwd) { return tiles_plan(a, bwd).total; }
+
+hipError_t vocab_tiles_fwd(const VocabArgs& a, void* ws, hipStream_t s) {
+  if (a.bf16) return Tiles<1>{a, tiles_plan(a, false), (char*)ws, s}.fwd();
+  return Tiles<3>{a, tiles_plan(a, false), (char*)ws, s}.fwd();
+}
+
+hipError_t vocab_tiles_bwd(const VocabArgs& a, void* ws, hipStream_t s) {
+  if (a.bf16) return Tiles<1>{a, tiles_plan(a, true), (char*)ws, s}.bwd();
+  return Tiles<3>{a, tiles_plan(a, true), (char*)ws, s}.bwd();
+}
+
+}  // namespace opfuse

@@ -84,11 +84,11 @@ class Call:
           self.dev_dloss.data_ptr() if self.dev_dloss is not None else None, gW.data_ptr() if gW is not None else None, opt,
           self.dx.data_ptr() if dx else None, *self._ws(L.OF_VOCAB_BWD), self._stream())
 
-    def reference(self, **kw):
+    def reference(self, device="cpu", **kw):
         a = dict(x=self.x, w=self.w, ids=self.ids, teacher=self.teacher, T=self.T, cap=self.cap, z_loss=self.z_loss,
                  dloss=self.dloss, u=TYPES[self.dtype][2])
         a.update(kw)
-        return Reference(**a)
+        return Reference(**{k: v.to(device) if torch.is_tensor(v) else v for k, v in a.items()})
 
     def check_fwd(self, r=None, mean=True):
         r = r or self.reference()
@@ -140,6 +140,21 @@ def test_distill(gpu, M, V, K, k, T, dtype):
     c.bwd()
     c.check_fwd()
     c.check_bwd()
+    c.untouched()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,V,K,kw", [(1024, 16384, 1024, {}), (1021, 16291, 712, dict(given=True, gap=3)),
+                                      (1900, 16384, 520, dict(k=40, T=2.0, cap=20.0)), (2000, 700, 300, dict(z_loss=1e-2)),
+                                      (70, 40000, 256, dict(k=3)), (16, 70001, 128, {})])
+def test_large(gpu, M, V, K, kw, dtype):
+    """Sizes that take the 256x256 tiles, parts of the reductions and more than one piece."""
+    c = Call(gpu, M, V, K, dtype, **kw)
+    c.fwd()
+    c.bwd()
+    r = c.reference(device=gpu)
+    c.check_fwd(r)
+    c.check_bwd(r)
     c.untouched()
 
 

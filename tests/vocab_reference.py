@@ -27,7 +27,7 @@ def target(ids, teacher, T, V):
 
 class Reference:
     def __init__(self, x, w, ids, teacher=None, T=1.0, cap=0.0, z_loss=0.0, dloss=None, u=2.0 ** -24):
-        """x [M, K], w [V, K], ids [M, k], all on the CPU; ids in [-1, V)."""
+        """x [M, K], w [V, K], ids [M, k], all on one device; ids in [-1, V)."""
         x, w = x.double(), w.double()
         M, K = x.shape
         V = w.shape[0]
@@ -42,7 +42,7 @@ class Reference:
         loss = T * T * (q * (log_q - zt / T + lse[:, None])).sum(1) + z_loss * lse * lse
         loss = torch.where(counts, loss, 0.0)
         n = max(1, int(counts.sum()))
-        g = torch.where(counts, dloss.double() if dloss is not None else torch.full((M,), 1.0 / n).double(), 0.0)
+        g = torch.where(counts, dloss.double() if dloss is not None else torch.full((M,), 1.0 / n, device=x.device).double(), 0.0)
         self.mean = (loss.sum() / n).item()
         self.dx, self.dw = torch.autograd.grad((loss * g).sum(), (x, w))
         self.loss, self.lse, self.zt, self.counts, self.g = loss.detach(), lse.detach(), zt.detach(), counts, g
@@ -80,6 +80,7 @@ class Reference:
 
 def near(name, got, want, bound, half=0.0):
     """|got - want| <= bound and the output's own rounding (half a step: 2^-8 for bf16)."""
-    got = got.detach().cpu().double()
+    got = got.detach().to(want.device).double()
+    bound = bound.to(want.device)
     over = (got - want).abs() - 1.01 * bound - (half + E) * want.abs() - 1e-30
     assert torch.isfinite(got).all() and (over <= 0).all(), (name, float(over.max()), int((over > 0).sum()), got.numel())
