@@ -32,6 +32,8 @@ using FewP = TileShape<1, 1, 1, 4, 64, 2>;   // 32 x 128
 
 constexpr int kFew = 32;                     // rows up to which a product's tiles are 32 wide
 
+typedef uint32_t au32x4 __attribute__((ext_vector_type(4)));
+
 int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 int64_t per(int64_t n, int64_t each) { return (n + each - 1) / each; }
 bool odd_rows(const void* p, int64_t ld, int64_t K) { return !aligned16(p) || ld % 8 != 0 || K % 8 != 0; }
@@ -133,17 +135,22 @@ __global__ __launch_bounds__(1024) void vocab_sort_kernel(VocabArgs a, Entries e
   }
 }
 
-// Two statistics in units of log2.
-__device__ __forceinline__ float2 stat2_join(float2 x, float2 y) {
+constexpr float kLog2E = 1.44269504088896341f;
+
+// Two statistics: a maximum of the (capped) logits, and the sum of exp((z - maximum) / T).  c: log2(e) / T.
+// Differences are taken before they are scaled: a maximum in units of log2 would be rounded by as much
+// as all the rest of lse.
+__device__ __forceinline__ float2 stat2_join(float2 x, float2 y, float c) {
   const float m = fmaxf(x.x, y.x), s = stat_shift(m);
-  return make_float2(m, __fadd_rn(__fmul_rn(x.y, __builtin_amdgcn_exp2f(x.x - s)), __fmul_rn(y.y, __builtin_amdgcn_exp2f(y.x - s))));
+  return make_float2(m, __fmaf_rn(x.y, __builtin_amdgcn_exp2f(__fmul_rn(x.x - s, c)),
+                                  __fmul_rn(y.y, __builtin_amdgcn_exp2f(__fmul_rn(y.x - s, c)))));
 }
 
 // A = W, B = X: a lane's accumulators are one row's logits, for statistics within the lane.
 template <class T>
 struct StatEpi {
   static constexpr int ROWS = ROWS_NONE;
-  float2* part;        // [vtiles][M]: maximum (in units of log2) and sum
+  float2* part;        // [vtiles][M]
   float* zt;
   Entries en;
   int tile0;           // the piece's first vocabulary tile
@@ -218,14 +225,13 @@ struct StatEpi {
 #pragma unroll
         for (int r = 0; r < 16; ++r) m[j] = fmaxf(m[j], acc[i][j][r]);
       m[j] = fmaxf(m[j], __shfl_xor(m[j], 32));
-      const float shift = __fmul_rn(stat_shift(m[j]), c);
+      const float shift = stat_shift(m[j]);
       s[j] = 0.f;
 #pragma unroll
       for (int i = 0; i < IP; ++i)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[j] = __fadd_rn(s[j], __builtin_amdgcn_exp2f(__fmaf_rn(acc[i][j][r], c, -shift)));
+        for (int r = 0; r < 16; ++r) s[j] = __fadd_rn(s[j], __builtin_amdgcn_exp2f(__fmul_rn(__fsub_rn(acc[i][j][r], shift), c)));
       s[j] = __fadd_rn(s[j], __shfl_xor(s[j], 32));
-      m[j] = m[j] == -INFINITY ? m[j] : shift;
     }
     // the wavefronts of a row's vocabulary entries join in LDS
     float2* sh = (float2*)ring[0];   // [WP][BQ]
@@ -239,7 +245,7 @@ struct StatEpi {
     if (q < T::BQ && q < t.nq) {
       float2 v = sh[q];
 #pragma unroll
-      for (int w = 1; w < T::WP; ++w) v = stat2_join(v, sh[w * T::BQ + q]);
+      for (int w = 1; w < T::WP; ++w) v = stat2_join(v, sh[w * T::BQ + q], c);
       part[(int64_t)tile * M + t.q0 + q] = v;
     }
   }
@@ -255,6 +261,7 @@ __global__ __launch_bounds__(256) void vocab_join_kernel(VocabArgs a, const floa
   __shared__ int last;
   const int t = threadIdx.x, lane = t & 63, wave = t >> 6;
   const int64_t row0 = (int64_t)blockIdx.x * RB, row = row0 + t % RB;
+  const float k = kLog2E / a.T;
   float2 v = make_float2(-INFINITY, 0.f);
   constexpr int U = 8, STEP = 256 / RB;
   for (int p = t / RB; p < parts; p += STEP * U) {
@@ -267,18 +274,18 @@ __global__ __launch_bounds__(256) void vocab_join_kernel(VocabArgs a, const floa
 #pragma unroll
     for (int u = 0; u < U; ++u) m = fmaxf(m, x[u].x);
     const float shift = stat_shift(m);
-    float s = __fmul_rn(v.y, __builtin_amdgcn_exp2f(v.x - shift));
+    float s = __fmul_rn(v.y, __builtin_amdgcn_exp2f(__fmul_rn(v.x - shift, k)));
 #pragma unroll
-    for (int u = 0; u < U; ++u) s = __fmaf_rn(x[u].y, __builtin_amdgcn_exp2f(x[u].x - shift), s);
+    for (int u = 0; u < U; ++u) s = __fmaf_rn(x[u].y, __builtin_amdgcn_exp2f(__fmul_rn(x[u].x - shift, k)), s);
     v = make_float2(m, s);
   }
   sh[t] = v;
   __syncthreads();
   for (int d = 128; d >= RB; d >>= 1) {
-    if (t < d) sh[t] = stat2_join(sh[t], sh[t + d]);
+    if (t < d) sh[t] = stat2_join(sh[t], sh[t + d], k);
     __syncthreads();
   }
-  auto lse_of = [&](int r) { return __fmul_rn(__fadd_rn(sh[r].x, log2f(sh[r].y)), 0.693147180559945309f); };
+  auto lse_of = [&](int r) { return __fadd_rn(__fdiv_rn(sh[r].x, a.T), logf(sh[r].y)); };
   if (a.teacher == nullptr) {   // a row's loss by one lane
     if (t < RB) {
       float loss = 0.f;
@@ -349,58 +356,74 @@ __global__ __launch_bounds__(256) void vocab_flag_kernel(VocabArgs a, uint8_t* f
 }
 
 // The rows with a gradient in order: at[i] is the i-th, place[row] its number or -1, n[0] how many;
-// scale: what the stored gradient leaves out.  rows[i]: lse in units of log2, the factors of the
-// probabilities and of the targets, the label.
+// scale: what the stored gradient leaves out.  rows[i]: lse, the factors of the probabilities and
+// of the targets, the label.
 struct RowCoef {
-  float lse2, cp, ct;
+  float lse, cp, ct;
   int label;           // cross-entropy; distillation: -1
 };
 __global__ __launch_bounds__(1024) void vocab_index_kernel(VocabArgs a, const uint8_t* flag, int* at, int* place, int* n,
                                                            float* scale, RowCoef* rows) {
-  __shared__ int waves[16], counted[16], base;
+  __shared__ int waves[16], counted[16];
   const int t = threadIdx.x, lane = t & 63, w = t >> 6;
-  if (t == 0) base = 0;
-  int counts = 0;
-  for (int64_t r0 = 0; r0 < a.M; r0 += 1024) {
-    const int64_t row = r0 + t;
-    int f = 0;
-    if (row < a.M) {
-      if (a.teacher) {
-        f = flag[row];
-      } else {
-        const int64_t y = a.ids[row];
-        f = y < 0 ? 0 : y >= a.V ? 1 : 2;
-      }
+  constexpr int U = 8;   // rows of a thread at a time
+  // (neighbouring threads take neighbouring rows' runs: one scan of the workgroup, not one every 1024 rows)
+  const int64_t each = (a.M + 1023) / 1024, r0 = min(a.M, t * each), r1 = min(a.M, r0 + each);
+  auto kinds = [&](int64_t r, int (&f)[U], int (&label)[U]) {
+    if (a.teacher) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) f[u] = r + u < r1 ? flag[r + u] : 0, label[u] = -1;
+    } else {
+      int64_t y[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) y[u] = r + u < r1 ? a.ids[r + u] : -1;
+#pragma unroll
+      for (int u = 0; u < U; ++u) f[u] = y[u] < 0 ? 0 : y[u] >= a.V ? 1 : 2, label[u] = (int)y[u];
     }
-    counts += f != 0;
-    const uint64_t b = __ballot(f == 2);
-    if (lane == 0) waves[w] = __popcll(b);
-    __syncthreads();
-    int before = base, all = base;
-    for (int i = 0; i < 16; ++i) {
-      if (i < w) before += waves[i];
-      all += waves[i];
-    }
-    before += __popcll(b & ((1ull << lane) - 1));
-    if (row < a.M) place[row] = f == 2 ? before : -1;
-    if (f == 2) {
-      at[before] = (int)row;
-      const float ct = a.dloss ? __fmul_rn(a.dloss[row], a.T) : 1.f;
-      rows[before] = RowCoef{__fmul_rn(a.lse[row], 1.44269504088896341f), __fmul_rn(ct, __fmaf_rn(2.f * a.z_loss, a.lse[row], 1.f)), ct,
-                             a.teacher ? -1 : (int)a.ids[row]};
-    }
-    __syncthreads();
-    if (t == 0) base = all;
-    __syncthreads();
+  };
+  int mine = 0, counts = 0, f[U], label[U];
+  for (int64_t r = r0; r < r1; r += U) {
+    kinds(r, f, label);
+#pragma unroll
+    for (int u = 0; u < U; ++u) mine += f[u] == 2, counts += f[u] != 0;
+  }
+  int before = mine;
+  for (int d = 1; d < 64; d <<= 1) {
+    const int v = __shfl_up(before, d);
+    if (lane >= d) before += v;
   }
   for (int d = 32; d > 0; d >>= 1) counts += __shfl_xor(counts, d);
-  if (lane == 0) counted[w] = counts;
+  if (lane == 63) waves[w] = before, counted[w] = counts;
   __syncthreads();
-  if (t) return;
-  int c = 0;
-  for (int i = 0; i < 16; ++i) c += counted[i];
-  *n = base;
-  *scale = a.dloss ? 1.f : (float)((double)a.T / (double)max(c, 1));
+  before -= mine;
+  int all = 0, c = 0;
+  for (int i = 0; i < 16; ++i) {
+    if (i < w) before += waves[i];
+    all += waves[i];
+    c += counted[i];
+  }
+  if (t == 0) {
+    *n = all;
+    *scale = a.dloss ? 1.f : (float)((double)a.T / (double)max(c, 1));
+  }
+  for (int64_t r = r0; r < r1; r += U) {
+    kinds(r, f, label);
+    float lse[U], g[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      lse[u] = r + u < r1 ? a.lse[r + u] : 0.f;
+      g[u] = r + u < r1 && a.dloss ? __fmul_rn(a.dloss[r + u], a.T) : 1.f;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (r + u >= r1) continue;
+      place[r + u] = f[u] == 2 ? before : -1;
+      if (f[u] != 2) continue;
+      at[before] = (int)(r + u);
+      rows[before] = RowCoef{lse[u], __fmul_rn(g[u], __fmaf_rn(2.f * a.z_loss, lse[u], 1.f)), g[u], label[u]};
+      ++before;
+    }
+  }
 }
 
 // dst[i] = rows at[i] of src (at NULL: row i), n of them, widened to ldd with zeros; fp32 rows as three
@@ -454,7 +477,7 @@ struct GradEpi {
   const RowCoef* rows;
   uint16_t* dz;
   int64_t ldz, plane;
-  float cap, rcap, c;
+  float cap, rcap, rT;
   int v0;              // the piece's first vocabulary entry
   template <class Acc>
   __device__ __forceinline__ void operator()(const TilePlace& t, Acc& acc, char* const (&ring)[4], int lane, int wave, int wp,
@@ -463,33 +486,39 @@ struct GradEpi {
     const int h = lane >> 5, l32 = lane & 31;
     const int np = t.np - wp * IP * 32, nq = t.nq - wq * IQ * 32;
     char* lds = own_lds<T, (IP * IQ * 2048 > 4096 ? IP * IQ * 2048 : 4096)>(ring, wave);
-    auto fill = [&](auto Capped) {
+    RowCoef rc[IQ];
 #pragma unroll
-      for (int j = 0; j < IQ; ++j) {
-        const int q = j * 32 + l32;
-        RowCoef rc{0.f, 0.f, 0.f, -1};
-        if (q < nq) rc = rows[t.q0 + wq * IQ * 32 + q];
-        const int label = rc.label < 0 ? -1 : rc.label - v0 - t.p0 - wp * IP * 32;   // among this wavefront's entries
+    for (int j = 0; j < IQ; ++j) {
+      rc[j] = RowCoef{0.f, 0.f, 0.f, -1};
+      if (j * 32 + l32 < nq) rc[j] = rows[t.q0 + (wq * IQ + j) * 32 + l32];
+    }
+    auto fill = [&](auto Capped) __attribute__((always_inline)) {
+      each(std::make_integer_sequence<int, IP * IQ>{}, [&](auto B_) __attribute__((always_inline)) {
+        constexpr int i = decltype(B_)::value / IQ, j = decltype(B_)::value % IQ;
+        // the label among this block's entries
+        const int label = rc[j].label < 0 ? -1 : rc[j].label - v0 - t.p0 - (wp * IP + i) * 32 - h * 4;
+        const bool here = __any(label >= 0 && label < 32);
 #pragma unroll
-        for (int i = 0; i < IP; ++i) {
-          const bool here = __any(label >= i * 32 && label < i * 32 + 32);
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int v = i * 32 + 8 * (r >> 2) + h * 4 + (r & 3);
-            const float z = vocab_cap(acc[i][j][r], decltype(Capped)::value ? cap : 0.f, rcap);
-            float d = __fmul_rn(__builtin_amdgcn_exp2f(__fmaf_rn(z, c, -rc.lse2)), rc.cp);
-            if (here) d = v == label ? __fsub_rn(d, rc.ct) : d;
-            if constexpr (decltype(Capped)::value) {
-              const float x = __fmul_rn(z, rcap);
-              d = __fmul_rn(d, __fmaf_rn(-x, x, 1.f));
-            }
-            acc[i][j][r] = v < np ? d : 0.f;
+        for (int r = 0; r < 16; ++r) {
+          const float z = vocab_cap(acc[i][j][r], decltype(Capped)::value ? cap : 0.f, rcap);
+          float d = __fmul_rn(__builtin_amdgcn_exp2f(__fmul_rn(kLog2E, __fmaf_rn(z, rT, -rc[j].lse))), rc[j].cp);
+          if (here) d = 8 * (r >> 2) + (r & 3) == label ? __fsub_rn(d, rc[j].ct) : d;
+          if constexpr (decltype(Capped)::value) {
+            const float x = __fmul_rn(z, rcap);
+            d = __fmul_rn(d, __fmaf_rn(-x, x, 1.f));
           }
+          acc[i][j][r] = d;
         }
-      }
+        if (np < IP * 32) {   // the piece's last tile: zeros to the end of its 16-byte pieces
+#pragma unroll
+          for (int r = 0; r < 16; ++r) acc[i][j][r] = i * 32 + 8 * (r >> 2) + h * 4 + (r & 3) < np ? acc[i][j][r] : 0.f;
+        }
+      });
     };
     if (cap > 0.f) fill(std::true_type{});
     else fill(std::false_type{});
+    // piece x of a row q of LDS to the row's place: lanes of a store take SLOTS pieces each of 64 / SLOTS rows
+    const int s16 = lane % SLOTS, q0 = lane / SLOTS;
 #pragma unroll
     for (int p = 0; p < PL; ++p) {
       if (p) wave_lds_sync();
@@ -515,12 +544,15 @@ struct GradEpi {
             *reinterpret_cast<uint2*>(lds + q * (IP * 64) + slot * 16 + h * 8) = w;
           }
       wave_lds_sync();
-      uint16_t* out = dz + p * plane + ((int64_t)t.q0 + wq * IQ * 32) * ldz + t.p0 + wp * IP * 32;
+      // (rows up to 2^21 elements apart, at most 64 of them)
+      const rsrc_t out = make_rsrc(dz + p * plane + ((int64_t)t.q0 + wq * IQ * 32) * ldz + t.p0 + wp * IP * 32);
+      const uint32_t off = s16 * 8 < np ? (uint32_t)((q0 * ldz + s16 * 8) * 2) : kOOB;
+      const uint32_t step = (uint32_t)(64 / SLOTS * ldz * 2);
 #pragma unroll
       for (int u = 0; u < IQ * 32 * SLOTS / 64; ++u) {
-        const int x = u * 64 + lane, q = x / SLOTS, s = x % SLOTS;
-        const uint4 v = *reinterpret_cast<const uint4*>(lds + q * (IP * 64) + (s ^ (q & (SLOTS - 1))) * 16);
-        if (q < nq && s * 8 < np) *reinterpret_cast<uint4*>(out + q * ldz + s * 8) = v;
+        const int q = u * (64 / SLOTS) + q0;
+        const au32x4 v = *reinterpret_cast<const au32x4*>(lds + q * (IP * 64) + (s16 ^ (q & (SLOTS - 1))) * 16);
+        __builtin_amdgcn_raw_buffer_store_b128(v, out, q < nq ? off + u * step : kOOB, 0, 0);
       }
     }
   }
@@ -529,7 +561,7 @@ struct GradEpi {
 // Distillation, the entries' places in a piece: p less the weights of all the row's entries that name it, by
 // the first of them, from the logit that the forward kept.
 __device__ __forceinline__ float entry_grad(const VocabArgs& a, const RowCoef& rc, float z, float q) {
-  const float p = __builtin_amdgcn_exp2f(__fmaf_rn(z, 1.44269504088896341f / a.T, -rc.lse2));
+  const float p = __builtin_amdgcn_exp2f(__fmul_rn(kLog2E, __fsub_rn(__fdiv_rn(z, a.T), rc.lse)));
   float d = __fmaf_rn(rc.cp, p, -__fmul_rn(rc.ct, q));
   if (a.cap > 0.f) {
     const float x = __fmul_rn(z, a.rcap);
@@ -579,23 +611,29 @@ struct PartEpi {
   __device__ __forceinline__ void operator()(const TilePlace& t, Acc& acc, char* const (&)[4], int lane, int, int wp, int wq) const {
     const int np = t.np - wp * T::IP * 32, nq = t.nq - wq * T::IQ * 32, h4 = (lane >> 5) * 4, l32 = lane & 31;
     float* o = out + ((int64_t)t.split * rows + t.p0 + wp * T::IP * 32) * ld + t.q0 + wq * T::IQ * 32;
+    auto store = [&](auto Add) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < T::IP; ++i)
+      for (int i = 0; i < T::IP; ++i)
 #pragma unroll
-      for (int j = 0; j < T::IQ; ++j) {
-        const bool in = j * 32 + l32 < nq;
-        float v[16];
+        for (int j = 0; j < T::IQ; ++j) {
+          const bool in = j * 32 + l32 < nq;
+          float v[16];
+          if constexpr (decltype(Add)::value) {
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int p = i * 32 + 8 * (r >> 2) + h4 + (r & 3);
-          v[r] = add && in && p < np ? o[p * ld + j * 32 + l32] : 0.f;
+            for (int r = 0; r < 16; ++r) {
+              const int p = i * 32 + 8 * (r >> 2) + h4 + (r & 3);
+              v[r] = in && p < np ? o[p * ld + j * 32 + l32] : 0.f;
+            }
+          }
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int p = i * 32 + 8 * (r >> 2) + h4 + (r & 3);
+            if (in && p < np) o[p * ld + j * 32 + l32] = decltype(Add)::value ? __fadd_rn(v[r], acc[i][j][r]) : acc[i][j][r];
+          }
         }
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const int p = i * 32 + 8 * (r >> 2) + h4 + (r & 3);
-          if (in && p < np) o[p * ld + j * 32 + l32] = __fadd_rn(v[r], acc[i][j][r]);
-        }
-      }
+    };
+    if (add) store(std::true_type{});
+    else store(std::false_type{});
   }
 };
 
@@ -634,27 +672,35 @@ struct HeadEpi {
     // bf16: lanes 2l and 2l + 1 trade a value so that each stores two columns of a row
     const bool pair = !UPDATE && g.gbf && !g.accumulate && g.K % 2 == 0 && ((uintptr_t)g.dw & 3u) == 0;
     auto at = [&](int r) { return 8 * (r >> 2) + h4 + (r & 3); };
+    constexpr int N = 8;
+    OptState1 st[2][N];
+    float e[2][N];
+    auto fetch = [&](auto G_) __attribute__((always_inline)) {   // the states of elements N G .. of this lane
+      constexpr int G = decltype(G_)::value, r0 = G % (16 / N) * N, i = G / (16 / N) / T::IQ, j = G / (16 / N) % T::IQ;
+#pragma unroll
+      for (int r = 0; r < N; ++r) {
+        if (j * 32 + l32 >= nq || at(r0 + r) >= np - i * 32) continue;
+        const int64_t x = org + (i * 32 + at(r0 + r)) * g.K + j * 32 + l32;
+        st[G & 1][r] = opt_load1(o, g.W, x);
+        e[G & 1][r] = g.gW ? g.gW[x] : 0.f;
+      }
+    };
+    if constexpr (UPDATE) fetch(std::integral_constant<int, 0>{});
     each(std::make_integer_sequence<int, T::IP * T::IQ>{}, [&](auto B_) __attribute__((always_inline)) {
       constexpr int i = decltype(B_)::value / T::IQ, j = decltype(B_)::value % T::IQ;
       const int q = j * 32 + l32, n = np - i * 32;
       const int64_t o0 = org + (int64_t)i * 32 * g.K + q;
       if constexpr (UPDATE) {
-        constexpr int N = 8;   // elements at a time: their states' loads are in flight together
+        // (the states of the next elements are asked for before these are updated)
         each(std::make_integer_sequence<int, 16 / N>{}, [&](auto R_) __attribute__((always_inline)) {
-          constexpr int r0 = decltype(R_)::value * N;
-          OptState1 st[N];
-          float e[N];
+          constexpr int g0 = decltype(B_)::value * (16 / N) + decltype(R_)::value;
+          if constexpr (g0 + 1 < T::IP * T::IQ * (16 / N)) fetch(std::integral_constant<int, g0 + 1>{});
 #pragma unroll
           for (int r = 0; r < N; ++r) {
-            if (q >= nq || at(r0 + r) >= n) continue;
-            st[r] = opt_load1(o, g.W, o0 + at(r0 + r) * g.K);
-            e[r] = g.gW ? g.gW[o0 + at(r0 + r) * g.K] : 0.f;
-          }
-#pragma unroll
-          for (int r = 0; r < N; ++r) {
+            constexpr int r0 = decltype(R_)::value * N;
             if (q >= nq || at(r0 + r) >= n) continue;
             const float d = __fmul_rn(acc[i][j][r0 + r], scale);
-            opt_apply1(o, g.W, st[r], g.gW ? __fadd_rn(e[r], d) : d, o0 + at(r0 + r) * g.K);
+            opt_apply1(o, g.W, st[g0 & 1][r], g.gW ? __fadd_rn(e[g0 & 1][r], d) : d, o0 + at(r0 + r) * g.K);
           }
         });
       } else if (pair) {
@@ -686,7 +732,14 @@ __global__ __launch_bounds__(256) void vocab_head_kernel(HeadGrad g, const float
     const int64_t r = i / g.K, c = i - r * g.K;
     const float* p = part + r * ld + c;
     float v = p[0];
-    for (int s = 1; s < S; ++s) v = __fadd_rn(v, p[s * rows * ld]);
+    for (int s = 1; s < S; s += 8) {   // eight loads in flight
+      float x[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) x[u] = s + u < S ? p[(s + u) * rows * ld] : 0.f;
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        if (s + u < S) v = __fadd_rn(v, x[u]);
+    }
     v = __fmul_rn(v, scale);
     if (g.dw) g.store(i, v);
     else update1(o, g.W, g.gW ? __fadd_rn(g.gW[i], v) : v, i);
@@ -706,14 +759,22 @@ __global__ __launch_bounds__(256) void vocab_dx_kernel(const float* part, int S,
 #pragma unroll
     for (int e = 0; e < V; ++e) v[e] = 0.f;
     if (r >= 0) {
-      for (int s = 0; s < S; ++s) {
-        const float* p = part + ((int64_t)s * M + r) * ld + c;
-        if constexpr (V == 4) {
-          const float4 x = ld4(p);
-          v[0] = __fadd_rn(v[0], x.x), v[1] = __fadd_rn(v[1], x.y), v[2] = __fadd_rn(v[2], x.z), v[3] = __fadd_rn(v[3], x.w);
-        } else {
-          v[0] = __fadd_rn(v[0], *p);
+      const float* p = part + (int64_t)r * ld + c;
+      for (int s = 0; s < S; s += 8) {   // eight loads in flight
+        float x[8][V];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+          if constexpr (V == 4) {
+            const float4 y = s + u < S ? ld4(p + (s + u) * M * ld) : make_float4(0.f, 0.f, 0.f, 0.f);
+            x[u][0] = y.x, x[u][1] = y.y, x[u][2] = y.z, x[u][3] = y.w;
+          } else {
+            x[u][0] = s + u < S ? p[(s + u) * M * ld] : 0.f;
+          }
         }
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+#pragma unroll
+          for (int e = 0; e < V; ++e) v[e] = __fadd_rn(v[e], x[u][e]);
       }
     }
 #pragma unroll
@@ -886,12 +947,12 @@ struct Tiles {
   template <class T>
   hipError_t stats(const Operand& x, const Operand& w, int64_t v0, int64_t n) const {
     const Entries en{at<int>(p.off), at<uint32_t>(p.list), (int)p.vtiles};
-    const StatEpi<T> e{at<float2>(p.part), a.zt, en, (int)(v0 / T::BP), a.M, a.k, a.cap, a.rcap, 1.44269504088896341f / a.T};
+    const StatEpi<T> e{at<float2>(p.part), a.zt, en, (int)(v0 / T::BP), a.M, a.k, a.cap, a.rcap, kLog2E / a.T};
     return product<T, PL, true, true>(w, x, n, a.M, a.K, nullptr, 1, e, s);
   }
   template <class T>
   hipError_t grads(const Operand& w, int64_t v0, int64_t n) const {
-    const GradEpi<T, PL> e{at<RowCoef>(p.rows), at<uint16_t>(p.dz), p.ldz, p.pz, a.cap, a.rcap, 1.44269504088896341f / a.T, (int)v0};
+    const GradEpi<T, PL> e{at<RowCoef>(p.rows), at<uint16_t>(p.dz), p.ldz, p.pz, a.cap, a.rcap, 1.f / a.T, (int)v0};
     return product<T, PL, true, true>(w, Operand{at<uint16_t>(p.x), p.Kp, p.px}, n, a.M, a.K, at<int>(p.n), 1, e, s);
   }
   template <class T>
