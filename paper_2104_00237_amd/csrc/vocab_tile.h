@@ -2,10 +2,10 @@
 // v_mfma_f32_32x32x16_bf16, with what becomes of a finished tile left to an epilogue.
 //
 // A workgroup's wavefronts (WP x WQ of them) hold IP x IQ blocks of 32x32 each.  Operands go from
-// memory straight to LDS, in stages of BK reduction elements, a ring of four of them:
-//   step 0 .. n-2 of stage c   MFMAs of step k, LDS reads of step k + 1, the rest of stage c + 3 requested
-//   barrier                    stage c has been read, stage c + 1 has landed; two stages stay in flight
-//   step n-1                   MFMAs, reads of stage c + 1's step 0, the first loads of stage c + 4
+// memory straight to LDS, in stages of BK reduction elements, a ring of NS of them:
+//   step 0 .. n-2 of stage c   MFMAs of step k, LDS reads of step k + 1, the rest of stage c + NS - 1 requested
+//   barrier                    stage c has been read, stage c + 1 has landed; NS - 2 stages stay in flight
+//   step n-1                   MFMAs, reads of stage c + 1's step 0, the first loads of stage c + NS
 // Loads are spread over all MFMAs: sixteen at once take a CU's load path twice the time of the MFMAs
 // beside them, and the wavefront, which issues in order, waits.
 //
@@ -46,9 +46,9 @@ __device__ __forceinline__ void each(std::integer_sequence<int, T...>, F&& f) {
   (f(std::integral_constant<int, T>{}), ...);
 }
 
-template <int IP_, int IQ_, int WP_, int WQ_, int BK_, int OCC_>
+template <int IP_, int IQ_, int WP_, int WQ_, int BK_, int NS_, int OCC_>
 struct TileShape {
-  static constexpr int IP = IP_, IQ = IQ_, WP = WP_, WQ = WQ_, BK = BK_, OCC = OCC_;
+  static constexpr int IP = IP_, IQ = IQ_, WP = WP_, WQ = WQ_, BK = BK_, NS = NS_, OCC = OCC_;
   static constexpr int NW = WP * WQ, NT = NW * 64;
   static constexpr int BP = WP * IP * 32, BQ = WQ * IQ * 32;
   static constexpr int ABYTES = BP * BK * 2, BBYTES = BQ * BK * 2;
@@ -56,6 +56,7 @@ struct TileShape {
   static constexpr int NK = BK / 16;                                                     // steps of a stage
   static_assert(NA * NW * 1024 == ABYTES && NB * NW * 1024 == BBYTES, "whole loads for every wavefront");
   static_assert(BK == 32 || BK == 64, "stages");
+  static_assert(NS == 3 || NS == 4, "stages of the ring");
 };
 
 // Loads of one operand's stages by one wavefront: N instructions of 1 KB.
@@ -143,71 +144,68 @@ __device__ __forceinline__ bool tile_place(const TileProblem& pr, int rows_dim, 
   return t->np > 0 && t->nq > 0;
 }
 
-// The main loop.  e(place, acc, lds, lane, wave, wp, wq): the finished tile; lds: the ring, free.
+// A workgroup's tile: what its main loop works on.
 template <class T, int PL, bool A_RC, bool B_RC, class Epi>
-__global__ __launch_bounds__(T::NT, T::OCC) void tile_kernel(TileProblem pr, Epi e) {
-  constexpr int IP = T::IP, IQ = T::IQ, NK = T::NK, NL = T::NL, STAGE = T::ABYTES + T::BBYTES;
-  __shared__ __attribute__((aligned(1024))) char s0[STAGE], s1[STAGE], s2[STAGE], s3[STAGE];
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wp = wave % T::WP, wq = wave / T::WP;
-  TilePlace t;
-  if (!tile_place<T>(pr, Epi::ROWS, &t)) return;
-  const int nst = (t.rend - t.rbeg + T::BK - 1) / T::BK;
-  const StageLoad<A_RC, T::BP, T::BK, T::NA> la(pr.lda, t.np, lane, wave);
-  const StageLoad<B_RC, T::BQ, T::BK, T::NB> lb(pr.ldb, t.nq, lane, wave);
-  const char* A = (const char*)(pr.A + (A_RC ? t.p0 * pr.lda + t.rbeg : t.rbeg * pr.lda + t.p0));
-  const char* B = (const char*)(pr.B + (B_RC ? t.q0 * pr.ldb + t.rbeg : t.rbeg * pr.ldb + t.q0));
-  const int64_t da = (A_RC ? 1 : pr.lda) * T::BK * 2, db = (B_RC ? 1 : pr.ldb) * T::BK * 2;
+struct TileLoop {
+  static constexpr int IP = T::IP, IQ = T::IQ, NK = T::NK, MF = IP * IQ;
+  static constexpr int READA = (A_RC ? 1 : 2) * IP, READB = (B_RC ? 1 : 2) * IQ;   // LDS reads of a step
+  const TileProblem& pr;
+  const TilePlace& t;
+  const int lane, wave, wp, wq, nst;
+  const StageLoad<A_RC, T::BP, T::BK, T::NA> la;
+  const StageLoad<B_RC, T::BQ, T::BK, T::NB> lb;
+  const char *A, *B;
+  const int64_t da, db;
+  vacc_t (&acc)[IP][IQ];
 
-  vacc_t acc[IP][IQ];
-#pragma unroll
-  for (int i = 0; i < IP; ++i)
-#pragma unroll
-    for (int j = 0; j < IQ; ++j)
-#pragma unroll
-      for (int k = 0; k < 16; ++k) acc[i][j][k] = 0.f;
-  struct Frags {
-    vbf16x8_t a[IP], b[IQ];
-  };
-  Frags f[2];
-
-  // loads [from, to) of stage c.  Planes: a stage for each of the products high high, high middle, high
-  // low, middle high, middle middle, low high of the same reduction elements
-  auto request = [&](char* s, int c, int from, int to) __attribute__((always_inline)) {
-    const int k = PL == 1 ? c : c / 6, pi = PL == 1 ? 0 : (c - k * 6) * 4;
-    const int nr = k < nst ? t.rend - t.rbeg - k * T::BK : 0;   // 0 past the end: zeros
-    const int64_t at = k < nst ? k : 0;
-    const char *a = A + at * da, *b = B + at * db;
-    if constexpr (PL == 3) a += (0x211000 >> pi & 3) * pr.pa * 2, b += (0x010210 >> pi & 3) * pr.pb * 2;
-    const rsrc_t ra = make_rsrc(a), rb = make_rsrc(b);
-#pragma unroll
-    for (int i = 0; i < NL; ++i) {
-      if (i < from || i >= to) continue;
-      if (i < T::NA) {
-        load_lds(ra, s + (wave * T::NA + i) * 1024, la.r[i % T::NA] < nr ? la.off[i % T::NA] : kOOB);
-      } else {
-        const int u = (i - T::NA) % T::NB;
-        load_lds(rb, s + T::ABYTES + (wave * T::NB + u) * 1024, lb.r[u] < nr ? lb.off[u] : kOOB);
-      }
-    }
-  };
-  auto read = [&](Frags& d, const char* s, int k) __attribute__((always_inline)) {
-#pragma unroll
-    for (int i = 0; i < IP; ++i) d.a[i] = stage_frag<A_RC, T::BP, T::BK>(s, (wp * IP + i) * 32, k, lane);
-#pragma unroll
-    for (int j = 0; j < IQ; ++j) d.b[j] = stage_frag<B_RC, T::BQ, T::BK>(s + T::ABYTES, (wq * IQ + j) * 32, k, lane);
-  };
-  auto mfma = [&](const Frags& d) __attribute__((always_inline)) {
+  __device__ __forceinline__ TileLoop(const TileProblem& pr_, const TilePlace& t_, vacc_t (&acc_)[IP][IQ], int lane_, int wave_)
+      : pr(pr_), t(t_), lane(lane_), wave(wave_), wp(wave_ % T::WP), wq(wave_ / T::WP),
+        nst((t_.rend - t_.rbeg + T::BK - 1) / T::BK), la(pr_.lda, t_.np, lane_, wave_), lb(pr_.ldb, t_.nq, lane_, wave_),
+        A((const char*)(pr_.A + (A_RC ? t_.p0 * pr_.lda + t_.rbeg : t_.rbeg * pr_.lda + t_.p0))),
+        B((const char*)(pr_.B + (B_RC ? t_.q0 * pr_.ldb + t_.rbeg : t_.rbeg * pr_.ldb + t_.q0))),
+        da((A_RC ? 1 : pr_.lda) * T::BK * 2), db((B_RC ? 1 : pr_.ldb) * T::BK * 2), acc(acc_) {
 #pragma unroll
     for (int i = 0; i < IP; ++i)
 #pragma unroll
-      for (int j = 0; j < IQ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(d.a[i], d.b[j], acc[i][j], 0, 0, 0);
-  };
-  // MFMAs with a share of the LDS reads and of the loads behind each
-  constexpr int READS = (A_RC ? 1 : 2) * IP + (B_RC ? 1 : 2) * IQ, MF = IP * IQ;
-  auto sched = [&](auto N) __attribute__((always_inline)) {
-    constexpr int n = decltype(N)::value;
+      for (int j = 0; j < IQ; ++j)
+#pragma unroll
+        for (int k = 0; k < 16; ++k) acc[i][j][k] = 0.f;
+  }
+  // Reduction elements of stage c inside the operands (0 past the end: zeros), and where it starts.
+  __device__ __forceinline__ int inside(int c) const { return c < nst ? t.rend - t.rbeg - c * T::BK : 0; }
+  __device__ __forceinline__ int64_t start(int c) const { return c < nst ? c : 0; }
+  // Loads [FROM, TO) of this wavefront of A's stage c, plane p.
+  template <int FROM, int TO>
+  __device__ __forceinline__ void load_a(char* s, int c, int p) const {
+    const int nr = inside(c);
+    const rsrc_t r = make_rsrc(A + start(c) * da + p * pr.pa * 2);
+#pragma unroll
+    for (int i = FROM; i < TO; ++i) load_lds(r, s + (wave * T::NA + i) * 1024, la.r[i] < nr ? la.off[i] : kOOB);
+  }
+  template <int FROM, int TO>
+  __device__ __forceinline__ void load_b(char* s, int c, int p) const {
+    const int nr = inside(c);
+    const rsrc_t r = make_rsrc(B + start(c) * db + p * pr.pb * 2);
+#pragma unroll
+    for (int i = FROM; i < TO; ++i) load_lds(r, s + (wave * T::NB + i) * 1024, lb.r[i] < nr ? lb.off[i] : kOOB);
+  }
+  __device__ __forceinline__ void read_a(vbf16x8_t (&f)[IP], const char* s, int k) const {
+#pragma unroll
+    for (int i = 0; i < IP; ++i) f[i] = stage_frag<A_RC, T::BP, T::BK>(s, (wp * IP + i) * 32, k, lane);
+  }
+  __device__ __forceinline__ void read_b(vbf16x8_t (&f)[IQ], const char* s, int k) const {
+#pragma unroll
+    for (int j = 0; j < IQ; ++j) f[j] = stage_frag<B_RC, T::BQ, T::BK>(s, (wq * IQ + j) * 32, k, lane);
+  }
+  __device__ __forceinline__ void mfma(const vbf16x8_t (&a)[IP], const vbf16x8_t (&b)[IQ]) const {
+#pragma unroll
+    for (int i = 0; i < IP; ++i)
+#pragma unroll
+      for (int j = 0; j < IQ; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[i], b[j], acc[i][j], 0, 0, 0);
+  }
+  // A step's MFMAs with a share of its LDS reads and of its loads behind each.
+  template <int READS, int LOADS>
+  __device__ __forceinline__ static void sched() {
 #pragma unroll
     for (int g = 0; g < MF; ++g) {
       __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
@@ -215,51 +213,190 @@ __global__ __launch_bounds__(T::NT, T::OCC) void tile_kernel(TileProblem pr, Epi
       for (int u = 0; u < READS; ++u)
         if (u * MF / READS / 2 == g) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
 #pragma unroll
-      for (int u = 0; u < n; ++u)
-        if (u * MF / n + MF / n / 2 == g) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+      for (int u = 0; u < LOADS; ++u)
+        if (u * MF / LOADS + MF / LOADS / 2 == g) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
     }
     __builtin_amdgcn_sched_barrier(0);
-  };
-  // loads that step k of a stage asks for (of stage c + 3; the last step: the first of stage c + 4)
-  constexpr int L1 = (NL + NK - 1) / NK;
-
-  // Stage c is in s, stage c + 1 lands in sn, stage c + 3 is asked for in s3n.
-  auto stage = [&](char* s, char* sn, char* s3n, int c) __attribute__((always_inline)) {
-    each(std::make_integer_sequence<int, NK - 1>{}, [&](auto K_) {
-      constexpr int k = decltype(K_)::value;
-      read(f[(k + 1) & 1], s, k + 1);
-      request(s3n, c + 3, L1 + k * (NL - L1) / (NK - 1), L1 + (k + 1) * (NL - L1) / (NK - 1));
-      mfma(f[k & 1]);
-      sched(std::integral_constant<int, L1 + (k + 1) * (NL - L1) / (NK - 1) - (L1 + k * (NL - L1) / (NK - 1))>{});
-    });
-    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * NL) : "memory");
+  }
+  // All LDS reads of this wavefront done and all but its LEFT latest loads landed; then everyone's.
+  template <int LEFT>
+  __device__ __forceinline__ static void sync() {
     __builtin_amdgcn_sched_barrier(0);
-    read(f[0], sn, 0);
-    request(s, c + 4, 0, L1);
-    mfma(f[(NK - 1) & 1]);
-    sched(std::integral_constant<int, L1>{});
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(LEFT) : "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  }
+};
+
+// LDS arrays by their addresses.  (Opaque to the compiler, which otherwise makes a constant table of
+// them, where LDS addresses cannot stand.)
+typedef __attribute__((address_space(3))) char lds_char;
+struct Ring {
+  uint32_t at[8];
+};
+__device__ __forceinline__ uint32_t lds_address(char* p) {
+  uint32_t a = (uint32_t)(uintptr_t)(lds_char*)p;
+  asm volatile("" : "+s"(a));
+  return a;
+}
+
+// The main loop.  e(place, acc, ring, lane, wave, wp, wq): the finished tile; ring: LDS, free, in arrays
+// of kRingBytes.
+template <class T, int PL>
+constexpr int kRingBytes = PL == 1 ? T::ABYTES + T::BBYTES : T::ABYTES < T::BBYTES ? T::ABYTES : T::BBYTES;
+template <class T, int PL>
+constexpr int kRingArrays = PL == 1 ? T::NS : 8;
+
+template <class T, bool A_RC, bool B_RC, class Epi>
+__device__ __forceinline__ void tile_body1(const TileProblem& pr, const TilePlace& t, const Epi& e, int lane, int wave) {
+  constexpr int IP = T::IP, IQ = T::IQ, NK = T::NK, NA = T::NA, NL = T::NL, NS = T::NS, STAGE = T::ABYTES + T::BBYTES;
+  using Loop = TileLoop<T, 1, A_RC, B_RC, Epi>;
+  __shared__ __attribute__((aligned(1024))) char s0[STAGE], s1[STAGE], s2[STAGE], s3[NS == 4 ? STAGE : 16];
+  vacc_t acc[IP][IQ];
+  const Loop l(pr, t, acc, lane, wave);
+  vbf16x8_t a[2][IP], b[2][IQ];
+
+  // loads [FROM, TO) of stage c, A's first
+  auto request = [&](char* s, int c, auto From, auto To) __attribute__((always_inline)) {
+    constexpr int from = decltype(From)::value, to = decltype(To)::value;
+    if constexpr (from < NA) l.template load_a<from, (to < NA ? to : NA)>(s, c, 0);
+    if constexpr (to > NA) l.template load_b<(from > NA ? from - NA : 0), to - NA>(s + T::ABYTES, c, 0);
+  };
+  auto read = [&](int f, const char* s, int k) __attribute__((always_inline)) {
+    l.read_a(a[f], s, k);
+    l.read_b(b[f], s + T::ABYTES, k);
+  };
+  // loads that the last step of a stage asks for, the first of stage c + NS
+  constexpr int L1 = (NL + NK - 1) / NK;
+  using First = std::integral_constant<int, L1>;
+  using Zero = std::integral_constant<int, 0>;
+  using All = std::integral_constant<int, NL>;
+  // Stage c is in s, stage c + 1 lands in sn, the rest of stage c + NS - 1 is asked for in sl.
+  auto stage = [&](char* s, char* sn, char* sl, int c) __attribute__((always_inline)) {
+    each(std::make_integer_sequence<int, NK - 1>{}, [&](auto K_) __attribute__((always_inline)) {
+      constexpr int k = decltype(K_)::value;
+      constexpr int from = L1 + k * (NL - L1) / (NK - 1), to = L1 + (k + 1) * (NL - L1) / (NK - 1);
+      read((k + 1) & 1, s, k + 1);
+      request(sl, c + NS - 1, std::integral_constant<int, from>{}, std::integral_constant<int, to>{});
+      l.mfma(a[k & 1], b[k & 1]);
+      Loop::template sched<Loop::READA + Loop::READB, to - from>();
+    });
+    Loop::template sync<(NS - 2) * NL>();
+    read(0, sn, 0);
+    request(s, c + NS, Zero{}, First{});
+    l.mfma(a[(NK - 1) & 1], b[(NK - 1) & 1]);
+    Loop::template sched<Loop::READA + Loop::READB, L1>();
   };
 
-  request(s0, 0, 0, NL);
-  request(s1, 1, 0, NL);
-  request(s2, 2, 0, NL);
-  request(s3, 3, 0, L1);
-  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(2 * NL + L1) : "memory");
-  __builtin_amdgcn_sched_barrier(0);
-  read(f[0], s0, 0);
+  request(s0, 0, Zero{}, All{});
+  request(s1, 1, Zero{}, All{});
+  if constexpr (NS == 4) {
+    request(s2, 2, Zero{}, All{});
+    request(s3, 3, Zero{}, First{});
+  } else {
+    request(s2, 2, Zero{}, First{});
+  }
+  Loop::template sync<(NS - 2) * NL + L1>();
+  read(0, s0, 0);
   __builtin_amdgcn_sched_barrier(0);
   // (stages past the end are zeros: a branch around them makes the compiler move accumulators
   // between register files)
-  for (int c = 0; c < (PL == 1 ? nst : 6 * nst); c += 4) {
-    stage(s0, s1, s3, c);
-    stage(s1, s2, s0, c + 1);
-    stage(s2, s3, s1, c + 2);
-    stage(s3, s0, s2, c + 3);
+  for (int c = 0; c < l.nst; c += NS) {
+    if constexpr (NS == 4) {
+      stage(s0, s1, s3, c);
+      stage(s1, s2, s0, c + 1);
+      stage(s2, s3, s1, c + 2);
+      stage(s3, s0, s2, c + 3);
+    } else {
+      stage(s0, s1, s2, c);
+      stage(s1, s2, s0, c + 1);
+      stage(s2, s0, s1, c + 2);
+    }
   }
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  Loop::template sync<0>();
+  const Ring ring{{lds_address(s0), lds_address(s1), lds_address(s2), NS == 4 ? lds_address(s3) : 0u, 0u, 0u, 0u, 0u}};
+  e(t, acc, ring, lane, wave, l.wp, l.wq);
+}
+
+// Three planes: six products of a stage's 32 reduction elements in six phases of two steps, each plane
+// loaded to LDS once,
+//   phase      0            1            2            3              4               5
+//   product    high high    high middle  high low     middle high    middle middle   low high
+//   loads      A low        B high'      A high'      B middle'      B low'          A middle'   (': next stage)
+// A's fragments stay in registers while their plane is in use.  A slot is asked for once its last reader
+// is behind a barrier, three phases before its first; B's high and middle planes have two slots each.
+template <class T, bool A_RC, bool B_RC, class Epi>
+__device__ __forceinline__ void tile_body3(const TileProblem& pr, const TilePlace& t, const Epi& e, int lane, int wave) {
+  constexpr int IP = T::IP, IQ = T::IQ, NA = T::NA, NB = T::NB, A1 = (NA + 1) / 2, B1 = (NB + 1) / 2;
+  static_assert(T::NK == 2, "stages of 32");
+  using Loop = TileLoop<T, 3, A_RC, B_RC, Epi>;
+  __shared__ __attribute__((aligned(1024))) char ah[T::ABYTES], am[T::ABYTES], al[T::ABYTES];
+  __shared__ __attribute__((aligned(1024))) char bh0[T::BBYTES], bh1[T::BBYTES], bm0[T::BBYTES], bm1[T::BBYTES], bl[T::BBYTES];
+  vacc_t acc[IP][IQ];
+  const Loop l(pr, t, acc, lane, wave);
+  vbf16x8_t a[2][IP], b[2][IQ];
+
+  // Stage c in ah, am, al, bh, bm, bl; the next one's in bhn, bmn and the others.
+  auto stage = [&](char* bh, char* bhn, char* bm, char* bmn, int c) __attribute__((always_inline)) {
+    each(std::make_integer_sequence<int, 12>{}, [&](auto S_) __attribute__((always_inline)) {
+      constexpr int s = decltype(S_)::value, f = s / 2, k = s % 2, s1 = (s + 1) % 12, f1 = s1 / 2;
+      // loads landed by the barriers of phases 5 (B high', A high'), 0 (B middle), 1 (B low), 2 (A middle) and 4 (A
+      // low): all but those of the two phases before
+      constexpr int left[6] = {NB + NA, NA + NA, NA + NB, NB + NA, NA + NB, NB + NB};
+      if constexpr (k == 1) Loop::template sync<left[f]>();
+      constexpr bool next_a = s1 < 2 || s1 == 6 || s1 == 7 || s1 >= 10;
+      if constexpr (next_a) l.read_a(a[s1 % 2], f1 < 3 ? ah : f1 < 5 ? am : al, s1 % 2);
+      l.read_b(b[s1 % 2], f1 == 2 ? bl : f1 == 1 || f1 == 4 ? bm : s == 11 ? bhn : bh, s1 % 2);
+      // a phase's loads: the first behind its barrier, the rest in the next step
+      constexpr int g = k == 1 ? f : (f + 5) % 6;   // whose
+      constexpr bool first = k == 1, of_a = g == 0 || g == 2 || g == 5;
+      if constexpr (g == 0) l.template load_a<first ? 0 : A1, first ? A1 : NA>(al, c, 2);
+      if constexpr (g == 1) l.template load_b<first ? 0 : B1, first ? B1 : NB>(bhn, c + 1, 0);
+      if constexpr (g == 2) l.template load_a<first ? 0 : A1, first ? A1 : NA>(ah, c + 1, 0);
+      if constexpr (g == 3) l.template load_b<first ? 0 : B1, first ? B1 : NB>(bmn, c + 1, 1);
+      if constexpr (g == 4) l.template load_b<first ? 0 : B1, first ? B1 : NB>(bl, c + 1, 2);
+      if constexpr (g == 5) l.template load_a<first ? 0 : A1, first ? A1 : NA>(am, first ? c + 1 : c, 1);
+      l.mfma(a[k], b[k]);
+      Loop::template sched<(next_a ? Loop::READA : 0) + Loop::READB, of_a ? (first ? A1 : NA - A1) : (first ? B1 : NB - B1)>();
+    });
+  };
+
+  l.template load_b<0, NB>(bh0, 0, 0);
+  l.template load_a<0, NA>(ah, 0, 0);
+  l.template load_b<0, NB>(bm0, 0, 1);
+  l.template load_b<0, NB>(bl, 0, 2);
+  l.template load_a<0, A1>(am, 0, 1);
+  Loop::template sync<NB + NB + A1>();
+  l.read_a(a[0], ah, 0);
+  l.read_b(b[0], bh0, 0);
   __builtin_amdgcn_sched_barrier(0);
-  char* const ring[4] = {s0, s1, s2, s3};
-  e(t, acc, ring, lane, wave, wp, wq);
+  for (int c = 0; c < l.nst; c += 2) {
+    stage(bh0, bh1, bm0, bm1, c);
+    stage(bh1, bh0, bm1, bm0, c + 1);
+  }
+  Loop::template sync<0>();
+  const Ring ring{{lds_address(ah), lds_address(am), lds_address(al), lds_address(bh0), lds_address(bh1), lds_address(bm0),
+                   lds_address(bm1), lds_address(bl)}};
+  e(t, acc, ring, lane, wave, l.wp, l.wq);
+}
+
+template <class T, int PL, bool A_RC, bool B_RC, class Epi>
+__global__ __launch_bounds__(T::NT, T::OCC) void tile_kernel(TileProblem pr, Epi e) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  TilePlace t;
+  if (!tile_place<T>(pr, Epi::ROWS, &t)) return;
+  if constexpr (PL == 1) tile_body1<T, A_RC, B_RC>(pr, t, e, lane, wave);
+  else tile_body3<T, A_RC, B_RC>(pr, t, e, lane, wave);
+}
+
+// Part i of the ring, BYTES each, of at least COUNT.
+template <class T, int PL, int BYTES, int COUNT>
+__device__ __forceinline__ char* ring_part(const Ring& ring, int i) {
+  constexpr int EACH = kRingBytes<T, PL> / BYTES;
+  static_assert(EACH * kRingArrays<T, PL> >= COUNT, "parts of the ring");
+  uint32_t a = ring.at[0];
+#pragma unroll
+  for (int r = 1; r < kRingArrays<T, PL>; ++r) a = i / EACH == r ? ring.at[r] : a;
+  return (char*)(lds_char*)(uintptr_t)(a + (uint32_t)(i % EACH) * BYTES);
 }
 
 }  // namespace opfuse

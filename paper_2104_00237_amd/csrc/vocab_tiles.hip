@@ -25,10 +25,11 @@ namespace {
 
 // Tiles (rows x columns, in wavefronts of 4x2, 2x2 and 1x1 blocks): a 256x256 tile a CU with two
 // wavefronts a SIMD, 128x128 where those would not fill the chip, 32 wide for few rows.
-using Big = TileShape<4, 2, 2, 4, 32, 2>;
-using Mid = TileShape<2, 2, 2, 2, 32, 2>;
-using FewQ = TileShape<1, 1, 4, 1, 64, 2>;   // 128 x 32
-using FewP = TileShape<1, 1, 1, 4, 64, 2>;   // 32 x 128
+using Big = TileShape<4, 2, 2, 4, 32, 4, 2>;
+using Mid = TileShape<2, 2, 2, 2, 32, 4, 2>;
+using Half = TileShape<4, 2, 2, 2, 32, 3, 2>;   // 256x128, two workgroups a CU: one's epilogue beside the other's MFMAs
+using FewQ = TileShape<1, 1, 4, 1, 64, 4, 2>;   // 128 x 32
+using FewP = TileShape<1, 1, 1, 4, 64, 4, 2>;   // 32 x 128
 
 constexpr int kFew = 32;                     // rows up to which a product's tiles are 32 wide
 
@@ -38,14 +39,6 @@ int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 int64_t per(int64_t n, int64_t each) { return (n + each - 1) / each; }
 bool odd_rows(const void* p, int64_t ld, int64_t K) { return !aligned16(p) || ld % 8 != 0 || K % 8 != 0; }
 
-// A wavefront's own part of the ring once the main loop is done: BYTES each.
-template <class T, int BYTES>
-__device__ __forceinline__ char* own_lds(char* const (&ring)[4], int wave) {
-  constexpr int EACH = (T::ABYTES + T::BBYTES) / BYTES;
-  static_assert(EACH * 4 >= T::NW, "room for every wavefront");
-  const int r = wave / EACH;
-  return (r == 0 ? ring[0] : r == 1 ? ring[1] : r == 2 ? ring[2] : ring[3]) + (wave % EACH) * BYTES;
-}
 // The nearest bf16s of two values, which keep what that leaves.  Infinity (and what would round to it)
 // counts as the largest bf16: with an infinite high part, the other operand's low parts of 0 would make a NaN.
 __device__ __forceinline__ uint32_t take_part(float& x, float& y) {
@@ -147,7 +140,7 @@ __device__ __forceinline__ float2 stat2_join(float2 x, float2 y, float c) {
 }
 
 // A = W, B = X: a lane's accumulators are one row's logits, for statistics within the lane.
-template <class T>
+template <class T, int PL>
 struct StatEpi {
   static constexpr int ROWS = ROWS_NONE;
   float2* part;        // [vtiles][M]
@@ -158,7 +151,7 @@ struct StatEpi {
   int k;
   float cap, rcap, c;  // c = log2(e) / T
   template <class Acc>
-  __device__ __forceinline__ void operator()(const TilePlace& t, Acc& acc, char* const (&ring)[4], int lane, int wave, int wp,
+  __device__ __forceinline__ void operator()(const TilePlace& t, Acc& acc, const Ring& ring, int lane, int wave, int wp,
                                              int wq) const {
     constexpr int IP = T::IP, IQ = T::IQ;
     const int h4 = (lane >> 5) * 4, l32 = lane & 31;
@@ -176,7 +169,7 @@ struct StatEpi {
     const int e0 = off[0], e1 = off[1];
     if (e1 > e0) {
       const uint32_t* list = en.list + (int64_t)rt * T::BQ * k;
-      float* lds = (float*)own_lds<T, (IP * IQ * 2048 > 4096 ? IP * IQ * 2048 : 4096)>(ring, wave);
+      float* lds = (float*)ring_part<T, PL, 4096, T::NW>(ring, wave);
       constexpr int U = 4;   // entries of a lane at a time
       for (int b = e0; b < e1; b += 64 * U) {
         uint32_t x[U];
@@ -234,7 +227,8 @@ struct StatEpi {
       s[j] = __fadd_rn(s[j], __shfl_xor(s[j], 32));
     }
     // the wavefronts of a row's vocabulary entries join in LDS
-    float2* sh = (float2*)ring[0];   // [WP][BQ]
+    static_assert(T::WP * T::BQ * 8 <= kRingBytes<T, PL>, "room for the join");
+    float2* sh = (float2*)ring_part<T, PL, T::WP * T::BQ * 8, 1>(ring, 0);   // [WP][BQ]
     __syncthreads();
     if (lane < 32) {
 #pragma unroll
@@ -480,21 +474,21 @@ struct GradEpi {
   float cap, rcap, rT;
   int v0;              // the piece's first vocabulary entry
   template <class Acc>
-  __device__ __forceinline__ void operator()(const TilePlace& t, Acc& acc, char* const (&ring)[4], int lane, int wave, int wp,
+  __device__ __forceinline__ void operator()(const TilePlace& t, Acc& acc, const Ring& ring, int lane, int wave, int wp,
                                              int wq) const {
     constexpr int IP = T::IP, IQ = T::IQ, SLOTS = IP * 4;   // 16-byte pieces of a row in LDS
     const int h = lane >> 5, l32 = lane & 31;
     const int np = t.np - wp * IP * 32, nq = t.nq - wq * IQ * 32;
-    char* lds = own_lds<T, (IP * IQ * 2048 > 4096 ? IP * IQ * 2048 : 4096)>(ring, wave);
     RowCoef rc[IQ];
 #pragma unroll
     for (int j = 0; j < IQ; ++j) {
       rc[j] = RowCoef{0.f, 0.f, 0.f, -1};
       if (j * 32 + l32 < nq) rc[j] = rows[t.q0 + (wq * IQ + j) * 32 + l32];
     }
-    auto fill = [&](auto Capped) __attribute__((always_inline)) {
-      each(std::make_integer_sequence<int, IP * IQ>{}, [&](auto B_) __attribute__((always_inline)) {
-        constexpr int i = decltype(B_)::value / IQ, j = decltype(B_)::value % IQ;
+    auto fill = [&](auto J_, auto Capped) __attribute__((always_inline)) {
+      constexpr int j = decltype(J_)::value;
+      each(std::make_integer_sequence<int, IP>{}, [&](auto I_) __attribute__((always_inline)) {
+        constexpr int i = decltype(I_)::value;
         // the label among this block's entries
         const int label = rc[j].label < 0 ? -1 : rc[j].label - v0 - t.p0 - (wp * IP + i) * 32 - h * 4;
         const bool here = __any(label >= 0 && label < 32);
@@ -515,20 +509,22 @@ struct GradEpi {
         }
       });
     };
-    if (cap > 0.f) fill(std::true_type{});
-    else fill(std::false_type{});
-    // piece x of a row q of LDS to the row's place: lanes of a store take SLOTS pieces each of 64 / SLOTS rows
+    // 32 rows at a time, by turns in two parts of the ring: lanes of a store take SLOTS pieces each of 64 / SLOTS rows
     const int s16 = lane % SLOTS, q0 = lane / SLOTS;
+    const uint32_t off = s16 * 8 < np ? (uint32_t)((q0 * ldz + s16 * 8) * 2) : kOOB;
+    const uint32_t step = (uint32_t)(64 / SLOTS * ldz * 2);
+    each(std::make_integer_sequence<int, IQ>{}, [&](auto J_) __attribute__((always_inline)) {
+      constexpr int j = decltype(J_)::value;
+      if (cap > 0.f) fill(J_, std::true_type{});
+      else fill(J_, std::false_type{});
 #pragma unroll
-    for (int p = 0; p < PL; ++p) {
-      if (p) wave_lds_sync();
-#pragma unroll
-      for (int j = 0; j < IQ; ++j)
+      for (int p = 0; p < PL; ++p) {
+        char* lds = ring_part<T, PL, IP * 2048, T::NW * 2>(ring, wave * 2 + ((j * PL + p) & 1));
 #pragma unroll
         for (int i = 0; i < IP; ++i)
 #pragma unroll
           for (int g = 0; g < 4; ++g) {
-            const int q = j * 32 + l32, slot = (i * 4 + g) ^ (q & (SLOTS - 1));
+            const int slot = (i * 4 + g) ^ (l32 & (SLOTS - 1));
             uint2 w;
             if constexpr (PL == 1) {
               w = make_uint2(pack2(acc[i][j][4 * g], acc[i][j][4 * g + 1]), pack2(acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]));
@@ -541,20 +537,19 @@ struct GradEpi {
 #pragma unroll
               for (int e = 0; e < 4; ++e) acc[i][j][4 * g + e] = x[e];
             }
-            *reinterpret_cast<uint2*>(lds + q * (IP * 64) + slot * 16 + h * 8) = w;
+            *reinterpret_cast<uint2*>(lds + l32 * (IP * 64) + slot * 16 + h * 8) = w;
           }
-      wave_lds_sync();
-      // (rows up to 2^21 elements apart, at most 64 of them)
-      const rsrc_t out = make_rsrc(dz + p * plane + ((int64_t)t.q0 + wq * IQ * 32) * ldz + t.p0 + wp * IP * 32);
-      const uint32_t off = s16 * 8 < np ? (uint32_t)((q0 * ldz + s16 * 8) * 2) : kOOB;
-      const uint32_t step = (uint32_t)(64 / SLOTS * ldz * 2);
+        wave_lds_sync();
+        // (rows up to 2^21 elements apart, 32 of them)
+        const rsrc_t out = make_rsrc(dz + p * plane + ((int64_t)t.q0 + (wq * IQ + j) * 32) * ldz + t.p0 + wp * IP * 32);
 #pragma unroll
-      for (int u = 0; u < IQ * 32 * SLOTS / 64; ++u) {
-        const int q = u * (64 / SLOTS) + q0;
-        const au32x4 v = *reinterpret_cast<const au32x4*>(lds + q * (IP * 64) + (s16 ^ (q & (SLOTS - 1))) * 16);
-        __builtin_amdgcn_raw_buffer_store_b128(v, out, q < nq ? off + u * step : kOOB, 0, 0);
+        for (int u = 0; u < 32 * SLOTS / 64; ++u) {
+          const int q = u * (64 / SLOTS) + q0;
+          const au32x4 v = *reinterpret_cast<const au32x4*>(lds + q * (IP * 64) + (s16 ^ (q & (SLOTS - 1))) * 16);
+          __builtin_amdgcn_raw_buffer_store_b128(v, out, j * 32 + q < nq ? off + u * step : kOOB, 0, 0);
+        }
       }
-    }
+    });
   }
 };
 
@@ -608,7 +603,7 @@ struct PartEpi {
   int64_t rows, ld;
   int add;
   template <class Acc>
-  __device__ __forceinline__ void operator()(const TilePlace& t, Acc& acc, char* const (&)[4], int lane, int, int wp, int wq) const {
+  __device__ __forceinline__ void operator()(const TilePlace& t, Acc& acc, const Ring&, int lane, int, int wp, int wq) const {
     const int np = t.np - wp * T::IP * 32, nq = t.nq - wq * T::IQ * 32, h4 = (lane >> 5) * 4, l32 = lane & 31;
     float* o = out + ((int64_t)t.split * rows + t.p0 + wp * T::IP * 32) * ld + t.q0 + wq * T::IQ * 32;
     auto store = [&](auto Add) __attribute__((always_inline)) {
@@ -662,7 +657,7 @@ struct HeadEpi {
   static constexpr int ROWS = ROWS_R;
   HeadGrad g;
   template <class Acc>
-  __device__ __forceinline__ void operator()(const TilePlace& t, Acc& acc, char* const (&)[4], int lane, int, int wp, int wq) const {
+  __device__ __forceinline__ void operator()(const TilePlace& t, Acc& acc, const Ring&, int lane, int, int wp, int wq) const {
     const int np = t.np - wp * T::IP * 32, nq = (int)min((int64_t)t.nq, g.K - t.q0) - wq * T::IQ * 32;
     const int h4 = (lane >> 5) * 4, l32 = lane & 31;
     const int64_t org = (int64_t)(t.p0 + wp * T::IP * 32) * g.K + t.q0 + wq * T::IQ * 32;
@@ -872,6 +867,7 @@ TilesPlan tiles_plan(const VocabArgs& a, bool bwd) {
   p.pz = a.M * p.ldz;
   p.dx = a.M <= kFew && a.bf16 ? Choice{FEW, few_parts(a.K, p.piece)} : choose(a.M, a.K, p.piece, p.PL, true);
   p.dw = choose(p.piece, a.K, a.M, p.PL, true);
+
   p.flag = take(a.M);
   p.weight = take(a.M * 8);
   p.at = take(a.M * 4);
@@ -947,7 +943,7 @@ struct Tiles {
   template <class T>
   hipError_t stats(const Operand& x, const Operand& w, int64_t v0, int64_t n) const {
     const Entries en{at<int>(p.off), at<uint32_t>(p.list), (int)p.vtiles};
-    const StatEpi<T> e{at<float2>(p.part), a.zt, en, (int)(v0 / T::BP), a.M, a.k, a.cap, a.rcap, kLog2E / a.T};
+    const StatEpi<T, PL> e{at<float2>(p.part), a.zt, en, (int)(v0 / T::BP), a.M, a.k, a.cap, a.rcap, kLog2E / a.T};
     return product<T, PL, true, true>(w, x, n, a.M, a.K, nullptr, 1, e, s);
   }
   template <class T>
@@ -971,7 +967,8 @@ struct Tiles {
       return hipGetLastError();
     }
     if (g.dw) return product<T, PL, false, false>(dz, x, n, p.Kp, a.M, rows, 1, HeadEpi<T, false>{g}, s);
-    return product<T, PL, false, false>(dz, x, n, p.Kp, a.M, rows, 1, HeadEpi<T, true>{g}, s);
+    using U = std::conditional_t<PL == 1 && std::is_same_v<T, Big>, Half, T>;
+    return product<U, PL, false, false>(dz, x, n, p.Kp, a.M, rows, 1, HeadEpi<U, true>{g}, s);
   }
 
   hipError_t fwd() const {
