@@ -508,8 +508,9 @@ struct VocabArgs {
 size_t vocab_ws_bytes(const VocabArgs& a, bool bwd);
 hipError_t vocab_fwd_launch(const VocabArgs& a, void* ws, hipStream_t stream);
 hipError_t vocab_bwd_launch(const VocabArgs& a, void* ws, hipStream_t stream);
-// Those of bf16 operands, and of fp32 operands of more than a few rows: logits in accumulators only.
-bool vocab_tiles_ok(const VocabArgs& a);
+// Those of bf16 operands, and of fp32 operands of more than a few rows (vocab_tiles_ok): logits in
+// accumulators only.
+bool vocab_tiles_ok(const VocabArgs& a, bool bwd);
 size_t vocab_tiles_ws_bytes(const VocabArgs& a, bool bwd);
 hipError_t vocab_tiles_fwd(const VocabArgs& a, void* ws, hipStream_t stream);
 hipError_t vocab_tiles_bwd(const VocabArgs& a, void* ws, hipStream_t stream);

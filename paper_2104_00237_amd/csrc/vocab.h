@@ -11,16 +11,9 @@
 
 namespace opfuse {
 
-// A running maximum and the sum of exponentials below it.  m = -infinity: nothing yet, or logits of
-// -infinity only; a NaN logit makes the sum NaN (a maximum alone would pass over it).
-struct Stat {
-  float m, s;
-};
+// Statistics are a maximum and the sum of exponentials below it.  A maximum of -infinity: nothing yet, or
+// logits of -infinity only; a NaN logit makes the sum NaN (a maximum alone would pass over it).
 __device__ __forceinline__ float stat_shift(float m) { return m == -INFINITY ? 0.f : m; }
-__device__ __forceinline__ Stat stat_join(Stat a, Stat b) {
-  const float m = fmaxf(a.m, b.m), t = stat_shift(m);
-  return Stat{m, __fadd_rn(__fmul_rn(a.s, expf(a.m - t)), __fmul_rn(b.s, expf(b.m - t)))};
-}
 __device__ __forceinline__ float wave_sum(float v) {
 #pragma unroll
   for (int d = 32; d > 0; d >>= 1) v = __fadd_rn(v, __shfl_xor(v, d));
@@ -45,6 +38,9 @@ __device__ __forceinline__ float vocab_tanh(float x) {
   p = __fmaf_rn(p, u, 1.f), q = __fmaf_rn(q, u, 1.f);
   return __fmul_rn(__fmul_rn(x, p), __builtin_amdgcn_rcpf(q));
 }
+// In full precision, for fp32 operands: a relative error of 1e-7 in a logit of 10 is one of 1e-6 in its
+// probability.
+__device__ __forceinline__ float vocab_cap_exact(float s, float cap) { return cap > 0.f ? __fmul_rn(cap, tanhf(__fdiv_rn(s, cap))) : s; }
 __device__ __forceinline__ float vocab_cap(float s, float cap, float rcap) {
   return cap > 0.f ? __fmul_rn(cap, vocab_tanh(__fmul_rn(s, rcap))) : s;
 }
@@ -111,5 +107,8 @@ __device__ __forceinline__ float row_loss(const VocabArgs& a, int64_t row, float
   }
   return a.T * a.T * wave_sum(loss);
 }
+
+// Statistics [parts][M] joined: lse, losses, their mean (vocab_tiles.hip).  sums: 16 bytes a row; done: 0.
+hipError_t vocab_join_launch(const VocabArgs& a, const float2* part, int parts, void* sums, int* done, hipStream_t s);
 
 }  // namespace opfuse

@@ -17,168 +17,165 @@ namespace opfuse {
 namespace {
 
 // ------------------------------------------------------------ rows of a piece
-// A workgroup's statistics of one row, joined in thread order.
-__device__ Stat block_stat(Stat v, Stat* sh) {
-  const int t = threadIdx.x;
-  sh[t] = v;
-  __syncthreads();
-  for (int d = 128; d > 0; d >>= 1) {
-    if (t < d) sh[t] = stat_join(sh[t], sh[t + d]);
-    __syncthreads();
-  }
-  return sh[0];
-}
+// Rows are worked on in chunks of kChunk logits, 16 a thread in registers: few rows alone would not fill
+// the chip (two rows of 22049: 40 us of 53 with a workgroup a row).
+constexpr int kChunk = 4096;
 
-// The piece [v0, v0 + n) of every row: its statistics join the row's, and the logits of the row's
-// entries in it are kept.
-__global__ __launch_bounds__(256) void vocab_stats_kernel(VocabArgs a, const float* __restrict__ z, int64_t ldz,
-                                                          int64_t v0, int n, Stat* stat) {
-  __shared__ Stat sh[256];
+struct Chunk {
+  float v[16];
+  // logits [from, n) of a row; what lies past n is `fill`
+  __device__ __forceinline__ void load(const float* s, int from, int n, float fill) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int i = from + (u * 256 + (int)threadIdx.x) * 4;
+      const float4 x = i < n ? ld4(s + i) : make_float4(fill, fill, fill, fill);   // (rows are padded to 4)
+      v[4 * u] = x.x, v[4 * u + 1] = i + 1 < n ? x.y : fill, v[4 * u + 2] = i + 2 < n ? x.z : fill,
+          v[4 * u + 3] = i + 3 < n ? x.w : fill;
+    }
+  }
+};
+
+// Statistics (a maximum of the logits, and the sum of exp((z - maximum) / T)) of a chunk of one row of
+// the piece [v0, v0 + n), and the logits of the row's entries in it.
+__global__ __launch_bounds__(256) void vocab_stats_kernel(VocabArgs a, const float* __restrict__ z, int64_t ldz, int64_t v0, int n,
+                                                          float2* part, int* done) {
+  __shared__ float red[2][4];
   const int64_t row = blockIdx.x;
+  const int t = threadIdx.x, from = blockIdx.y * kChunk;
   const float* s = z + row * ldz;
+  if (v0 == 0 && from == 0 && row == 0 && t == 0) *done = 0;
+  Chunk c;
+  c.load(s, from, n, -INFINITY);
   float m = -INFINITY;
-  for (int v = threadIdx.x; v < n; v += 256) m = fmaxf(m, __fdiv_rn(vocab_cap(s[v], a.cap, a.rcap), a.T));
+#pragma unroll
+  for (int u = 0; u < 16; ++u) {
+    // (what lies past the end stays -infinity: a cap would make it a logit)
+    if (c.v[u] != -INFINITY || from + (u / 4 * 256 + t) * 4 + u % 4 < n) c.v[u] = vocab_cap_exact(c.v[u], a.cap);
+    m = fmaxf(m, c.v[u]);
+  }
+  m = wave_max(m);
+  if ((t & 63) == 0) red[0][t >> 6] = m;
+  __syncthreads();
+  m = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
   const float shift = stat_shift(m);
   float sum = 0.f;
-  for (int v = threadIdx.x; v < n; v += 256)
-    sum = __fadd_rn(sum, expf(__fdiv_rn(vocab_cap(s[v], a.cap, a.rcap), a.T) - shift));
-  const Stat mine = block_stat(Stat{m, sum}, sh);
-  if (threadIdx.x == 0) stat[row] = v0 == 0 ? mine : stat_join(stat[row], mine);
-  for (int j = threadIdx.x; j < a.k; j += 256) {
-    const int64_t i = row * a.k + j, id = a.ids[i];
-    if (id >= v0 && id < v0 + n) a.zt[i] = vocab_cap(s[id - v0], a.cap, a.rcap);
-    else if (v0 == 0 && (id < 0 || id >= a.V)) a.zt[i] = 0.f;
-  }
-}
-
-// A wavefront per row: lse and loss from the statistics; counts[row] for the mean.
-__global__ __launch_bounds__(256) void vocab_loss_kernel(VocabArgs a, const Stat* stat, float* counts) {
-  const int lane = threadIdx.x & 63;
-  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (row >= a.M) return;
-  const Stat s = stat[row];
-  const float lse = __fadd_rn(s.m, logf(s.s));
-  bool c;
-  const float loss = row_loss(a, row, lse, lane, &c);
-  if (lane == 0) {
-    a.lse[row] = lse;
-    a.loss[row] = loss;
-    counts[row] = c ? 1.f : 0.f;
-  }
-}
-
-// Sum of the rows' losses over the number that count, in float64 and one order.
-__global__ __launch_bounds__(1024) void vocab_mean_kernel(const float* loss, const float* counts, int64_t M, float* mean) {
-  __shared__ double sh[2][1024];
-  const int t = threadIdx.x;
-  double l = 0.0, c = 0.0;
-  for (int64_t i = t; i < M; i += 1024) l += (double)loss[i], c += (double)counts[i];
-  sh[0][t] = l, sh[1][t] = c;
+#pragma unroll
+  for (int u = 0; u < 16; ++u) sum = __fadd_rn(sum, expf(__fdiv_rn(c.v[u] - shift, a.T)));
+  sum = wave_sum(sum);
+  if ((t & 63) == 0) red[1][t >> 6] = sum;
   __syncthreads();
-  for (int d = 512; d > 0; d >>= 1) {
-    if (t < d) sh[0][t] += sh[0][t + d], sh[1][t] += sh[1][t + d];
-    __syncthreads();
+  if (t == 0) part[(int64_t)blockIdx.y * a.M + row] = make_float2(m, (red[1][0] + red[1][1]) + (red[1][2] + red[1][3]));
+  const int end = min(n, from + kChunk);
+  for (int j = t; j < a.k; j += 256) {
+    const int64_t i = row * a.k + j, id = a.ids[i];
+    if (id >= v0 + from && id < v0 + end) a.zt[i] = vocab_cap_exact(s[id - v0], a.cap);
+    else if (v0 == 0 && from == 0 && (id < 0 || id >= a.V)) a.zt[i] = 0.f;
   }
-  if (t == 0) *mean = (float)(sh[0][0] / fmax(sh[1][0], 1.0));
 }
 
 // ------------------------------------------------------------------- backward
-// What scales a row's gradient: g T for its targets; g T (1 + 2 c lse) for its probabilities.
-// Without given gradients g is 1 / (rows that count), which vocab_scale_kernel finds from counts.
-__global__ __launch_bounds__(256) void vocab_coef_kernel(VocabArgs a, float2* coef, float* counts) {
-  const int lane = threadIdx.x & 63;
-  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (row >= a.M) return;
-  const RowTarget r = row_target(a, row, lane);
-  if (lane) return;
-  // (a row that does not count has no gradient, whatever its g)
-  const float g = r.counts && !r.bad ? (a.dloss ? a.dloss[row] : 1.f) * a.T : 0.f;
-  coef[row] = make_float2(g, r.counts && !r.bad ? __fmul_rn(g, __fmaf_rn(2.f * a.z_loss, a.lse[row], 1.f)) : 0.f);
-  counts[row] = r.counts ? 1.f : 0.f;
-}
-
-__global__ __launch_bounds__(1024) void vocab_scale_kernel(const float* counts, int64_t M, float* scale) {
-  __shared__ double sh[1024];
+// A workgroup a row: what scales its gradient (g T for its targets; g T (1 + 2 c lse) for its
+// probabilities; without given gradients g is 1 here, and 1 / (rows that count) where it is used), and its
+// X for the products: zeros for a row that gets no gradient, so that nothing it holds (a NaN times
+// its zero gradient, too) reaches dW.
+__global__ __launch_bounds__(256) void vocab_prepare_kernel(VocabArgs a, float2* coef, float* counts, float* x) {
+  __shared__ int on;
   const int t = threadIdx.x;
-  double c = 0.0;
-  for (int64_t i = t; i < M; i += 1024) c += (double)counts[i];
-  sh[t] = c;
-  __syncthreads();
-  for (int d = 512; d > 0; d >>= 1) {
-    if (t < d) sh[t] += sh[t + d];
-    __syncthreads();
+  const int64_t row = blockIdx.x;
+  if (t < 64) {
+    const RowTarget r = row_target(a, row, t);
+    if (t == 0) {
+      const bool live = r.counts && !r.bad;
+      const float g = live ? (a.dloss ? a.dloss[row] : 1.f) * a.T : 0.f;
+      coef[row] = make_float2(g, live ? __fmul_rn(g, __fmaf_rn(2.f * a.z_loss, a.lse[row], 1.f)) : 0.f);
+      counts[row] = r.counts ? 1.f : 0.f;
+      on = live;
+    }
   }
-  if (t == 0) *scale = (float)(1.0 / fmax(sh[0], 1.0));
+  __syncthreads();
+  const float* src = (const float*)a.x + row * a.ldx;
+  for (int64_t c = t; c < a.K; c += 256) x[row * a.K + c] = on ? src[c] : 0.f;
 }
 
-// The gradient of a row's logits, in place of them.  An entry's place is written by its first entry
-// with the weights of all that name it; its logit is taken before the row is overwritten.
+// The gradient of a chunk of a row's logits, in place of them.  An entry's place is written by its first
+// entry with the weights of all that name it; its logit is taken before the row is overwritten.
 __global__ __launch_bounds__(256) void vocab_grad_kernel(VocabArgs a, float* __restrict__ z, int64_t ldz, int64_t v0, int n,
-                                                         const float2* coef, const float* scale) {
+                                                         const float2* coef, const float* counts) {
   constexpr int EACH = kTopMax / 256;
+  __shared__ float red[4];
   const int64_t row = blockIdx.x;
+  const int t = threadIdx.x, from = blockIdx.y * kChunk, end = min(n, from + kChunk);
   float* s = z + row * ldz;
   const float2 c = coef[row];
   if (c.x == 0.f && c.y == 0.f) {
-    for (int v = threadIdx.x; v < n; v += 256) s[v] = 0.f;
+    for (int v = from + t; v < end; v += 256) s[v] = 0.f;
     return;
   }
-  const float g = scale ? *scale : 1.f, lse = a.lse[row];
-  const float ct = __fmul_rn(c.x, g), cp = __fmul_rn(c.y, g);
+  float g = 1.f;
+  if (a.dloss == nullptr) {   // (whole numbers: exact in any order)
+    float count = 0.f;
+    for (int64_t i = t; i < a.M; i += 256) count += counts[i];
+    count = wave_sum(count);
+    if ((t & 63) == 0) red[t >> 6] = count;
+    __syncthreads();
+    g = 1.f / fmaxf(red[0] + red[1] + red[2] + red[3], 1.f);
+  }
+  const float lse = a.lse[row], ct = __fmul_rn(c.x, g), cp = __fmul_rn(c.y, g);
   auto grad = [&](float logit, float q) {
-    const float zc = vocab_cap(logit, a.cap, a.rcap);
-    const float p = expf(__fdiv_rn(zc, a.T) - lse);
+    const float zc = vocab_cap_exact(logit, a.cap);
+    const float p = expf(__fsub_rn(__fdiv_rn(zc, a.T), lse));
     float d = __fmaf_rn(cp, p, -__fmul_rn(ct, q));
     if (a.cap > 0.f) {
-      const float r = __fmul_rn(zc, a.rcap);
+      const float r = zc / a.cap;
       d = __fmul_rn(d, __fmaf_rn(-r, r, 1.f));
     }
     return d;
   };
-  const RowTarget r = row_target(a, row, threadIdx.x & 63);
   const int64_t at = row * a.k;
   int where[EACH];
   float d[EACH];
+  if (a.teacher == nullptr) {
+    where[0] = -1;
+    if (t == 0) {
+      const int64_t id = a.ids[row] - v0;
+      if (id >= from && id < end) where[0] = (int)id, d[0] = grad(s[id], 1.f);
+    }
 #pragma unroll
-  for (int u = 0; u < EACH; ++u) {
-    where[u] = -1;
-    const int j = threadIdx.x + u * 256;
-    if (j >= a.k) continue;
-    const int64_t id = a.ids[at + j];
-    if (id < v0 || id >= v0 + n) continue;
-    float q = a.teacher ? 0.f : 1.f;
-    bool first = true;
-    if (a.teacher) {
+    for (int u = 1; u < EACH; ++u) where[u] = -1;
+  } else {
+    const RowTarget r = row_target(a, row, t & 63);
+#pragma unroll
+    for (int u = 0; u < EACH; ++u) {
+      where[u] = -1;
+      const int j = t + u * 256;
+      if (j >= a.k) continue;
+      const int64_t id = a.ids[at + j];
+      if (id < v0 + from || id >= v0 + end) continue;
+      float q = 0.f;
+      bool first = true;
       for (int i = 0; i < a.k; ++i) {
         if (a.ids[at + i] != id) continue;
-        if (i < j) first = false;
+        first &= i >= j;
         q = __fadd_rn(q, r.weight(teacher_logit(a, at + i)));
       }
+      if (!first) continue;
+      where[u] = (int)(id - v0);
+      d[u] = grad(s[id - v0], q);
     }
-    if (!first) continue;
-    where[u] = (int)(id - v0);
-    d[u] = grad(s[id - v0], q);
   }
+  Chunk k;
+  k.load(s, from, n, 0.f);
   __syncthreads();
-  for (int v = threadIdx.x; v < n; v += 256) s[v] = grad(s[v], 0.f);
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const int i = from + (u * 256 + t) * 4;
+    if (i < n) st4(s + i, make_float4(grad(k.v[4 * u], 0.f), grad(k.v[4 * u + 1], 0.f), grad(k.v[4 * u + 2], 0.f), grad(k.v[4 * u + 3], 0.f)));
+  }
   __syncthreads();
 #pragma unroll
   for (int u = 0; u < EACH; ++u)
     if (where[u] >= 0) s[where[u]] = d[u];
 }
-
-// X for the backward's products: rows that get no gradient are zeros there, so that nothing they hold
-// (a NaN times their zero gradient, too) reaches dW.
-__global__ __launch_bounds__(256) void vocab_rows_kernel(const float* x, int64_t ldx, const float2* coef, float* dst, int64_t M,
-                                                         int64_t K) {
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < M * K; i += (int64_t)gridDim.x * 256) {
-    const int64_t r = i / K;
-    const float2 c = coef[r];
-    dst[i] = c.x == 0.f && c.y == 0.f ? 0.f : x[r * ldx + (i - r * K)];
-  }
-}
-
-int store_grid(int64_t n) { return (int)std::min<int64_t>(4096, std::max<int64_t>(1, (n + 255) / 256)); }
 
 // ---------------------------------------------------------------------- pieces
 int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
@@ -192,14 +189,15 @@ int64_t piece_of(const VocabArgs& a) {
 }
 
 struct Plan {
-  int64_t piece, ldz;
-  size_t z, stat, counts, coef, scale, x, gemm, total;   // offsets; total: bytes
+  int64_t piece, ldz, chunks;   // chunks: of a piece
+  size_t z, part, sums, done, counts, coef, x, gemm, total;   // offsets; total: bytes
 };
 
 Plan plan_of(const VocabArgs& a, bool bwd) {
   Plan p{};
   p.piece = piece_of(a);
   p.ldz = up(p.piece, 4);
+  p.chunks = (p.piece + kChunk - 1) / kChunk;
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t here = at;
@@ -207,20 +205,23 @@ Plan plan_of(const VocabArgs& a, bool bwd) {
     return here;
   };
   p.z = take((size_t)a.M * p.ldz * 4);
-  p.stat = take((size_t)a.M * 8);
-  p.coef = p.stat;
-  p.counts = take((size_t)a.M * 4);
-  p.scale = take(4);
-  auto bytes = [&](int kind, int64_t P, int64_t Q, int64_t R) {
-    return gemm_workspace_bytes(kind, (int)P, (int)Q, (int)R);
-  };
   size_t g = 0;
   for (int64_t n : {p.piece, a.V % p.piece ? a.V % p.piece : p.piece}) {
-    g = std::max(g, bytes(EPI_FWD, a.M, n, a.K));
-    if (bwd) g = std::max({g, bytes(EPI_DGRAD, a.M, a.K, n), bytes(EPI_WGRAD, n, a.K, a.M)});
+    g = std::max(g, gemm_workspace_bytes(EPI_FWD, (int)a.M, (int)n, (int)a.K));
+    if (bwd)
+      g = std::max({g, gemm_workspace_bytes(EPI_DGRAD, (int)a.M, (int)a.K, (int)n),
+                    gemm_workspace_bytes(EPI_WGRAD, (int)n, (int)a.K, (int)a.M)});
   }
-  if (bwd) p.x = take((size_t)a.M * a.K * 4);
   p.gemm = take(g);
+  if (bwd) {
+    p.counts = take((size_t)a.M * 4);
+    p.coef = take((size_t)a.M * 8);
+    p.x = take((size_t)a.M * a.K * 4);
+  } else {
+    p.part = take((size_t)((a.V + p.piece - 1) / p.piece * p.chunks) * a.M * 8);
+    p.sums = take((size_t)a.M * 16);
+    p.done = take(4);
+  }
   p.total = at;
   return p;
 }
@@ -250,6 +251,7 @@ struct Pieces {
   hipError_t product(int kind, const GemmProblem& pr, const EpiArgs& ea) const {
     return gemm_launch(kind, pr, ea, ws + p.gemm, s);
   }
+  dim3 rows(int64_t n) const { return dim3((unsigned)a.M, (unsigned)((n + kChunk - 1) / kChunk)); }
   const float* w(int64_t v0) const { return a.W.w + v0 * a.K; }
   hipError_t logits(const float* x, int64_t ldx, int64_t v0, int64_t n) const {
     const GemmProblem pr{x, ldx, 1, w(v0), a.K, 1, (int)a.M, (int)n, (int)a.K};
@@ -268,45 +270,39 @@ struct Pieces {
 }  // namespace
 
 size_t vocab_ws_bytes(const VocabArgs& a, bool bwd) {
-  return vocab_tiles_ok(a) ? vocab_tiles_ws_bytes(a, bwd) : plan_of(a, bwd).total;
+  return vocab_tiles_ok(a, bwd) ? vocab_tiles_ws_bytes(a, bwd) : plan_of(a, bwd).total;
 }
 
 hipError_t vocab_fwd_launch(const VocabArgs& a, void* ws, hipStream_t s) {
-  if (vocab_tiles_ok(a)) return vocab_tiles_fwd(a, ws, s);
+  if (vocab_tiles_ok(a, false)) return vocab_tiles_fwd(a, ws, s);
   const Pieces g{a, plan_of(a, false), (char*)ws, s};
-  Stat* stat = (Stat*)(g.ws + g.p.stat);
-  float* counts = (float*)(g.ws + g.p.counts);
+  float2* part = (float2*)(g.ws + g.p.part);
+  int* done = (int*)(g.ws + g.p.done);
+  int64_t parts = 0;
   for (int64_t v0 = 0; v0 < a.V; v0 += g.p.piece) {
     const int64_t n = std::min(g.p.piece, a.V - v0);
     TRY(g.logits((const float*)a.x, a.ldx, v0, n));
-    hipLaunchKernelGGL(vocab_stats_kernel, dim3((unsigned)a.M), dim3(256), 0, s, a, g.z(), g.p.ldz, v0, (int)n, stat);
+    const dim3 grid = g.rows(n);
+    hipLaunchKernelGGL(vocab_stats_kernel, grid, dim3(256), 0, s, a, g.z(), g.p.ldz, v0, (int)n, part + parts * a.M, done);
     TRY(hipGetLastError());
+    parts += grid.y;
   }
-  hipLaunchKernelGGL(vocab_loss_kernel, dim3((unsigned)((a.M + 3) / 4)), dim3(256), 0, s, a, stat, counts);
-  TRY(hipGetLastError());
-  if (a.mean) hipLaunchKernelGGL(vocab_mean_kernel, dim3(1), dim3(1024), 0, s, a.loss, counts, a.M, a.mean);
-  return hipGetLastError();
+  return vocab_join_launch(a, part, (int)parts, g.ws + g.p.sums, done, s);
 }
 
 hipError_t vocab_bwd_launch(const VocabArgs& a, void* ws, hipStream_t s) {
-  if (vocab_tiles_ok(a)) return vocab_tiles_bwd(a, ws, s);
+  if (vocab_tiles_ok(a, true)) return vocab_tiles_bwd(a, ws, s);
   const Pieces g{a, plan_of(a, true), (char*)ws, s};
   const Plan& p = g.p;
   float2* coef = (float2*)(g.ws + p.coef);
-  float* counts = (float*)(g.ws + p.counts);
-  float* scale = a.dloss ? nullptr : (float*)(g.ws + p.scale);
-  hipLaunchKernelGGL(vocab_coef_kernel, dim3((unsigned)((a.M + 3) / 4)), dim3(256), 0, s, a, coef, counts);
-  TRY(hipGetLastError());
-  if (scale) hipLaunchKernelGGL(vocab_scale_kernel, dim3(1), dim3(1024), 0, s, counts, a.M, scale);
-  TRY(hipGetLastError());
-  float* x = (float*)(g.ws + p.x);
-  hipLaunchKernelGGL(vocab_rows_kernel, dim3(store_grid(a.M * a.K)), dim3(256), 0, s, (const float*)a.x, a.ldx, coef, x, a.M, a.K);
+  float *counts = (float*)(g.ws + p.counts), *x = (float*)(g.ws + p.x);
+  hipLaunchKernelGGL(vocab_prepare_kernel, dim3((unsigned)a.M), dim3(256), 0, s, a, coef, counts, x);
   TRY(hipGetLastError());
   float* dx = (float*)a.dx;
   for (int64_t v0 = 0; v0 < a.V; v0 += p.piece) {
     const int64_t n = std::min(p.piece, a.V - v0);
     TRY(g.logits(x, a.K, v0, n));
-    hipLaunchKernelGGL(vocab_grad_kernel, dim3((unsigned)a.M), dim3(256), 0, s, a, g.z(), p.ldz, v0, (int)n, coef, scale);
+    hipLaunchKernelGGL(vocab_grad_kernel, g.rows(n), dim3(256), 0, s, a, g.z(), p.ldz, v0, (int)n, coef, counts);
     TRY(hipGetLastError());
     if (a.dx) {
       const GemmProblem pr{g.z(), p.ldz, 1, g.w(v0), 1, a.K, (int)a.M, (int)a.K, (int)n};

@@ -394,8 +394,10 @@ __device__ __forceinline__ char* ring_part(const Ring& ring, int i) {
   constexpr int EACH = kRingBytes<T, PL> / BYTES;
   static_assert(EACH * kRingArrays<T, PL> >= COUNT, "parts of the ring");
   uint32_t a = ring.at[0];
+  if constexpr (COUNT > EACH) {
 #pragma unroll
-  for (int r = 1; r < kRingArrays<T, PL>; ++r) a = i / EACH == r ? ring.at[r] : a;
+    for (int r = 1; r < kRingArrays<T, PL>; ++r) a = i / EACH == r ? ring.at[r] : a;
+  }
   return (char*)(lds_char*)(uintptr_t)(a + (uint32_t)(i % EACH) * BYTES);
 }
 

@@ -162,7 +162,7 @@ struct StatEpi {
 #pragma unroll
         for (int j = 0; j < IQ; ++j)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) acc[i][j][r] = vocab_cap(acc[i][j][r], cap, rcap);
+          for (int r = 0; r < 16; ++r) acc[i][j][r] = PL == 1 ? vocab_cap(acc[i][j][r], cap, rcap) : vocab_cap_exact(acc[i][j][r], cap);
     }
     const int tile = tile0 + t.p0 / T::BP, rt = t.q0 / T::BQ;
     const int* off = en.off + (int64_t)rt * (en.vtiles + 1) + tile;
@@ -494,7 +494,8 @@ struct GradEpi {
         const bool here = __any(label >= 0 && label < 32);
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          const float z = vocab_cap(acc[i][j][r], decltype(Capped)::value ? cap : 0.f, rcap);
+          const float c = decltype(Capped)::value ? cap : 0.f;
+          const float z = PL == 1 ? vocab_cap(acc[i][j][r], c, rcap) : vocab_cap_exact(acc[i][j][r], c);
           float d = __fmul_rn(__builtin_amdgcn_exp2f(__fmul_rn(kLog2E, __fmaf_rn(z, rT, -rc[j].lse))), rc[j].cp);
           if (here) d = 8 * (r >> 2) + (r & 3) == label ? __fsub_rn(d, rc[j].ct) : d;
           if constexpr (decltype(Capped)::value) {
@@ -967,7 +968,8 @@ struct Tiles {
       return hipGetLastError();
     }
     if (g.dw) return product<T, PL, false, false>(dz, x, n, p.Kp, a.M, rows, 1, HeadEpi<T, false>{g}, s);
-    using U = std::conditional_t<PL == 1 && std::is_same_v<T, Big>, Half, T>;
+    // an update's memory traffic beside another workgroup's MFMAs: two workgroups a CU
+    using U = std::conditional_t<std::is_same_v<T, Big>, std::conditional_t<PL == 1, Half, Mid>, T>;
     return product<U, PL, false, false>(dz, x, n, p.Kp, a.M, rows, 1, HeadEpi<U, true>{g}, s);
   }
 
@@ -994,13 +996,7 @@ struct Tiles {
           if constexpr (PL == 1) TRY(stats<FewQ>(x, w, v0, n));
       }
     }
-    if (a.M <= kJoinFew)
-      hipLaunchKernelGGL(vocab_join_kernel<1>, dim3((unsigned)a.M), dim3(256), 0, s, a, at<const float2>(p.part), (int)p.vtiles,
-                         at<double2>(p.sums), at<int>(p.done));
-    else
-      hipLaunchKernelGGL(vocab_join_kernel<kJoinRows>, dim3((unsigned)per(a.M, kJoinRows)), dim3(256), 0, s, a,
-                         at<const float2>(p.part), (int)p.vtiles, at<double2>(p.sums), at<int>(p.done));
-    return hipGetLastError();
+    return vocab_join_launch(a, at<const float2>(p.part), (int)p.vtiles, at<double2>(p.sums), at<int>(p.done), s);
   }
 
   hipError_t bwd() const {
@@ -1073,7 +1069,22 @@ struct Tiles {
 
 }  // namespace
 
-bool vocab_tiles_ok(const VocabArgs& a) { return a.bf16 || a.M > 2 * kFew; }
+hipError_t vocab_join_launch(const VocabArgs& a, const float2* part, int parts, void* sums, int* done, hipStream_t s) {
+  if (a.M <= kJoinFew)
+    hipLaunchKernelGGL(vocab_join_kernel<1>, dim3((unsigned)a.M), dim3(256), 0, s, a, part, parts, (double2*)sums, done);
+  else
+    hipLaunchKernelGGL(vocab_join_kernel<kJoinRows>, dim3((unsigned)per(a.M, kJoinRows)), dim3(256), 0, s, a, part, parts,
+                       (double2*)sums, done);
+  return hipGetLastError();
+}
+
+// fp32 W is made into planes first, which few rows do not pay for, and small calls lose to launches.  Pieces of
+// the library's fp32 products / tiles, us: 32768 x 1024 forward 256 rows 139 / 161, 512 244 / 214, backward 128
+// rows 255 / 281, 192 366 / 346, 512 796 / 557; 2048 x 512 forward 1024 rows 40 / 50, 4096 99 / 80, backward 512
+// 62 / 77, 2048 153 / 118.
+bool vocab_tiles_ok(const VocabArgs& a, bool bwd) {
+  return a.bf16 || (bwd ? a.M >= 192 && a.M * a.V >= (1 << 21) : a.M > 400 && a.M * a.V >= (1 << 22));
+}
 
 size_t vocab_tiles_ws_bytes(const VocabArgs& a, bool bwd) { return tiles_plan(a, bwd).total; }
 
