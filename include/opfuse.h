@@ -831,7 +831,7 @@ of_status of_attn_bwd(const of_attn_desc* d, const void* q, const void* k, const
  * V * K <= 2^36, M * K < 2^29, X < 2 GiB.
  */
 typedef struct of_vocab_desc {
-  int64_t M, V, K;        /* rows (<= 2^22), vocabulary (<= 2^21), width (<= 2^20) */
+  int64_t M, V, K;        /* rows (<= 2^22), vocabulary, width (<= 2^20 each) */
   int64_t ldx;            /* row stride of X and dX; 0 means K; <= 2^21 */
   int32_t dtype;          /* of_dtype of X and W */
   int32_t grad_dtype;     /* backward: of_dtype of dX and dW (OF_BF16 only with dtype OF_BF16).  bf16 operands:

@@ -1412,8 +1412,9 @@ of_status check_vocab(const of_vocab_desc* d, bool bwd, VocabArgs* a) {
   memset(a, 0, sizeof(*a));
   a->M = d->M, a->V = d->V, a->K = d->K;
   a->ldx = d->ldx ? d->ldx : d->K;
-  REQUIRE(a->M <= (1LL << 22) && a->V <= (1LL << 21) && a->K <= (1LL << 20), OF_EUNSUPPORTED,
-          "M must be <= 2^22, V <= 2^21, K <= 2^20");
+  // (the entries' sort has a count for each of up to V / 128 tiles in LDS)
+  REQUIRE(a->M <= (1LL << 22) && a->V <= (1LL << 20) && a->K <= (1LL << 20), OF_EUNSUPPORTED,
+          "M must be <= 2^22, V and K <= 2^20");
   // (a launch has fewer than 2^32 threads)
   REQUIRE(a->M * a->V < (1LL << 37) && a->V * a->K <= (1LL << 36), OF_EUNSUPPORTED,
           "M * V must be < 2^37 and V * K <= 2^36");

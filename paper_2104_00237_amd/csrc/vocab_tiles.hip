@@ -139,6 +139,28 @@ __device__ __forceinline__ float2 stat2_join(float2 x, float2 y, float c) {
                                   __fmul_rn(y.y, __builtin_amdgcn_exp2f(__fmul_rn(y.x - s, c)))));
 }
 
+// tanh of a block's logits over their cap.  Trained logits stay well inside it: a wavefront whose 1024 all
+// lie within 0.75 of it takes the short form.
+__device__ __forceinline__ void tanh_block(vacc_t& v, float rcap) {
+  float m = 0.f;
+#pragma unroll
+  for (int r = 0; r < 16; ++r) m = fmaxf(m, fabsf(v[r]));
+  if (__all(m * rcap <= kTanhNear)) {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) v[r] = vocab_tanh_near(__fmul_rn(v[r], rcap));
+  } else {
+#pragma unroll
+    for (int r = 0; r < 16; ++r) v[r] = vocab_tanh(__fmul_rn(v[r], rcap));
+  }
+}
+// A block's logits capped.
+template <int PL>
+__device__ __forceinline__ void cap_block(vacc_t& v, float cap, float rcap) {
+  if constexpr (PL == 1) tanh_block(v, rcap);
+#pragma unroll
+  for (int r = 0; r < 16; ++r) v[r] = PL == 1 ? __fmul_rn(cap, v[r]) : vocab_cap_exact(v[r], cap);
+}
+
 // A = W, B = X: a lane's accumulators are one row's logits, for statistics within the lane.
 template <class T, int PL>
 struct StatEpi {
@@ -157,12 +179,9 @@ struct StatEpi {
     const int h4 = (lane >> 5) * 4, l32 = lane & 31;
     const int np = t.np - wp * IP * 32;   // vocabulary entries from this wavefront's first
     if (cap > 0.f) {
-#pragma unroll
-      for (int i = 0; i < IP; ++i)
-#pragma unroll
-        for (int j = 0; j < IQ; ++j)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) acc[i][j][r] = PL == 1 ? vocab_cap(acc[i][j][r], cap, rcap) : vocab_cap_exact(acc[i][j][r], cap);
+      each(std::make_integer_sequence<int, IP * IQ>{}, [&](auto B_) __attribute__((always_inline)) {
+        cap_block<PL>(acc[decltype(B_)::value / IQ][decltype(B_)::value % IQ], cap, rcap);
+      });
     }
     const int tile = tile0 + t.p0 / T::BP, rt = t.q0 / T::BQ;
     const int* off = en.off + (int64_t)rt * (en.vtiles + 1) + tile;
@@ -360,37 +379,30 @@ __global__ __launch_bounds__(1024) void vocab_index_kernel(VocabArgs a, const ui
                                                            float* scale, RowCoef* rows) {
   __shared__ int waves[16], counted[16];
   const int t = threadIdx.x, lane = t & 63, w = t >> 6;
-  constexpr int U = 8;   // rows of a thread at a time
-  // (neighbouring threads take neighbouring rows' runs: one scan of the workgroup, not one every 1024 rows)
-  const int64_t each = (a.M + 1023) / 1024, r0 = min(a.M, t * each), r1 = min(a.M, r0 + each);
-  auto kinds = [&](int64_t r, int (&f)[U], int (&label)[U]) {
+  constexpr int U = 8;   // 64 rows each at a time
+  // (a run of rows each wavefront: one scan of the workgroup, not one every 1024 rows)
+  const int64_t run = ((a.M + 15) / 16 + 63) / 64 * 64, r0 = min(a.M, w * run), r1 = min(a.M, r0 + run);
+  auto kinds = [&](int64_t r, int (&f)[U], int (&label)[U]) {   // of rows r + 64 u + lane
     if (a.teacher) {
 #pragma unroll
-      for (int u = 0; u < U; ++u) f[u] = r + u < r1 ? flag[r + u] : 0, label[u] = -1;
+      for (int u = 0; u < U; ++u) f[u] = r + u * 64 + lane < r1 ? flag[r + u * 64 + lane] : 0, label[u] = -1;
     } else {
       int64_t y[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) y[u] = r + u < r1 ? a.ids[r + u] : -1;
+      for (int u = 0; u < U; ++u) y[u] = r + u * 64 + lane < r1 ? a.ids[r + u * 64 + lane] : -1;
 #pragma unroll
       for (int u = 0; u < U; ++u) f[u] = y[u] < 0 ? 0 : y[u] >= a.V ? 1 : 2, label[u] = (int)y[u];
     }
   };
   int mine = 0, counts = 0, f[U], label[U];
-  for (int64_t r = r0; r < r1; r += U) {
+  for (int64_t r = r0; r < r1; r += 64 * U) {
     kinds(r, f, label);
 #pragma unroll
-    for (int u = 0; u < U; ++u) mine += f[u] == 2, counts += f[u] != 0;
+    for (int u = 0; u < U; ++u) mine += __popcll(__ballot(f[u] == 2)), counts += __popcll(__ballot(f[u] != 0));
   }
-  int before = mine;
-  for (int d = 1; d < 64; d <<= 1) {
-    const int v = __shfl_up(before, d);
-    if (lane >= d) before += v;
-  }
-  for (int d = 32; d > 0; d >>= 1) counts += __shfl_xor(counts, d);
-  if (lane == 63) waves[w] = before, counted[w] = counts;
+  if (lane == 0) waves[w] = mine, counted[w] = counts;
   __syncthreads();
-  before -= mine;
-  int all = 0, c = 0;
+  int before = 0, all = 0, c = 0;
   for (int i = 0; i < 16; ++i) {
     if (i < w) before += waves[i];
     all += waves[i];
@@ -400,22 +412,26 @@ __global__ __launch_bounds__(1024) void vocab_index_kernel(VocabArgs a, const ui
     *n = all;
     *scale = a.dloss ? 1.f : (float)((double)a.T / (double)max(c, 1));
   }
-  for (int64_t r = r0; r < r1; r += U) {
+  for (int64_t r = r0; r < r1; r += 64 * U) {
     kinds(r, f, label);
     float lse[U], g[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      lse[u] = r + u < r1 ? a.lse[r + u] : 0.f;
-      g[u] = r + u < r1 && a.dloss ? __fmul_rn(a.dloss[r + u], a.T) : 1.f;
+      const int64_t row = r + u * 64 + lane;
+      lse[u] = row < r1 ? a.lse[row] : 0.f;
+      g[u] = row < r1 && a.dloss ? __fmul_rn(a.dloss[row], a.T) : 1.f;
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      if (r + u >= r1) continue;
-      place[r + u] = f[u] == 2 ? before : -1;
+      const int64_t row = r + u * 64 + lane;
+      const uint64_t b = __ballot(f[u] == 2);
+      const int to = before + __popcll(b & ((1ull << lane) - 1));
+      before += __popcll(b);
+      if (row >= r1) continue;
+      place[row] = f[u] == 2 ? to : -1;
       if (f[u] != 2) continue;
-      at[before] = (int)(r + u);
-      rows[before] = RowCoef{lse[u], __fmul_rn(g[u], __fmaf_rn(2.f * a.z_loss, lse[u], 1.f)), g[u], label[u]};
-      ++before;
+      at[to] = (int)row;
+      rows[to] = RowCoef{lse[u], __fmul_rn(g[u], __fmaf_rn(2.f * a.z_loss, lse[u], 1.f)), g[u], label[u]};
     }
   }
 }
@@ -492,17 +508,25 @@ struct GradEpi {
         // the label among this block's entries
         const int label = rc[j].label < 0 ? -1 : rc[j].label - v0 - t.p0 - (wp * IP + i) * 32 - h * 4;
         const bool here = __any(label >= 0 && label < 32);
+        constexpr bool capped = decltype(Capped)::value;
+        // bf16 operands: what is left of the logit is tanh alone, and lse is taken off in units of log2 (its
+        // rounding there, 1e-6 of a probability, is nothing beside bf16's)
+        if constexpr (capped && PL == 1) tanh_block(acc[i][j], rcap);
+        const float c2 = rT * kLog2E * (capped ? cap : 1.f), lse2 = rc[j].lse * kLog2E;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          const float c = decltype(Capped)::value ? cap : 0.f;
-          const float z = PL == 1 ? vocab_cap(acc[i][j][r], c, rcap) : vocab_cap_exact(acc[i][j][r], c);
-          float d = __fmul_rn(__builtin_amdgcn_exp2f(__fmul_rn(kLog2E, __fmaf_rn(z, rT, -rc[j].lse))), rc[j].cp);
-          if (here) d = 8 * (r >> 2) + (r & 3) == label ? __fsub_rn(d, rc[j].ct) : d;
-          if constexpr (decltype(Capped)::value) {
-            const float x = __fmul_rn(z, rcap);
-            d = __fmul_rn(d, __fmaf_rn(-x, x, 1.f));
+          float d, x = 0.f;   // x: the logit over its cap
+          if constexpr (PL == 1) {
+            x = acc[i][j][r];
+            d = __builtin_amdgcn_exp2f(__fmaf_rn(x, c2, -lse2));
+          } else {
+            const float z = vocab_cap_exact(acc[i][j][r], capped ? cap : 0.f);
+            x = __fmul_rn(z, rcap);
+            d = __builtin_amdgcn_exp2f(__fmul_rn(kLog2E, __fmaf_rn(z, rT, -rc[j].lse)));
           }
-          acc[i][j][r] = d;
+          d = __fmul_rn(d, rc[j].cp);
+          if (here) d = 8 * (r >> 2) + (r & 3) == label ? __fsub_rn(d, rc[j].ct) : d;
+          acc[i][j][r] = capped ? __fmul_rn(d, __fmaf_rn(-x, x, 1.f)) : d;
         }
         if (np < IP * 32) {   // the piece's last tile: zeros to the end of its 16-byte pieces
 #pragma unroll

@@ -56,8 +56,8 @@ BAD = [(L.OF_EINVAL, dict(M=0)), (L.OF_EINVAL, dict(V=0)), (L.OF_EINVAL, dict(K=
        (L.OF_EINVAL, dict(softcap=float("nan"))), (L.OF_EUNSUPPORTED, dict(softcap=2.0 ** 41)),
        (L.OF_EINVAL, dict(z_loss=-1e-4)), (L.OF_EINVAL, dict(z_loss=float("inf"))), (L.OF_EINVAL, dict(temperature=-1.0)),
        (L.OF_EUNSUPPORTED, dict(temperature=2.0 ** -41)), (L.OF_EUNSUPPORTED, dict(M=(1 << 22) + 1)),
-       (L.OF_EUNSUPPORTED, dict(V=(1 << 21) + 1)), (L.OF_EUNSUPPORTED, dict(K=(1 << 20) + 1)),
-       (L.OF_EUNSUPPORTED, dict(M=1 << 20, V=1 << 17)), (L.OF_EUNSUPPORTED, dict(V=1 << 21, K=(1 << 15) + 1)),
+       (L.OF_EUNSUPPORTED, dict(V=(1 << 20) + 1)), (L.OF_EUNSUPPORTED, dict(K=(1 << 20) + 1)),
+       (L.OF_EUNSUPPORTED, dict(M=1 << 20, V=1 << 17)), (L.OF_EUNSUPPORTED, dict(V=1 << 20, K=(1 << 16) + 1)),
        (L.OF_EUNSUPPORTED, dict(ldx=(1 << 21) + 1)), (L.OF_EUNSUPPORTED, dict(M=1 << 20, ldx=1 << 10)),
        (L.OF_EUNSUPPORTED, dict(M=1 << 21, topk=1024))]
 
@@ -69,6 +69,19 @@ def test_descriptors(want, kw):
         assert L.of_last_error()
     kind = "distill_bwd" if "topk" in kw else "xent_bwd"
     assert refused(kind, desc(**kw)) == want, L.of_last_error()
+
+
+@pytest.mark.parametrize("kw", [dict(M=1 << 22, V=1000, K=100), dict(M=1, V=1 << 20, K=1 << 16), dict(M=1 << 16, V=1 << 20, K=64),
+                                dict(M=(1 << 20) - 1, V=4096, K=512), dict(M=1, V=1, K=1), dict(M=1 << 21, V=32, K=32, topk=1023),
+                                dict(M=500, V=1 << 20, K=1 << 15)])
+@pytest.mark.parametrize("dtype", [L.OF_F32, L.OF_BF16])
+def test_workspace_of_the_largest(kw, dtype):
+    """Grows with what it holds: X, the entries, a gradient of at most 512 MB and partial sums beside it."""
+    d = desc(dtype=dtype, grad_dtype=dtype, **kw)
+    wide = d.M * d.K * 4
+    for op in (L.OF_VOCAB_FWD, L.OF_VOCAB_BWD):
+        size = L.of_vocab_workspace_size(d, op)
+        assert 0 < size < (1 << 31) + 70 * wide + 24 * d.M * max(d.topk, 1) + 64 * d.V * d.K + d.M * d.V // 8 + (1 << 22), (size, L.of_last_error())
 
 
 def test_workspace_query():

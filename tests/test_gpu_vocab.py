@@ -353,6 +353,12 @@ def test_update(gpu, dtype, M, V, K, k, hyper):
     assert (c.dx == 7.0).all()
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_update_on_large_tiles(gpu, dtype):
+    """The update's tiles are not those of a stored gradient: the same sums all the same."""
+    test_update(gpu, dtype, 1024, 16384, 1024, 0, OPTS[2])
+
+
 @pytest.mark.parametrize("dtype,k", [("f32", 0), ("bf16", 0), ("f32", 5), ("bf16", 5)])
 def test_differences(gpu, dtype, k):
     """dX and dW against differences of the mean loss.
@@ -449,3 +455,111 @@ def test_repeats(gpu):
         for _ in range(3):
             c.fwd(), c.bwd()
             assert all(torch.equal(x, y) for x, y in zip((c.loss, c.lse, c.zt, c.mean, c.dx, c.dw), want))
+
+
+@pytest.mark.parametrize("dtype,M,V,K,k", [("bf16", 3, 1 << 20, 1100, 0), ("f32", 2, 1 << 20, 520, 4), ("bf16", 40000, 60000, 8, 0),
+                                           ("bf16", 2000, 300000, 64, 2)])
+def test_offsets_past_32_bits(gpu, dtype, M, V, K, k):
+    """W of more than 2^31 bytes, more than 2^31 logits, several pieces: rows at both ends against float64."""
+    t, kind, u = TYPES[dtype]
+    g = torch.Generator(device=gpu).manual_seed(4)
+    w = torch.empty(V, K, dtype=t, device=gpu)
+    for a in range(0, V, 1 << 16):
+        w[a:a + (1 << 16)] = (torch.randn(min(1 << 16, V - a), K, generator=g, device=gpu) * 2 / math.sqrt(K)).to(t)
+    x = torch.randn(M, K, generator=g, device=gpu).to(t)
+    ids = torch.randint(0, V, (M, max(k, 1)), generator=g, device=gpu)
+    ids[0, 0], ids[-1, 0] = V - 1, V - 2
+    teacher = torch.randn(M, max(k, 1), generator=g, device=gpu)
+    loss, lse, zt = (torch.full(s, 7.0, device=gpu) for s in ((M,), (M,), (M, max(k, 1))))
+    d = L.OfVocabDesc(M=M, V=V, K=K, dtype=kind, grad_dtype=kind, topk=k)
+    p = L.OfParam(numel=V * K, **{"w" if dtype == "f32" else "w_bf16": w.data_ptr()})
+    ws = torch.empty(max(L.of_vocab_workspace_size(d, op) for op in (0, 1)), dtype=torch.uint8, device=gpu)
+    st = torch.cuda.current_stream().cuda_stream
+    name = "distill" if k else "xent"
+    targets = [ids.data_ptr()] + ([teacher.data_ptr()] if k else [])
+    getattr(L, f"of_vocab_{name}_fwd")(d, x.data_ptr(), p, *targets, loss.data_ptr(), lse.data_ptr(), zt.data_ptr(), None,
+                                       ws.data_ptr(), ws.numel(), st)
+    dloss = torch.zeros(M, device=gpu)
+    rows = torch.tensor(sorted({0, 1, M // 2, M - 1}), device=gpu)
+    dloss[rows] = 1.0
+    dx, dw = torch.full((M, K), 7.0, dtype=t, device=gpu), torch.full((V, K), 7.0, dtype=t, device=gpu)
+    getattr(L, f"of_vocab_{name}_bwd")(d, x.data_ptr(), p, *targets, lse.data_ptr(), zt.data_ptr(), dloss.data_ptr(),
+                                       dx.data_ptr(), dw.data_ptr(), 0, ws.data_ptr(), ws.numel(), st)
+    torch.cuda.synchronize()
+    r = Reference(x[rows], w, ids[rows], teacher[rows] if k else None, dloss=torch.ones(len(rows), device=gpu), u=u)
+    near("lse", lse[rows], r.lse, r.e_lse)
+    near("zt", zt[rows], r.zt, r.e_zt)
+    near("loss", loss[rows], r.loss, r.e_loss)
+    near("dx", dx[rows], r.dx, r.e_dx, u)
+    near("dw", dw, r.dw, r.e_dw, u)
+    assert torch.isfinite(lse).all() and torch.isfinite(loss).all() and torch.isfinite(dx).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_head_of_a_student(gpu, dtype):
+    """As a training step uses them together: LayerNorm's output under one head, the label's loss and the teacher's,
+    one update of the head from both, dX of both back through LayerNorm."""
+    M, V, K, k, lr = 96, 700, 64, 5, 0.5
+    t, kind, u = TYPES[dtype]
+    g = torch.Generator().manual_seed(11)
+    h = torch.randn(M, K, generator=g).to(gpu)
+    gamma, beta = (1 + 0.1 * torch.randn(K, generator=g)).to(gpu), (0.1 * torch.randn(K, generator=g)).to(gpu)
+    w = (torch.randn(V, K, generator=g) * 0.25).to(gpu)
+    shadow = w.bfloat16() if dtype == "bf16" else None
+    labels = torch.randint(0, V, (M, 1), generator=g)
+    labels[::5] = -1
+    ids = torch.stack([torch.randperm(V, generator=g)[:k] for _ in range(M)])
+    teacher = torch.randn(M, k, generator=g)
+    st = torch.cuda.current_stream().cuda_stream
+    x, mean, rstd = torch.empty(M, K, dtype=t, device=gpu), torch.empty(M, device=gpu), torch.empty(M, device=gpu)
+    ln = L.of_layernorm_fwd_bf16 if dtype == "bf16" else L.of_layernorm_fwd
+    ln(h.data_ptr(), M, K, gamma.data_ptr(), beta.data_ptr(), 1e-5, x.data_ptr(), mean.data_ptr(), rstd.data_ptr(), st)
+    head = L.param_of(w, torch.zeros_like(w), w_bf16=shadow)
+    m = torch.zeros_like(w)
+    head.m = m.data_ptr()
+    w0, x0 = (shadow if dtype == "bf16" else w).detach().cpu().clone(), x.detach().cpu()
+    d1 = L.OfVocabDesc(M=M, V=V, K=K, dtype=kind, grad_dtype=L.OF_F32)
+    d2 = L.OfVocabDesc(M=M, V=V, K=K, dtype=kind, grad_dtype=L.OF_F32, topk=k, temperature=2.0)
+    ws = torch.empty(max(L.of_vocab_workspace_size(d, op) for d in (d1, d2) for op in (0, 1)), dtype=torch.uint8, device=gpu)
+    wa = (ws.data_ptr(), ws.numel())
+    new = lambda *s: torch.empty(*s, device=gpu)  # noqa: E731
+    l1, e1, z1, l2, e2, z2 = new(M), new(M), new(M), new(M), new(M), new(M, k)
+    dev = [v.to(gpu) for v in (labels, ids, teacher)]
+    lab, idp, tea = (v.data_ptr() for v in dev)
+    means = new(2)
+    L.of_vocab_xent_fwd(d1, x.data_ptr(), head, lab, l1.data_ptr(), e1.data_ptr(), z1.data_ptr(), means.data_ptr(), *wa, st)
+    L.of_vocab_distill_fwd(d2, x.data_ptr(), head, idp, tea, l2.data_ptr(), e2.data_ptr(), z2.data_ptr(),
+                           means[1:].data_ptr(), *wa, st)
+    dx1, dx2, dw = new(M, K), new(M, K), new(V, K)
+    L.of_vocab_xent_bwd(d1, x.data_ptr(), head, lab, e1.data_ptr(), z1.data_ptr(), None, dx1.data_ptr(), dw.data_ptr(), 0, *wa, st)
+    opt = L.make_opt(dict(kind="sgd", lr=lr, momentum=0.9), 1)
+    L.of_vocab_distill_bwd_fused(d2, x.data_ptr(), head, idp, tea, e2.data_ptr(), z2.data_ptr(), None, dw.data_ptr(), opt,
+                                 dx2.data_ptr(), *wa, st)
+    L.of_add(dx1.data_ptr(), dx2.data_ptr(), M * K, dx1.data_ptr(), st)
+    dh, rows = new(M, K), int(L.of_layernorm_partial_rows(M))
+    dg, db = new(rows, K), new(rows, K)
+    L.of_layernorm_bwd(dx1.data_ptr(), h.data_ptr(), mean.data_ptr(), rstd.data_ptr(), gamma.data_ptr(), None, M, K,
+                       dh.data_ptr(), dg.data_ptr(), db.data_ptr(), st)
+    torch.cuda.synchronize()
+    a = Reference(x0, w0, labels, u=u)
+    b = Reference(x0, w0, ids, teacher, T=2.0, u=u)
+    for i, (r, loss, lse) in enumerate(((a, l1, e1), (b, l2, e2))):
+        near("loss", loss, r.loss, r.e_loss)
+        near("lse", lse, r.lse, r.e_lse)
+        near("mean", means[i], torch.tensor(r.mean, dtype=torch.float64), torch.tensor(r.e_mean, dtype=torch.float64))
+    grad, e_grad = a.dw + b.dw, a.e_dw + b.e_dw + 2.0 ** -23 * (a.dw.abs() + b.dw.abs())
+    near("m", m, grad, e_grad)
+    if dtype == "f32":
+        start = w0.double()
+        near("w", w, start - lr * grad, lr * e_grad + 2.0 ** -23 * (start.abs() + lr * grad.abs()))
+    else:   # the shadow is the new master's rounding
+        assert torch.equal(shadow, w.bfloat16())
+    dx, e_dx = a.dx + b.dx, a.e_dx + b.e_dx + 2.0 ** -24 * (a.dx + b.dx).abs()
+    near("dx", dx1, dx, e_dx)
+    # LayerNorm's backward is linear in dx: its own error at this width is below 2^-16 of its input
+    hd, gd = h.cpu().double(), gamma.cpu().double()
+    hat = (hd - hd.mean(1, keepdim=True)) / torch.sqrt(hd.var(1, unbiased=False, keepdim=True) + 1e-5)
+    rs = 1 / torch.sqrt(hd.var(1, unbiased=False, keepdim=True) + 1e-5)
+    back = lambda v: rs * (v - v.mean(1, keepdim=True) - hat * (v * hat).mean(1, keepdim=True))  # noqa: E731
+    most = rs * (e_dx * gd.abs() + (e_dx * gd.abs()).mean(1, keepdim=True) + hat.abs() * (e_dx * gd.abs() * hat.abs()).mean(1, keepdim=True))
+    near("dh", dh, back(dx * gd), most + 2.0 ** -16 * rs * (dx * gd).abs().amax(1, keepdim=True))
