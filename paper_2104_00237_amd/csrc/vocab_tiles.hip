@@ -1,9 +1,9 @@
 // Vocabulary losses on the bf16 matrix cores: the logits' product ends in the rows' statistics (forward)
 // or in the logits' gradient (backward), so that logits exist in accumulators only.
 //
-// Forward, three launches: the rows' entries sorted by the tile of logits that holds them; the logits'
-// product, whose tiles leave a maximum and a sum of exponentials a row and the entries' logits; the
-// statistics joined, losses and their mean.
+// Forward: distillation's entries sorted by the tile of logits that holds them; the logits' product, whose
+// tiles leave a maximum and a sum of exponentials a row and the entries' logits; the statistics joined,
+// losses and their mean.
 // Backward: the rows that get a gradient, gathered (what others hold is never read, and they cost no
 // work); then per piece of the vocabulary the logits' product again, stored as their gradient in bf16,
 // dX summed over the pieces in fp32, dW (or the update) of the piece's rows; at the end dX rounded and
@@ -165,6 +165,9 @@ __device__ __forceinline__ void cap_block(vacc_t& v, float cap, float rcap) {
 template <class T, int PL>
 struct StatEpi {
   static constexpr int ROWS = ROWS_NONE;
+  const int64_t* labels;   // cross-entropy: found by the tiles themselves; distillation: NULL, entries are sorted
+  int64_t V;
+  int* done;               // the join's count, cleared here for cross-entropy
   float2* part;        // [vtiles][M]
   float* zt;
   Entries en;
@@ -184,8 +187,28 @@ struct StatEpi {
       });
     }
     const int tile = tile0 + t.p0 / T::BP, rt = t.q0 / T::BQ;
-    const int* off = en.off + (int64_t)rt * (en.vtiles + 1) + tile;
-    const int e0 = off[0], e1 = off[1];
+    int e0 = 0, e1 = 0;
+    if (labels) {
+      if (blockIdx.x == 0 && tile0 == 0 && wave == 0 && lane == 0) *done = 0;
+      each(std::make_integer_sequence<int, IQ>{}, [&](auto J_) __attribute__((always_inline)) {
+        constexpr int j = decltype(J_)::value;
+        const int q = (wq * IQ + j) * 32 + l32;
+        const int64_t y = q < t.nq ? labels[t.q0 + q] : -1;
+        if (tile == 0 && wp == 0 && lane < 32 && q < t.nq && (y < 0 || y >= V)) zt[t.q0 + q] = 0.f;
+        const int64_t far = y - ((int64_t)tile * T::BP + wp * IP * 32 + h4);
+        const int label = y >= 0 && y < V && far >= 0 && far < IP * 32 ? (int)far : -1;   // from this lane's first entry
+        each(std::make_integer_sequence<int, IP>{}, [&](auto I_) __attribute__((always_inline)) {
+          constexpr int i = decltype(I_)::value;
+          if (!__any(label >= i * 32 && label < i * 32 + 32)) return;
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            if (i * 32 + 8 * (r >> 2) + (r & 3) == label) zt[t.q0 + q] = acc[i][j][r];
+        });
+      });
+    } else {
+      const int* off = en.off + (int64_t)rt * (en.vtiles + 1) + tile;
+      e0 = off[0], e1 = off[1];
+    }
     if (e1 > e0) {
       const uint32_t* list = en.list + (int64_t)rt * T::BQ * k;
       float* lds = (float*)ring_part<T, PL, 4096, T::NW>(ring, wave);
@@ -593,27 +616,37 @@ template <int PL>
 __global__ __launch_bounds__(256) void vocab_entry_kernel(VocabArgs a, const int* at, const int* n, const RowCoef* rows,
                                                           const float2* weight, int64_t v0, int64_t nv, uint16_t* dz,
                                                           int64_t ldz, int64_t plane) {
-  __shared__ int64_t ids[4][kTopMax];
+  __shared__ __attribute__((aligned(16))) int places[4][kTopMax];   // in the piece, or -1
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int i = blockIdx.x * 4 + w;
   if (i >= *n) return;
   const int64_t row = at[i], first = row * a.k;
-  for (int j = lane; j < a.k; j += 64) ids[w][j] = a.ids[first + j];
+  const int k4 = (a.k + 3) & ~3;
+  for (int j = lane; j < k4; j += 64) {
+    const int64_t id = j < a.k ? a.ids[first + j] : -1;
+    places[w][j] = id >= v0 && id < v0 + nv ? (int)(id - v0) : -1;
+  }
   wave_lds_sync();
   const RowTarget r{weight[row].x, weight[row].y, true, false};
   const RowCoef rc = rows[i];
-  for (int j = lane; j < a.k; j += 64) {
-    const int64_t id = ids[w][j];
-    if (id < v0 || id >= v0 + nv) continue;
-    float q = 0.f;
-    bool lead = true;
-    for (int e = 0; e < a.k; ++e) {
-      if (ids[w][e] != id) continue;
-      lead &= e >= j;
-      q = __fadd_rn(q, r.weight(teacher_logit(a, first + e)));
+  for (int j0 = 0; j0 < a.k; j0 += 64) {
+    const int j = j0 + lane, place = j < a.k ? places[w][j] : -1;
+    if (!__any(place >= 0)) continue;
+    // (entries that name one place twice are rare: four compares an LDS read, weights only where one matches)
+    float q = place >= 0 ? r.weight(teacher_logit(a, first + j)) : 0.f;
+    bool lead = place >= 0;
+    for (int e = 0; e < k4; e += 4) {
+      const int4 p = *reinterpret_cast<const int4*>(&places[w][e]);
+      const int x[4] = {p.x, p.y, p.z, p.w};
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        if (x[u] != place || place < 0 || e + u == j) continue;
+        lead &= e + u > j;
+        q = __fadd_rn(q, r.weight(teacher_logit(a, first + e + u)));
+      }
     }
     if (!lead) continue;
-    uint16_t* d = dz + (int64_t)i * ldz + (id - v0);
+    uint16_t* d = dz + (int64_t)i * ldz + place;
     float x = entry_grad(a, rc, a.zt[first + j], q), y = 0.f;
 #pragma unroll
     for (int p = 0; p < PL; ++p) d[p * plane] = (uint16_t)take_part(x, y);
@@ -818,16 +851,23 @@ struct Choice {
 
 // Time of a product of P x Q tiles over R: rounds of workgroups, each its stages of 32 elements and an
 // epilogue; parts are written and read again.  us, fitted to products of 512 to 32768 rows and columns.
-Choice choose(int64_t P, int64_t Q, int64_t R, int planes, bool split) {
+// few_p, few_q: the 32-wide tiles' rows and columns where they may be taken (bf16): they read operands more often, and
+// are the only ones to fill the chip with a few hundred rows over a small vocabulary (backward of 579 rows over
+// 338 of width 4160: 77 -> 52 us).
+Choice choose(int64_t P, int64_t Q, int64_t R, int planes, bool split, int few_p = 0, int few_q = 0) {
   Choice best{MID, 1};
   double least = 1e300;
-  for (const Shape s : {BIG, MID}) {
-    const int64_t b = s == BIG ? 256 : 128, tiles = per(P, b) * per(Q, b);
+  for (const Shape s : {BIG, MID, FEW}) {
+    if (s == FEW && (!few_p || planes == 3)) continue;
+    const int64_t bp = s == BIG ? 256 : s == MID ? 128 : few_p, bq = s == BIG ? 256 : s == MID ? 128 : few_q;
+    const int64_t tiles = per(P, bp) * per(Q, bq);
     for (int S = 1; S <= (split ? 64 : 1); S += S < 4 ? 1 : S / 2) {
       if (S > 1 && R / S < 128) break;
       const int64_t wg = tiles * S;
-      const double stages = (double)up(per(per(R, 32), S) * (planes == 3 ? 6 : 1), 4);
-      const double one = s == BIG ? stages * 0.85 + 8 : stages * (wg > 256 ? 0.58 : 0.36) + 4;
+      const double stages = (double)up(per(per(R, 32), S) * (planes == 3 ? 6 : 1), s == FEW ? 8 : 4);
+      const double one = s == BIG   ? stages * 0.85 + 8
+                         : s == MID ? stages * (wg > 256 ? 0.58 : 0.36) + 4
+                                    : stages * (wg > 256 ? 0.3 : 0.18) + 4;
       const double time = per(wg, s == BIG ? 256 : 512) * one + (S > 1 ? 2 + (double)P * Q * S * 8 / 4e6 : 0);
       if (time < least) least = time, best = Choice{s, S};
     }
@@ -861,7 +901,7 @@ TilesPlan tiles_plan(const VocabArgs& a, bool bwd) {
     here += (size_t)up(bytes, 256);
     return at;
   };
-  p.logits = a.M <= kFew && a.bf16 ? Choice{FEW, 1} : choose(a.V, a.M, a.K, p.PL, false);
+  p.logits = a.M <= kFew && a.bf16 ? Choice{FEW, 1} : choose(a.V, a.M, a.K, p.PL, false, FewQ::BP, FewQ::BQ);
   p.BP = p.logits.shape == BIG ? 256 : 128;
   p.BQ = p.logits.shape == BIG ? 256 : p.logits.shape == MID ? 128 : 32;
   p.vtiles = per(a.V, p.BP), p.rtiles = per(a.M, p.BQ);
@@ -890,7 +930,7 @@ TilesPlan tiles_plan(const VocabArgs& a, bool bwd) {
   p.w = take(p.pw * p.PL * 2);
   p.ldz = p.piece;
   p.pz = a.M * p.ldz;
-  p.dx = a.M <= kFew && a.bf16 ? Choice{FEW, few_parts(a.K, p.piece)} : choose(a.M, a.K, p.piece, p.PL, true);
+  p.dx = a.M <= kFew && a.bf16 ? Choice{FEW, few_parts(a.K, p.piece)} : choose(a.M, a.K, p.piece, p.PL, true, FewP::BP, FewP::BQ);
   p.dw = choose(p.piece, a.K, a.M, p.PL, true);
 
   p.flag = take(a.M);
@@ -968,7 +1008,7 @@ struct Tiles {
   template <class T>
   hipError_t stats(const Operand& x, const Operand& w, int64_t v0, int64_t n) const {
     const Entries en{at<int>(p.off), at<uint32_t>(p.list), (int)p.vtiles};
-    const StatEpi<T, PL> e{at<float2>(p.part), a.zt, en, (int)(v0 / T::BP), a.M, a.k, a.cap, a.rcap, kLog2E / a.T};
+    const StatEpi<T, PL> e{a.teacher ? nullptr : a.ids, a.V, at<int>(p.done), at<float2>(p.part), a.zt, en, (int)(v0 / T::BP), a.M, a.k, a.cap, a.rcap, kLog2E / a.T};
     return product<T, PL, true, true>(w, x, n, a.M, a.K, nullptr, 1, e, s);
   }
   template <class T>
@@ -1003,10 +1043,12 @@ struct Tiles {
       TRY(gather(a.x, a.ldx, nullptr, nullptr, a.M, at<uint16_t>(p.x), p.px));
       x = Operand{at<uint16_t>(p.x), p.Kp, p.px};
     }
-    switch (p.logits.shape) {
-      case BIG: TRY(sort_entries<Big>()); break;
-      case MID: TRY(sort_entries<Mid>()); break;
-      default: TRY(sort_entries<FewQ>()); break;
+    if (a.teacher) {
+      switch (p.logits.shape) {
+        case BIG: TRY(sort_entries<Big>()); break;
+        case MID: TRY(sort_entries<Mid>()); break;
+        default: TRY(sort_entries<FewQ>()); break;
+      }
     }
     const int64_t piece = copies_w() ? p.copied : a.V;
     for (int64_t v0 = 0; v0 < a.V; v0 += piece) {
