@@ -67,57 +67,92 @@ __device__ __forceinline__ float teacher_logit(const VocabArgs& a, int64_t i) {
   const float t = a.tbf ? __uint_as_float((uint32_t)((const uint16_t*)a.teacher)[i] << 16) : ((const float*)a.teacher)[i];
   return __fdiv_rn(t, a.T);
 }
-__device__ __forceinline__ RowTarget row_target(const VocabArgs& a, int64_t row, int lane) {
-  RowTarget r{0.f, 1.f, false, false};
-  if (a.teacher == nullptr) {
-    const int64_t y = a.ids[row];
-    r.counts = y >= 0;
-    r.bad = y >= a.V;
+
+// A distillation row's entries, the lanes' first E each in registers: f(n, j, has, t) for entry j with its
+// logit over T, n its number in the registers or -1 behind them.
+template <int E>
+struct RowEntries {
+  float t[E];
+  bool has[E], bad[E];
+  __device__ __forceinline__ void load(const VocabArgs& a, int64_t row, int lane) {
+    const int64_t at = row * a.k;
+    int64_t id[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) id[e] = lane + e * 64 < a.k ? a.ids[at + lane + e * 64] : -1;
+#pragma unroll
+    for (int e = 0; e < E; ++e) t[e] = lane + e * 64 < a.k ? teacher_logit(a, at + lane + e * 64) : 0.f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) has[e] = id[e] >= 0, bad[e] = id[e] >= a.V;
+  }
+  template <class F>
+  __device__ __forceinline__ void all(const VocabArgs& a, int64_t row, int lane, F&& f) const {
+#pragma unroll
+    for (int e = 0; e < E; ++e)
+      if (has[e]) f(e, lane + e * 64, bad[e], t[e]);
+    for (int j = lane + E * 64; j < a.k; j += 64) {
+      const int64_t id = a.ids[row * a.k + j];
+      if (id >= 0) f(-1, j, id >= a.V, teacher_logit(a, row * a.k + j));
+    }
+  }
+  __device__ __forceinline__ RowTarget target(const VocabArgs& a, int64_t row, int lane) const {
+    RowTarget r{0.f, 1.f, false, false};
+    float top = -INFINITY;
+    bool past = false, nan = false;
+    all(a, row, lane, [&](int, int, bool b, float x) {
+      past |= b;
+      nan |= x != x;
+      top = fmaxf(top, x);
+    });
+    r.top = wave_max(top);
+    r.bad = __any(past);
+    r.counts = r.top != -INFINITY || __any(nan);
+    r.top = stat_shift(r.top);
+    float total = 0.f;
+    all(a, row, lane, [&](int, int, bool, float x) { total += expf(x - r.top); });
+    total = wave_sum(total);
+    r.total = total == 0.f ? 1.f : total;
     return r;
   }
-  const int64_t at = row * a.k;
-  float top = -INFINITY;
-  bool bad = false, nan = false;
-  for (int j = lane; j < a.k; j += 64) {
-    const int64_t id = a.ids[at + j];
-    if (id < 0) continue;
-    const float t = teacher_logit(a, at + j);
-    bad |= id >= a.V;
-    nan |= t != t;
-    top = fmaxf(top, t);
+};
+constexpr int kRowEntries = 4;   // 256 entries a row without a second load
+
+__device__ __forceinline__ RowTarget row_target(const VocabArgs& a, int64_t row, int lane) {
+  if (a.teacher == nullptr) {
+    const int64_t y = a.ids[row];
+    return RowTarget{0.f, 1.f, y >= 0, y >= a.V};
   }
-  r.top = wave_max(top);
-  r.bad = __any(bad);
-  r.counts = r.top != -INFINITY || __any(nan);
-  r.top = stat_shift(r.top);
-  float total = 0.f;
-  for (int j = lane; j < a.k; j += 64)
-    if (a.ids[at + j] >= 0) total += expf(teacher_logit(a, at + j) - r.top);
-  total = wave_sum(total);
-  r.total = total == 0.f ? 1.f : total;
-  return r;
+  RowEntries<kRowEntries> e;
+  e.load(a, row, lane);
+  return e.target(a, row, lane);
 }
 
-// The row's loss from its lse and the (capped) logits of its entries; every lane gets it.
+// A distillation row's loss from its lse and the (capped) logits of its entries; every lane gets it.
 __device__ __forceinline__ float row_loss(const VocabArgs& a, int64_t row, float lse, int lane, bool* counts) {
-  const RowTarget r = row_target(a, row, lane);
+  RowEntries<kRowEntries> e;
+  float z[kRowEntries];
+#pragma unroll
+  for (int n = 0; n < kRowEntries; ++n) z[n] = lane + n * 64 < a.k ? a.zt[row * a.k + lane + n * 64] : 0.f;
+  e.load(a, row, lane);
+  const RowTarget r = e.target(a, row, lane);
   *counts = r.counts;
   if (!r.counts) return 0.f;
   if (r.bad) return NAN;
-  if (a.teacher == nullptr) return __fmaf_rn(__fmul_rn(a.z_loss, lse), lse, __fsub_rn(lse, a.zt[row]));
   float loss = 0.f;
   const float log_total = logf(r.total);
-  for (int j = lane; j < a.k; j += 64) {
-    const int64_t i = row * a.k + j;
-    if (a.ids[i] < 0) continue;
-    const float t = teacher_logit(a, i), q = r.weight(t);
+  e.all(a, row, lane, [&](int n, int j, bool, float t) {
+    float zt = 0.f;
+    if (n < 0) zt = a.zt[row * a.k + j];
+#pragma unroll
+    for (int u = 0; u < kRowEntries; ++u) zt = n == u ? z[u] : zt;
+    const float q = r.weight(t);
     // (an entry of weight 0 adds nothing, also where its logarithm or logit is infinite)
-    if (q != 0.f) loss = __fmaf_rn(q, (t - r.top - log_total) - (__fdiv_rn(a.zt[i], a.T) - lse), loss);
-  }
+    if (q != 0.f) loss = __fmaf_rn(q, (t - r.top - log_total) - (__fdiv_rn(zt, a.T) - lse), loss);
+  });
   return a.T * a.T * wave_sum(loss);
 }
 
-// Statistics [parts][M] joined: lse, losses, their mean (vocab_tiles.hip).  sums: 16 bytes a row; done: 0.
+// Statistics [parts][M] joined: lse, losses, their mean (vocab_tiles.hip).  sums: vocab_join_bytes; done: 0.
+size_t vocab_join_bytes(const VocabArgs& a);
 hipError_t vocab_join_launch(const VocabArgs& a, const float2* part, int parts, void* sums, int* done, hipStream_t s);
 
 }  // namespace opfuse

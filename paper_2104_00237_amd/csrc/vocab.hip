@@ -219,7 +219,7 @@ Plan plan_of(const VocabArgs& a, bool bwd) {
     p.x = take((size_t)a.M * a.K * 4);
   } else {
     p.part = take((size_t)((a.V + p.piece - 1) / p.piece * p.chunks) * a.M * 8);
-    p.sums = take((size_t)a.M * 16);
+    p.sums = take(vocab_join_bytes(a));
     p.done = take(4);
   }
   p.total = at;

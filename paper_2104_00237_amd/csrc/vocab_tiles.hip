@@ -58,52 +58,62 @@ __device__ __forceinline__ void wave_lds_sync() {
 }
 
 // ---------------------------------------------------------------------- forward
-// A row's entries by tile: off[row tile][vocabulary tile] .. of list[row tile], each entry its row and
-// its column in the tile and its number in the row.
+// Rows' entries by tile, a wavefront's rows (a group) at a time: off[group][vocabulary tile] .. of
+// list[group], each entry its row in the group, its place in the tile and its number in the row.
 struct Entries {
-  int* off;            // [row tiles][vtiles + 1]
-  uint32_t* list;      // [row tiles][BQ * k]
+  int* off;            // [groups][vtiles + 1]
+  uint32_t* list;      // [groups][rows of a group * k]
   int vtiles;
 };
 
-template <int BP, int BQ>
-__global__ __launch_bounds__(1024) void vocab_sort_kernel(VocabArgs a, Entries en, int* done) {
+template <int BP, int GROUP>
+__global__ __launch_bounds__(1024) void vocab_sort_kernel(VocabArgs a, Entries en, FastDiv dk, int* done) {
   extern __shared__ int bins[];   // [vtiles]
-  __shared__ int part[1024];
-  const int t = threadIdx.x;
-  const int64_t row0 = (int64_t)blockIdx.x * BQ;
-  const int n = (int)min((int64_t)BQ, a.M - row0) * a.k;
+  __shared__ int waves[16];
+  const int t = threadIdx.x, lane = t & 63, w = t >> 6;
+  const int64_t row0 = (int64_t)blockIdx.x * GROUP;
+  const int n = (int)min((int64_t)GROUP, a.M - row0) * a.k;
   const int64_t* ids = a.ids + row0 * a.k;
   if (blockIdx.x == 0 && t == 0) *done = 0;
   for (int i = t; i < en.vtiles; i += 1024) bins[i] = 0;
   __syncthreads();
-  constexpr int U = 8;   // loads in flight
-  for (int i0 = t; i0 < n; i0 += 1024 * U) {
-    int64_t id[U];
+  constexpr int U = 8;   // ids of a thread at a time; one batch (64 rows of 128) stays in registers
+  int id[U];
+  auto load = [&](int i0) {   // -1: no entry
+    int64_t y[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) id[u] = i0 + u * 1024 < n ? ids[i0 + u * 1024] : 0;
+    for (int u = 0; u < U; ++u) y[u] = i0 + u * 1024 < n ? ids[i0 + u * 1024] : -1;
+#pragma unroll
+    for (int u = 0; u < U; ++u) id[u] = y[u] >= 0 && y[u] < a.V ? (int)y[u] : -1;
+  };
+  for (int i0 = t; i0 < n; i0 += 1024 * U) {
+    load(i0);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int i = i0 + u * 1024;
       if (i >= n) continue;
-      if (id[u] >= 0 && id[u] < a.V) atomicAdd(&bins[(int)id[u] / BP], 1);
+      if (id[u] >= 0) atomicAdd(&bins[id[u] / BP], 1);
       else a.zt[row0 * a.k + i] = 0.f;
     }
   }
   __syncthreads();
-  // exclusive sums: a run of bins each thread, the runs' totals in steps of doubling
+  // exclusive sums: a run of bins each thread, then the runs' totals
   const int run = (en.vtiles + 1023) / 1024, b0 = min(en.vtiles, t * run), b1 = min(en.vtiles, b0 + run);
   int sum = 0;
   for (int b = b0; b < b1; ++b) sum += bins[b];
-  part[t] = sum;
-  __syncthreads();
-  for (int d = 1; d < 1024; d <<= 1) {
-    const int v = t >= d ? part[t - d] : 0;
-    __syncthreads();
-    part[t] += v;
-    __syncthreads();
+  int at = sum;
+  for (int d = 1; d < 64; d <<= 1) {
+    const int v = __shfl_up(at, d);
+    if (lane >= d) at += v;
   }
-  int at = part[t] - sum;
+  if (lane == 63) waves[w] = at;
+  __syncthreads();
+  at -= sum;
+  int all = 0;
+  for (int i = 0; i < 16; ++i) {
+    if (i < w) at += waves[i];
+    all += waves[i];
+  }
   int* off = en.off + (int64_t)blockIdx.x * (en.vtiles + 1);
   for (int b = b0; b < b1; ++b) {
     const int c = bins[b];
@@ -111,19 +121,18 @@ __global__ __launch_bounds__(1024) void vocab_sort_kernel(VocabArgs a, Entries e
     bins[b] = at;
     at += c;
   }
-  if (t == 1023) off[en.vtiles] = part[1023];
+  if (t == 0) off[en.vtiles] = all;
   __syncthreads();
   // (the order of a tile's entries may differ from run to run: each goes to a place of its own)
-  uint32_t* list = en.list + (int64_t)blockIdx.x * BQ * a.k;
+  uint32_t* list = en.list + (int64_t)blockIdx.x * GROUP * a.k;
   for (int i0 = t; i0 < n; i0 += 1024 * U) {
-    int64_t id[U];
-#pragma unroll
-    for (int u = 0; u < U; ++u) id[u] = i0 + u * 1024 < n ? ids[i0 + u * 1024] : -1;
+    if (n > 1024 * U) load(i0);
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-      if (id[u] < 0 || id[u] >= a.V) continue;
-      const int i = i0 + u * 1024, tile = (int)id[u] / BP, row = i / a.k;
-      list[atomicAdd(&bins[tile], 1)] = (uint32_t)row | (uint32_t)((int)id[u] - tile * BP) << 8 | (uint32_t)(i - row * a.k) << 16;
+      const int i = i0 + u * 1024;
+      if (i >= n || id[u] < 0) continue;
+      const int tile = id[u] / BP, row = fdiv(i, dk);
+      list[atomicAdd(&bins[tile], 1)] = (uint32_t)row | (uint32_t)(id[u] - tile * BP) << 8 | (uint32_t)(i - row * a.k) << 16;
     }
   }
 }
@@ -186,7 +195,9 @@ struct StatEpi {
         cap_block<PL>(acc[decltype(B_)::value / IQ][decltype(B_)::value % IQ], cap, rcap);
       });
     }
-    const int tile = tile0 + t.p0 / T::BP, rt = t.q0 / T::BQ;
+    constexpr int GROUP = IQ * 32;
+    const int tile = tile0 + t.p0 / T::BP;
+    const int64_t group = t.q0 / GROUP + wq;
     int e0 = 0, e1 = 0;
     if (labels) {
       if (blockIdx.x == 0 && tile0 == 0 && wave == 0 && lane == 0) *done = 0;
@@ -205,12 +216,12 @@ struct StatEpi {
             if (i * 32 + 8 * (r >> 2) + (r & 3) == label) zt[t.q0 + q] = acc[i][j][r];
         });
       });
-    } else {
-      const int* off = en.off + (int64_t)rt * (en.vtiles + 1) + tile;
+    } else if (wq * GROUP < t.nq) {
+      const int* off = en.off + group * (en.vtiles + 1) + tile;
       e0 = off[0], e1 = off[1];
     }
     if (e1 > e0) {
-      const uint32_t* list = en.list + (int64_t)rt * T::BQ * k;
+      const uint32_t* list = en.list + group * GROUP * k;
       float* lds = (float*)ring_part<T, PL, 4096, T::NW>(ring, wave);
       constexpr int U = 4;   // entries of a lane at a time
       for (int b = e0; b < e1; b += 64 * U) {
@@ -220,8 +231,8 @@ struct StatEpi {
         for (int u = 0; u < U; ++u) {
           const int e = b + u * 64 + lane;
           x[u] = e < e1 ? list[e] : 0;
-          const int i = ((x[u] >> 13) & 7) - wp * IP, j = ((x[u] >> 5) & 7) - wq * IQ;
-          block[u] = e < e1 && i >= 0 && i < IP && j >= 0 && j < IQ ? i * IQ + j : -1;
+          const int i = ((x[u] >> 13) & 7) - wp * IP, j = (x[u] >> 5) & 7;
+          block[u] = e < e1 && i >= 0 && i < IP ? i * IQ + j : -1;
         }
 #pragma unroll
         for (int i = 0; i < IP; ++i)
@@ -237,7 +248,7 @@ struct StatEpi {
 #pragma unroll
             for (int u = 0; u < U; ++u)
               if (block[u] == i * IQ + j)
-                zt[((int64_t)t.q0 + (x[u] & 255)) * k + (x[u] >> 16)] = lds[((x[u] >> 8) & 31) * 32 + (x[u] & 31)];
+                zt[(group * GROUP + (x[u] & 255)) * k + (x[u] >> 16)] = lds[((x[u] >> 8) & 31) * 32 + (x[u] & 31)];
             wave_lds_sync();
           }
       }
@@ -287,11 +298,14 @@ struct StatEpi {
   }
 };
 
-// Rows' statistics joined, RB rows a workgroup; their losses; the last workgroup takes the mean from
-// the workgroups' sums, in their order.
-constexpr int kJoinRows = 8, kJoinFew = 256;   // one row a workgroup up to kJoinFew rows
+// Rows' statistics joined, RB rows a workgroup, and their losses.  With few workgroups the last one takes the
+// mean from the workgroups' sums, in their order: a launch less; with many, each one's fence (it writes the
+// XCD's L2 back) costs more than that launch (1024 of them: 31 us).
+// (one row a workgroup up to kJoinFew rows; distillation: a wavefront for each row's entries)
+constexpr int kJoinRows = 8, kJoinRowsTop = 4, kJoinFew = 256, kMeanFew = 32;
 template <int RB>
-__global__ __launch_bounds__(256) void vocab_join_kernel(VocabArgs a, const float2* part, int parts, double2* sums, int* done) {
+__global__ __launch_bounds__(256) void vocab_join_kernel(VocabArgs a, const float2* part, int parts, float* counts_out,
+                                                         bool in_kernel_mean, double2* sums, int* done) {
   __shared__ float2 sh[256];
   __shared__ float ll[RB], cc[RB];
   __shared__ int last;
@@ -336,6 +350,7 @@ __global__ __launch_bounds__(256) void vocab_join_kernel(VocabArgs a, const floa
       }
       ll[t] = loss;
       cc[t] = counts ? 1.f : 0.f;
+      if (row < a.M) counts_out[row] = cc[t];
     }
   } else {
     for (int r = wave; r < RB; r += 4) {
@@ -347,6 +362,7 @@ __global__ __launch_bounds__(256) void vocab_join_kernel(VocabArgs a, const floa
         if (lane == 0) {
           a.lse[row0 + r] = lse;
           a.loss[row0 + r] = loss;
+          counts_out[row0 + r] = counts ? 1.f : 0.f;
         }
       }
       if (lane == 0) {
@@ -355,7 +371,7 @@ __global__ __launch_bounds__(256) void vocab_join_kernel(VocabArgs a, const floa
       }
     }
   }
-  if (a.mean == nullptr) return;
+  if (!in_kernel_mean) return;
   __syncthreads();
   if (t == 0) {
     double l = 0.0, c = 0.0;
@@ -367,16 +383,33 @@ __global__ __launch_bounds__(256) void vocab_join_kernel(VocabArgs a, const floa
   __syncthreads();
   if (!last) return;
   __threadfence();
-  __shared__ double2 tot[256];
-  double l = 0.0, c = 0.0;
-  for (int i = t; i < (int)gridDim.x; i += 256) l += sums[i].x, c += sums[i].y;
-  tot[t] = make_double2(l, c);
-  __syncthreads();
-  for (int d = 128; d > 0; d >>= 1) {
-    if (t < d) tot[t].x += tot[t + d].x, tot[t].y += tot[t + d].y;
-    __syncthreads();
+  if (t == 0) {
+    double l = 0.0, c = 0.0;
+    for (int i = 0; i < (int)gridDim.x; ++i) l += sums[i].x, c += sums[i].y;
+    *a.mean = (float)(l / fmax(c, 1.0));
   }
-  if (t == 0) *a.mean = (float)(tot[0].x / fmax(tot[0].y, 1.0));
+}
+
+// The mean of many rows: their losses over the number that count, in float64 and one order.
+__global__ __launch_bounds__(1024) void vocab_mean_kernel(const float* loss, const float* counts, int64_t M, float* mean) {
+  __shared__ double sh[2][16];
+  const int t = threadIdx.x;
+  double l = 0.0, c = 0.0;
+  constexpr int U = 8;
+  for (int64_t i = t; i < M; i += 1024 * U) {
+    float x[U], y[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) x[u] = i + u * 1024 < M ? loss[i + u * 1024] : 0.f, y[u] = i + u * 1024 < M ? counts[i + u * 1024] : 0.f;
+#pragma unroll
+    for (int u = 0; u < U; ++u) l += (double)x[u], c += (double)y[u];
+  }
+#pragma unroll
+  for (int d = 32; d > 0; d >>= 1) l += __shfl_xor(l, d), c += __shfl_xor(c, d);
+  if ((t & 63) == 0) sh[0][t >> 6] = l, sh[1][t >> 6] = c;
+  __syncthreads();
+  if (t) return;
+  for (int i = 1; i < 16; ++i) l += sh[0][i], c += sh[1][i];
+  *mean = (float)(l / fmax(c, 1.0));
 }
 
 // --------------------------------------------------------------------- backward
@@ -884,8 +917,8 @@ struct TilesPlan {
   int PL;                           // planes of an operand
   int64_t Kp, piece, copied, ldz;   // widened rows; vocabulary entries of a piece, and of one whose W is copied
   Choice logits, dx, dw;
-  int BP, BQ;                       // the logits' tiles
-  int64_t vtiles, rtiles;
+  int BP, group;                    // the logits' tiles: vocabulary entries, and rows of a wavefront
+  int64_t vtiles, groups;
   int64_t px, pw, pz;               // elements of a plane of X, W and the gradient
   size_t x, w, off, list, part, sums, done;
   size_t flag, weight, at, place, n, scale, rows, dz, pdx, pdw, total;
@@ -903,8 +936,8 @@ TilesPlan tiles_plan(const VocabArgs& a, bool bwd) {
   };
   p.logits = a.M <= kFew && a.bf16 ? Choice{FEW, 1} : choose(a.V, a.M, a.K, p.PL, false, FewQ::BP, FewQ::BQ);
   p.BP = p.logits.shape == BIG ? 256 : 128;
-  p.BQ = p.logits.shape == BIG ? 256 : p.logits.shape == MID ? 128 : 32;
-  p.vtiles = per(a.V, p.BP), p.rtiles = per(a.M, p.BQ);
+  p.group = 32 * (p.logits.shape == BIG ? Big::IQ : p.logits.shape == MID ? Mid::IQ : FewQ::IQ);
+  p.vtiles = per(a.V, p.BP), p.groups = per(a.M, p.group);
   // fp32 W, and W whose rows are not whole 16-byte pieces, is copied: up to 512 MB at a time, in copies of
   // one size
   const int64_t room = std::max<int64_t>(256, (1LL << 28) / (p.Kp * p.PL) / 256 * 256);
@@ -914,10 +947,10 @@ TilesPlan tiles_plan(const VocabArgs& a, bool bwd) {
   if (!bwd) {
     p.pw = p.copied * p.Kp;
     p.w = take(p.pw * p.PL * 2);
-    p.off = take(p.rtiles * (p.vtiles + 1) * 4);
-    p.list = take(p.rtiles * p.BQ * a.k * 4);
+    p.off = take(p.groups * (p.vtiles + 1) * 4);
+    p.list = take(p.groups * p.group * a.k * 4);
     p.part = take(p.vtiles * a.M * 8);
-    p.sums = take(per(a.M, a.M <= kJoinFew ? 1 : kJoinRows) * 16);
+    p.sums = take((int64_t)vocab_join_bytes(a));
     p.done = take(4);
     p.total = here;
     return p;
@@ -1001,8 +1034,8 @@ struct Tiles {
   template <class T>
   hipError_t sort_entries() const {
     const Entries en{at<int>(p.off), at<uint32_t>(p.list), (int)p.vtiles};
-    hipLaunchKernelGGL((vocab_sort_kernel<T::BP, T::BQ>), dim3((unsigned)p.rtiles), dim3(1024), (size_t)p.vtiles * 4, s, a, en,
-                       at<int>(p.done));
+    hipLaunchKernelGGL((vocab_sort_kernel<T::BP, T::IQ * 32>), dim3((unsigned)p.groups), dim3(1024), (size_t)p.vtiles * 4, s, a, en,
+                       make_fastdiv((uint32_t)a.k), at<int>(p.done));
     return hipGetLastError();
   }
   template <class T>
@@ -1136,13 +1169,20 @@ struct Tiles {
 }  // namespace
 
 hipError_t vocab_join_launch(const VocabArgs& a, const float2* part, int parts, void* sums, int* done, hipStream_t s) {
-  if (a.M <= kJoinFew)
-    hipLaunchKernelGGL(vocab_join_kernel<1>, dim3((unsigned)a.M), dim3(256), 0, s, a, part, parts, (double2*)sums, done);
-  else
-    hipLaunchKernelGGL(vocab_join_kernel<kJoinRows>, dim3((unsigned)per(a.M, kJoinRows)), dim3(256), 0, s, a, part, parts,
-                       (double2*)sums, done);
+  // sums: the rows' counts, or up to kMeanFew workgroups' sums
+  float* counts = (float*)((char*)sums + kMeanFew * sizeof(double2));
+  const bool few = a.mean && a.M <= kMeanFew;
+  auto go = [&](auto* kernel, int64_t rows) {
+    hipLaunchKernelGGL(kernel, dim3((unsigned)per(a.M, rows)), dim3(256), 0, s, a, part, parts, counts, few, (double2*)sums, done);
+  };
+  if (a.M <= kJoinFew) go(vocab_join_kernel<1>, 1);
+  else if (a.teacher) go(vocab_join_kernel<kJoinRowsTop>, kJoinRowsTop);
+  else go(vocab_join_kernel<kJoinRows>, kJoinRows);
+  TRY(hipGetLastError());
+  if (a.mean && !few) hipLaunchKernelGGL(vocab_mean_kernel, dim3(1), dim3(1024), 0, s, a.loss, counts, a.M, a.mean);
   return hipGetLastError();
 }
+size_t vocab_join_bytes(const VocabArgs& a) { return kMeanFew * sizeof(double2) + (size_t)a.M * 4; }
 
 // fp32 W is made into planes first, which few rows do not pay for, and small calls lose to launches.  Pieces of
 // the library's fp32 products / tiles, us: 32768 x 1024 forward 256 rows 139 / 161, 512 244 / 214, backward 128
