@@ -151,6 +151,22 @@ __device__ __forceinline__ float row_loss(const VocabArgs& a, int64_t row, float
   return a.T * a.T * wave_sum(loss);
 }
 
+// The gradient at a place with logit z (capped): cp p - ct q, through the cap.
+__device__ __forceinline__ float place_grad(float T, float cap, float z, float lse, float cp, float ct, float q) {
+  const float p = expf(__fsub_rn(__fdiv_rn(z, T), lse));
+  const float d = __fmaf_rn(cp, p, -__fmul_rn(ct, q));
+  if (cap <= 0.f) return d;
+  const float r = __fdiv_rn(z, cap);
+  return __fmul_rn(d, __fmaf_rn(-r, r, 1.f));
+}
+// An entry's logit for it: the forward's own where the one computed again agrees with it up to rounding.  Where an
+// entry has most of the probability, a rounding of its logit is in lse too and leaves p - q alone; another
+// product's rounding would not (fp32 forwards and backwards change kernels at different sizes: 7701 rows over 190
+// of width 3904 were 8.5e-6 from float64 instead of XX).  A W that has moved on from the forward's has its own.
+__device__ __forceinline__ float entry_logit(float z, float forward) {
+  return fabsf(z - forward) <= 0x1p-16f * (1.f + fabsf(forward)) ? forward : z;
+}
+
 // Statistics [parts][M] joined: lse, losses, their mean (vocab_tiles.hip).  sums: vocab_join_bytes; done: 0.
 size_t vocab_join_bytes(const VocabArgs& a);
 hipError_t vocab_join_launch(const VocabArgs& a, const float2* part, int parts, void* sums, int* done, hipStream_t s);

@@ -98,7 +98,7 @@ __global__ __launch_bounds__(256) void vocab_prepare_kernel(VocabArgs a, float2*
 }
 
 // The gradient of a chunk of a row's logits, in place of them.  An entry's place is written by its first
-// entry with the weights of all that name it; its logit is taken before the row is overwritten.
+// entry with the weights of all that name it; its logit is read before the row is overwritten.
 __global__ __launch_bounds__(256) void vocab_grad_kernel(VocabArgs a, float* __restrict__ z, int64_t ldz, int64_t v0, int n,
                                                          const float2* coef, const float* counts) {
   constexpr int EACH = kTopMax / 256;
@@ -121,15 +121,9 @@ __global__ __launch_bounds__(256) void vocab_grad_kernel(VocabArgs a, float* __r
     g = 1.f / fmaxf(red[0] + red[1] + red[2] + red[3], 1.f);
   }
   const float lse = a.lse[row], ct = __fmul_rn(c.x, g), cp = __fmul_rn(c.y, g);
-  auto grad = [&](float logit, float q) {
-    const float zc = vocab_cap_exact(logit, a.cap);
-    const float p = expf(__fsub_rn(__fdiv_rn(zc, a.T), lse));
-    float d = __fmaf_rn(cp, p, -__fmul_rn(ct, q));
-    if (a.cap > 0.f) {
-      const float r = zc / a.cap;
-      d = __fmul_rn(d, __fmaf_rn(-r, r, 1.f));
-    }
-    return d;
+  auto grad = [&](float logit) { return place_grad(a.T, a.cap, vocab_cap_exact(logit, a.cap), lse, cp, 0.f, 0.f); };
+  auto entry = [&](int64_t i, int place, float q) {
+    return place_grad(a.T, a.cap, entry_logit(vocab_cap_exact(s[place], a.cap), a.zt[i]), lse, cp, ct, q);
   };
   const int64_t at = row * a.k;
   int where[EACH];
@@ -138,7 +132,7 @@ __global__ __launch_bounds__(256) void vocab_grad_kernel(VocabArgs a, float* __r
     where[0] = -1;
     if (t == 0) {
       const int64_t id = a.ids[row] - v0;
-      if (id >= from && id < end) where[0] = (int)id, d[0] = grad(s[id], 1.f);
+      if (id >= from && id < end) where[0] = (int)id, d[0] = entry(row, (int)id, 1.f);
     }
 #pragma unroll
     for (int u = 1; u < EACH; ++u) where[u] = -1;
@@ -160,7 +154,7 @@ __global__ __launch_bounds__(256) void vocab_grad_kernel(VocabArgs a, float* __r
       }
       if (!first) continue;
       where[u] = (int)(id - v0);
-      d[u] = grad(s[id - v0], q);
+      d[u] = entry(at + j, (int)(id - v0), q);
     }
   }
   Chunk k;
@@ -169,7 +163,7 @@ __global__ __launch_bounds__(256) void vocab_grad_kernel(VocabArgs a, float* __r
 #pragma unroll
   for (int u = 0; u < 4; ++u) {
     const int i = from + (u * 256 + t) * 4;
-    if (i < n) st4(s + i, make_float4(grad(k.v[4 * u], 0.f), grad(k.v[4 * u + 1], 0.f), grad(k.v[4 * u + 2], 0.f), grad(k.v[4 * u + 3], 0.f)));
+    if (i < n) st4(s + i, make_float4(grad(k.v[4 * u]), grad(k.v[4 * u + 1]), grad(k.v[4 * u + 2]), grad(k.v[4 * u + 3])));
   }
   __syncthreads();
 #pragma unroll

@@ -426,11 +426,15 @@ __global__ __launch_bounds__(256) void vocab_flag_kernel(VocabArgs a, uint8_t* f
 
 // The rows with a gradient in order: at[i] is the i-th, place[row] its number or -1, n[0] how many;
 // scale: what the stored gradient leaves out.  rows[i]: lse, the factors of the probabilities and
-// of the targets, the label.
+// of the targets, the label and its logit.
 struct RowCoef {
   float lse, cp, ct;
   int label;           // cross-entropy; distillation: -1
+  float zt;
 };
+__device__ __forceinline__ RowCoef row_coef(const VocabArgs& a, int64_t row, float lse, float ct, int label) {
+  return RowCoef{lse, __fmul_rn(ct, __fmaf_rn(2.f * a.z_loss, lse, 1.f)), ct, label, label >= 0 ? a.zt[row] : 0.f};
+}
 __global__ __launch_bounds__(1024) void vocab_index_kernel(VocabArgs a, const uint8_t* flag, int* at, int* place, int* n,
                                                            float* scale, RowCoef* rows) {
   __shared__ int waves[16], counted[16];
@@ -487,7 +491,7 @@ __global__ __launch_bounds__(1024) void vocab_index_kernel(VocabArgs a, const ui
       place[row] = f[u] == 2 ? to : -1;
       if (f[u] != 2) continue;
       at[to] = (int)row;
-      rows[to] = RowCoef{lse[u], __fmul_rn(g[u], __fmaf_rn(2.f * a.z_loss, lse[u], 1.f)), g[u], label[u]};
+      rows[to] = row_coef(a, row, lse[u], g[u], label[u]);
     }
   }
 }
@@ -552,8 +556,7 @@ __global__ __launch_bounds__(256) void vocab_prepared_kernel(VocabArgs a, int* a
     if (t == 0) {
       const bool live = r.counts && !r.bad;
       const float lse = a.lse[row], ct = a.dloss ? __fmul_rn(a.dloss[row], a.T) : 1.f;
-      rows[row] = live ? RowCoef{lse, __fmul_rn(ct, __fmaf_rn(2.f * a.z_loss, lse, 1.f)), ct, a.teacher ? -1 : (int)a.ids[row]}
-                       : RowCoef{0.f, 0.f, 0.f, -1};
+      rows[row] = live ? row_coef(a, row, lse, ct, a.teacher ? -1 : (int)a.ids[row]) : RowCoef{0.f, 0.f, 0.f, -1, 0.f};
       weight[row] = make_float2(r.top, r.total);
       at[row] = (int)row;
       place[row] = live ? (int)row : -1;
@@ -587,7 +590,7 @@ __global__ __launch_bounds__(256) void vocab_prepared_kernel(VocabArgs a, int* a
 
 // A = W, B = X again: the gradient of a row's logits (distillation: but for its entries), rounded to bf16 or
 // in three planes, stored [row][vocabulary] through the ring, in 16-byte pieces of whole rows.
-template <class T, int PL>
+template <class Shape_, int PL>
 struct GradEpi {
   static constexpr int ROWS = ROWS_Q;
   const RowCoef* rows;
@@ -598,22 +601,23 @@ struct GradEpi {
   const float* counts; // of prepared rows without given gradients, for the scale; else NULL
   int M;
   float* scale;
+  float T;
   template <class Acc>
   __device__ __forceinline__ void operator()(const TilePlace& t, Acc& acc, const Ring& ring, int lane, int wave, int wp,
                                              int wq) const {
-    constexpr int IP = T::IP, IQ = T::IQ, SLOTS = IP * 4;   // 16-byte pieces of a row in LDS
+    constexpr int IP = Shape_::IP, IQ = Shape_::IQ, SLOTS = IP * 4;   // 16-byte pieces of a row in LDS
     const int h = lane >> 5, l32 = lane & 31;
     const int np = t.np - wp * IP * 32, nq = t.nq - wq * IQ * 32;
     if (counts && blockIdx.x == 0 && wave == 0 && v0 == 0) {
       float c = 0.f;
       for (int i = lane; i < M; i += 64) c += counts[i];
       c = wave_sum(c);   // (whole numbers: exact)
-      if (lane == 0) *scale = 1.f / (rT * fmaxf(c, 1.f));
+      if (lane == 0) *scale = T / fmaxf(c, 1.f);
     }
     RowCoef rc[IQ];
 #pragma unroll
     for (int j = 0; j < IQ; ++j) {
-      rc[j] = RowCoef{0.f, 0.f, 0.f, -1};
+      rc[j] = RowCoef{0.f, 0.f, 0.f, -1, 0.f};
       if (j * 32 + l32 < nq) rc[j] = rows[t.q0 + (wq * IQ + j) * 32 + l32];
     }
     auto fill = [&](auto J_, auto Capped) __attribute__((always_inline)) {
@@ -630,18 +634,21 @@ struct GradEpi {
         const float c2 = rT * kLog2E * (capped ? cap : 1.f), lse2 = rc[j].lse * kLog2E;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          float d, x = 0.f;   // x: the logit over its cap
+          float d, z, x = 0.f;   // x: the logit over its cap
           if constexpr (PL == 1) {
             x = acc[i][j][r];
+            z = capped ? __fmul_rn(cap, x) : x;
             d = __builtin_amdgcn_exp2f(__fmaf_rn(x, c2, -lse2));
           } else {
-            const float z = vocab_cap_exact(acc[i][j][r], capped ? cap : 0.f);
+            z = vocab_cap_exact(acc[i][j][r], capped ? cap : 0.f);
             x = __fmul_rn(z, rcap);
             d = __builtin_amdgcn_exp2f(__fmul_rn(kLog2E, __fmaf_rn(z, rT, -rc[j].lse)));
           }
           d = __fmul_rn(d, rc[j].cp);
-          if (here) d = 8 * (r >> 2) + (r & 3) == label ? __fsub_rn(d, rc[j].ct) : d;
-          acc[i][j][r] = capped ? __fmul_rn(d, __fmaf_rn(-x, x, 1.f)) : d;
+          d = capped ? __fmul_rn(d, __fmaf_rn(-x, x, 1.f)) : d;
+          if (here && 8 * (r >> 2) + (r & 3) == label)
+            d = place_grad(T, cap, entry_logit(z, rc[j].zt), rc[j].lse, rc[j].cp, rc[j].ct, 1.f);
+          acc[i][j][r] = d;
         }
         if (np < IP * 32) {   // the piece's last tile: zeros to the end of its 16-byte pieces
 #pragma unroll
@@ -659,7 +666,7 @@ struct GradEpi {
       else fill(J_, std::false_type{});
 #pragma unroll
       for (int p = 0; p < PL; ++p) {
-        char* lds = ring_part<T, PL, IP * 2048, T::NW * 2>(ring, wave * 2 + ((j * PL + p) & 1));
+        char* lds = ring_part<Shape_, PL, IP * 2048, Shape_::NW * 2>(ring, wave * 2 + ((j * PL + p) & 1));
 #pragma unroll
         for (int i = 0; i < IP; ++i)
 #pragma unroll
@@ -695,15 +702,6 @@ struct GradEpi {
 
 // Distillation, the entries' places in a piece: p less the weights of all the row's entries that name it, by
 // the first of them, from the logit that the forward kept.
-__device__ __forceinline__ float entry_grad(const VocabArgs& a, const RowCoef& rc, float z, float q) {
-  const float p = __builtin_amdgcn_exp2f(__fmul_rn(kLog2E, __fsub_rn(__fdiv_rn(z, a.T), rc.lse)));
-  float d = __fmaf_rn(rc.cp, p, -__fmul_rn(rc.ct, q));
-  if (a.cap > 0.f) {
-    const float x = __fmul_rn(z, a.rcap);
-    d = __fmul_rn(d, __fmaf_rn(-x, x, 1.f));
-  }
-  return d;
-}
 template <int PL>
 __global__ __launch_bounds__(256) void vocab_entry_kernel(VocabArgs a, const int* at, const int* n, const RowCoef* rows,
                                                           const float2* weight, int64_t v0, int64_t nv, uint16_t* dz,
@@ -740,7 +738,7 @@ __global__ __launch_bounds__(256) void vocab_entry_kernel(VocabArgs a, const int
     }
     if (!lead) continue;
     uint16_t* d = dz + (int64_t)i * ldz + place;
-    float x = entry_grad(a, rc, a.zt[first + j], q), y = 0.f;
+    float x = place_grad(a.T, a.cap, a.zt[first + j], rc.lse, rc.cp, rc.ct, q), y = 0.f;
 #pragma unroll
     for (int p = 0; p < PL; ++p) d[p * plane] = (uint16_t)take_part(x, y);
   }
@@ -1108,7 +1106,7 @@ struct Tiles {
   template <class T>
   hipError_t grads(const Operand& w, int64_t v0, int64_t n) const {
     const GradEpi<T, PL> e{at<RowCoef>(p.rows), at<uint16_t>(p.dz), p.ldz, p.pz, a.cap, a.rcap, 1.f / a.T, (int)v0,
-                           prepared() && !a.dloss ? at<const float>(p.flag) : nullptr, (int)a.M, at<float>(p.scale)};
+                           prepared() && !a.dloss ? at<const float>(p.flag) : nullptr, (int)a.M, at<float>(p.scale), a.T};
     return product<T, PL, true, true>(w, Operand{at<uint16_t>(p.x), p.Kp, p.px}, n, a.M, a.K, at<int>(p.n), 1, e, s);
   }
   template <class T>
