@@ -162,7 +162,7 @@ __device__ __forceinline__ float place_grad(float T, float cap, float z, float l
 // An entry's logit for it: the forward's own where the one computed again agrees with it up to rounding.  Where an
 // entry has most of the probability, a rounding of its logit is in lse too and leaves p - q alone; another
 // product's rounding would not (fp32 forwards and backwards change kernels at different sizes: 7701 rows over 190
-// of width 3904 were 8.5e-6 from float64 instead of XX).  A W that has moved on from the forward's has its own.
+// of width 3904 were 8.5e-6 from float64 instead of 2.4e-6).  A W that has moved on from the forward's has its own.
 __device__ __forceinline__ float entry_logit(float z, float forward) {
   return fabsf(z - forward) <= 0x1p-16f * (1.f + fabsf(forward)) ? forward : z;
 }

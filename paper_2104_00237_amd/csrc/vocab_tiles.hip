@@ -547,7 +547,7 @@ constexpr int kPrepared = 384;
 template <int PL>
 __global__ __launch_bounds__(256) void vocab_prepared_kernel(VocabArgs a, int* at, int* place, int* n, float* scale, float* counts,
                                                              RowCoef* rows, float2* weight, uint16_t* x, int64_t ldd,
-                                                             int64_t plane) {
+                                                             int64_t plane, int twice) {
   __shared__ int on;
   const int t = threadIdx.x;
   const int64_t row = blockIdx.x;
@@ -562,7 +562,8 @@ __global__ __launch_bounds__(256) void vocab_prepared_kernel(VocabArgs a, int* a
       place[row] = live ? (int)row : -1;
       counts[row] = r.counts ? 1.f : 0.f;
       if (row == 0) {
-        *n = (int)a.M;
+        n[0] = (int)a.M;
+        n[1] = 2 * n[0];
         if (a.dloss) *scale = 1.f;
       }
       on = live;
@@ -580,7 +581,9 @@ __global__ __launch_bounds__(256) void vocab_prepared_kernel(VocabArgs a, int* a
       v[e] = PL == 1 ? __uint_as_float((uint32_t)((const uint16_t*)a.x)[i] << 16) : ((const float*)a.x)[i];
     }
     if constexpr (PL == 1) {
-      *reinterpret_cast<uint32_t*>(d) = __float_as_uint(v[0]) >> 16 | (__float_as_uint(v[1]) & 0xffff0000u);
+      const uint32_t two = __float_as_uint(v[0]) >> 16 | (__float_as_uint(v[1]) & 0xffff0000u);
+      *reinterpret_cast<uint32_t*>(d) = two;
+      if (twice) *reinterpret_cast<uint32_t*>(d + plane) = two;
     } else {
 #pragma unroll
       for (int p = 0; p < 3; ++p) *reinterpret_cast<uint32_t*>(d + p * plane) = take_part(v[0], v[1]);
@@ -590,8 +593,13 @@ __global__ __launch_bounds__(256) void vocab_prepared_kernel(VocabArgs a, int* a
 
 // A = W, B = X again: the gradient of a row's logits (distillation: but for its entries), rounded to bf16 or
 // in three planes, stored [row][vocabulary] through the ring, in 16-byte pieces of whole rows.
-template <class Shape_, int PL>
+// A row's gradient is mostly its label's, and one rounding of that to bf16 (up to 2^-8) is a common factor of the
+// row's dX, where the others' roundings average out: what it leaves is kept (rest: id, value) and taken with W's
+// row when dX is stored.  dW adds rows up, which averages too unless they are few: up
+// to kFew of them have a second plane, which dW's reduction takes as more rows.
+template <class Shape_, int PL, bool TWO>
 struct GradEpi {
+  static constexpr int NP = TWO ? 2 : PL;
   static constexpr int ROWS = ROWS_Q;
   const RowCoef* rows;
   uint16_t* dz;
@@ -602,6 +610,7 @@ struct GradEpi {
   int M;
   float* scale;
   float T;
+  int2* rest;          // bf16 cross-entropy; else NULL
   template <class Acc>
   __device__ __forceinline__ void operator()(const TilePlace& t, Acc& acc, const Ring& ring, int lane, int wave, int wp,
                                              int wq) const {
@@ -631,6 +640,7 @@ struct GradEpi {
         // bf16 operands: what is left of the logit is tanh alone, and lse is taken off in units of log2 (its
         // rounding there, 1e-6 of a probability, is nothing beside bf16's)
         if constexpr (capped && PL == 1) tanh_block(acc[i][j], rcap);
+        float at_label = 0.f;
         const float c2 = rT * kLog2E * (capped ? cap : 1.f), lse2 = rc[j].lse * kLog2E;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
@@ -646,9 +656,18 @@ struct GradEpi {
           }
           d = __fmul_rn(d, rc[j].cp);
           d = capped ? __fmul_rn(d, __fmaf_rn(-x, x, 1.f)) : d;
-          if (here && 8 * (r >> 2) + (r & 3) == label)
-            d = place_grad(T, cap, entry_logit(z, rc[j].zt), rc[j].lse, rc[j].cp, rc[j].ct, 1.f);
           acc[i][j][r] = d;
+          if (here) at_label = 8 * (r >> 2) + (r & 3) == label ? z : at_label;
+        }
+        if (here) {
+          const float d = place_grad(T, cap, entry_logit(at_label, rc[j].zt), rc[j].lse, rc[j].cp, rc[j].ct, 1.f);
+#pragma unroll
+          for (int r = 0; r < 16; ++r) acc[i][j][r] = 8 * (r >> 2) + (r & 3) == label ? d : acc[i][j][r];
+          if (rest && label >= 0 && label < 32 && !(label & 4)) {
+            float left = d, none = 0.f;
+            take_part(left, none);
+            rest[t.q0 + (wq * IQ + j) * 32 + l32] = make_int2(rc[j].label, __float_as_int(left));
+          }
         }
         if (np < IP * 32) {   // the piece's last tile: zeros to the end of its 16-byte pieces
 #pragma unroll
@@ -665,15 +684,15 @@ struct GradEpi {
       if (cap > 0.f) fill(J_, std::true_type{});
       else fill(J_, std::false_type{});
 #pragma unroll
-      for (int p = 0; p < PL; ++p) {
-        char* lds = ring_part<Shape_, PL, IP * 2048, Shape_::NW * 2>(ring, wave * 2 + ((j * PL + p) & 1));
+      for (int p = 0; p < NP; ++p) {
+        char* lds = ring_part<Shape_, PL, IP * 2048, Shape_::NW * 2>(ring, wave * 2 + ((j * NP + p) & 1));
 #pragma unroll
         for (int i = 0; i < IP; ++i)
 #pragma unroll
           for (int g = 0; g < 4; ++g) {
             const int slot = (i * 4 + g) ^ (l32 & (SLOTS - 1));
             uint2 w;
-            if constexpr (PL == 1) {
+            if constexpr (NP == 1) {
               w = make_uint2(pack2(acc[i][j][4 * g], acc[i][j][4 * g + 1]), pack2(acc[i][j][4 * g + 2], acc[i][j][4 * g + 3]));
             } else {
               float x[4];
@@ -702,10 +721,11 @@ struct GradEpi {
 
 // Distillation, the entries' places in a piece: p less the weights of all the row's entries that name it, by
 // the first of them, from the logit that the forward kept.
-template <int PL>
+// rest (bf16): as GradEpi's, of the entry with the largest so far.
+template <int NP>
 __global__ __launch_bounds__(256) void vocab_entry_kernel(VocabArgs a, const int* at, const int* n, const RowCoef* rows,
                                                           const float2* weight, int64_t v0, int64_t nv, uint16_t* dz,
-                                                          int64_t ldz, int64_t plane) {
+                                                          int64_t ldz, int64_t plane, int2* rest) {
   __shared__ __attribute__((aligned(16))) int places[4][kTopMax];   // in the piece, or -1
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
   const int i = blockIdx.x * 4 + w;
@@ -719,7 +739,11 @@ __global__ __launch_bounds__(256) void vocab_entry_kernel(VocabArgs a, const int
   wave_lds_sync();
   const RowTarget r{weight[row].x, weight[row].y, true, false};
   const RowCoef rc = rows[i];
-  if (rc.cp == 0.f && rc.ct == 0.f) return;   // (zeros already)
+  int2 most = rest && v0 > 0 && lane == 0 ? rest[i] : make_int2(-1, 0);
+  if (rc.cp == 0.f && rc.ct == 0.f) {   // (zeros already)
+    if (rest && lane == 0) rest[i] = most;
+    return;
+  }
   for (int j0 = 0; j0 < a.k; j0 += 64) {
     const int j = j0 + lane, place = j < a.k ? places[w][j] : -1;
     if (!__any(place >= 0)) continue;
@@ -740,8 +764,15 @@ __global__ __launch_bounds__(256) void vocab_entry_kernel(VocabArgs a, const int
     uint16_t* d = dz + (int64_t)i * ldz + place;
     float x = place_grad(a.T, a.cap, a.zt[first + j], rc.lse, rc.cp, rc.ct, q), y = 0.f;
 #pragma unroll
-    for (int p = 0; p < PL; ++p) d[p * plane] = (uint16_t)take_part(x, y);
+    for (int p = 0; p < NP; ++p) {
+      d[p * plane] = (uint16_t)take_part(x, y);
+      if (p == 0 && fabsf(x) > fabsf(__int_as_float(most.y))) most = make_int2((int)v0 + place, __float_as_int(x));
+    }
   }
+  if (!rest) return;
+  const float big = wave_max(fabsf(__int_as_float(most.y)));
+  const uint64_t who = __ballot(most.x >= 0 && fabsf(__int_as_float(most.y)) == big);
+  if (who ? lane == __ffsll((unsigned long long)who) - 1 : lane == 0) rest[i] = most;
 }
 
 // Sums of a part of the reduction: stored, or added to those of the pieces before.
@@ -890,10 +921,22 @@ __global__ __launch_bounds__(256) void vocab_head_kernel(HeadGrad g, const float
   }
 }
 
-// dX from its parts [S][M][ld]: their sum in order, scaled, at its row; zeros where a row has none.
+// W's rows of a piece that dX still takes (rest), before the update.
+__global__ __launch_bounds__(256) void vocab_rest_kernel(const int2* rest, const int* n, int64_t v0, int64_t nv, const uint16_t* w,
+                                                         int64_t K, uint16_t* kept, int64_t ld) {
+  const int64_t count = *n;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < count * K; i += (int64_t)gridDim.x * 256) {
+    const int64_t r = i / K, c = i - r * K, id = rest[r].x;
+    if (id >= v0 && id < v0 + nv) kept[r * ld + c] = w[id * K + c];
+  }
+}
+
+// dX from its parts [S][M][ld]: their sum in order and the rest (of W, or kept rows of it), scaled, at its row;
+// zeros where a row has none.
 template <int V>
 __global__ __launch_bounds__(256) void vocab_dx_kernel(const float* part, int S, int64_t M, int64_t ld, const int* place,
-                                                       const float* scale, int64_t K, void* dx, int64_t ldx, int gbf) {
+                                                       const float* scale, int64_t K, void* dx, int64_t ldx, int gbf, const int2* rest,
+                                                       const uint16_t* w, int64_t ldw, int kept) {
   const float f = *scale;
   const int64_t each = K / V;
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < M * each; i += (int64_t)gridDim.x * 256) {
@@ -919,6 +962,19 @@ __global__ __launch_bounds__(256) void vocab_dx_kernel(const float* part, int S,
         for (int u = 0; u < 8; ++u)
 #pragma unroll
           for (int e = 0; e < V; ++e) v[e] = __fadd_rn(v[e], x[u][e]);
+      }
+      const int2 left = rest ? rest[r] : make_int2(-1, 0);
+      if (left.x >= 0) {
+        const uint16_t* y = w + (kept ? r : left.x) * ldw + c;
+        uint32_t x[V];
+        if constexpr (V == 4) {
+          const uint2 z = *reinterpret_cast<const uint2*>(y);
+          x[0] = z.x << 16, x[1] = z.x & 0xffff0000u, x[2] = z.y << 16, x[3] = z.y & 0xffff0000u;
+        } else {
+          x[0] = (uint32_t)y[0] << 16;
+        }
+#pragma unroll
+        for (int e = 0; e < V; ++e) v[e] = __fmaf_rn(__int_as_float(left.y), __uint_as_float(x[e]), v[e]);
       }
     }
 #pragma unroll
@@ -979,7 +1035,8 @@ struct TilesPlan {
   int64_t vtiles, groups;
   int64_t px, pw, pz;               // elements of a plane of X, W and the gradient
   size_t x, w, off, list, part, sums, done;
-  size_t flag, weight, at, place, n, scale, rows, dz, pdx, pdw, total;
+  bool two;                         // two planes of a bf16 gradient, for dW
+  size_t flag, weight, at, place, n, scale, rows, rest, kept, dz, pdx, pdw, total;
 };
 
 TilesPlan tiles_plan(const VocabArgs& a, bool bwd) {
@@ -1000,8 +1057,9 @@ TilesPlan tiles_plan(const VocabArgs& a, bool bwd) {
   // one size
   const int64_t room = std::max<int64_t>(256, (1LL << 28) / (p.Kp * p.PL) / 256 * 256);
   p.copied = std::min(up(per(a.V, per(a.V, room)), 256), up(a.V, 8));
+  p.two = bwd && a.bf16 && a.M <= kFew;
   p.px = a.M * p.Kp;
-  p.x = take(p.px * p.PL * 2);
+  p.x = take(p.px * (p.two ? 2 : p.PL) * 2);
   if (!bwd) {
     p.pw = p.copied * p.Kp;
     p.w = take(p.pw * p.PL * 2);
@@ -1022,16 +1080,18 @@ TilesPlan tiles_plan(const VocabArgs& a, bool bwd) {
   p.ldz = p.piece;
   p.pz = a.M * p.ldz;
   p.dx = a.M <= kFew && a.bf16 ? Choice{FEW, few_parts(a.K, p.piece)} : choose(a.M, a.K, p.piece, p.PL, true, FewP::BP, FewP::BQ);
-  p.dw = choose(p.piece, a.K, a.M, p.PL, true);
+  p.dw = choose(p.piece, a.K, p.two ? 2 * a.M : a.M, p.PL, true);
 
   p.flag = take(a.M <= kPrepared ? a.M * 4 : a.M);   // flags, or prepared rows' counts
   p.weight = take(a.M * 8);
   p.at = take(a.M * 4);
   p.place = take(a.M * 4);
-  p.n = take(4);
+  p.n = take(8);
   p.scale = take(4);
   p.rows = take(a.M * (int64_t)sizeof(RowCoef));
-  p.dz = take(p.pz * p.PL * 2);
+  p.rest = take(a.bf16 ? a.M * 8 : 0);
+  p.kept = take(a.bf16 ? p.px * 2 : 0);
+  p.dz = take(p.pz * (p.two ? 2 : p.PL) * 2);
   p.pdx = take((int64_t)p.dx.S * a.M * p.Kp * 4);
   p.pdw = take(p.dw.S > 1 ? (int64_t)p.dw.S * p.piece * p.Kp * 4 : 0);
   p.total = here;
@@ -1103,10 +1163,11 @@ struct Tiles {
     const StatEpi<T, PL> e{a.teacher ? nullptr : a.ids, a.V, at<int>(p.done), at<float2>(p.part), a.zt, en, (int)(v0 / T::BP), a.M, a.k, a.cap, a.rcap, kLog2E / a.T};
     return product<T, PL, true, true>(w, x, n, a.M, a.K, nullptr, 1, e, s);
   }
-  template <class T>
+  int2* rest() const { return PL == 1 ? at<int2>(p.rest) : nullptr; }
+  template <class T, bool TWO = false>
   hipError_t grads(const Operand& w, int64_t v0, int64_t n) const {
-    const GradEpi<T, PL> e{at<RowCoef>(p.rows), at<uint16_t>(p.dz), p.ldz, p.pz, a.cap, a.rcap, 1.f / a.T, (int)v0,
-                           prepared() && !a.dloss ? at<const float>(p.flag) : nullptr, (int)a.M, at<float>(p.scale), a.T};
+    const GradEpi<T, PL, TWO> e{at<RowCoef>(p.rows), at<uint16_t>(p.dz), p.ldz, p.pz, a.cap, a.rcap, 1.f / a.T, (int)v0,
+                           prepared() && !a.dloss ? at<const float>(p.flag) : nullptr, (int)a.M, at<float>(p.scale), a.T, a.teacher ? nullptr : rest()};
     return product<T, PL, true, true>(w, Operand{at<uint16_t>(p.x), p.Kp, p.px}, n, a.M, a.K, at<int>(p.n), 1, e, s);
   }
   template <class T>
@@ -1117,17 +1178,18 @@ struct Tiles {
   template <class T>
   hipError_t head_grad(const HeadGrad& g, int64_t n) const {
     const Operand dz{at<uint16_t>(p.dz), p.ldz, p.pz}, x{at<uint16_t>(p.x), p.Kp, p.px};
-    const int* rows = at<int>(p.n);
+    const int* rows = at<int>(p.n) + (p.two ? 1 : 0);
+    const int64_t R = p.two ? 2 * a.M : a.M;
     if (p.dw.S > 1) {
       const PartEpi<T, ROWS_R> e{at<float>(p.pdw), n, p.Kp, 0};
-      TRY((product<T, PL, false, false>(dz, x, n, p.Kp, a.M, rows, p.dw.S, e, s)));
+      TRY((product<T, PL, false, false>(dz, x, n, p.Kp, R, rows, p.dw.S, e, s)));
       hipLaunchKernelGGL(vocab_head_kernel, dim3(grid_of(n * a.K)), dim3(256), 0, s, g, at<const float>(p.pdw), p.dw.S, n, p.Kp);
       return hipGetLastError();
     }
-    if (g.dw) return product<T, PL, false, false>(dz, x, n, p.Kp, a.M, rows, 1, HeadEpi<T, false>{g}, s);
+    if (g.dw) return product<T, PL, false, false>(dz, x, n, p.Kp, R, rows, 1, HeadEpi<T, false>{g}, s);
     // an update's memory traffic beside another workgroup's MFMAs: two workgroups a CU
     using U = std::conditional_t<std::is_same_v<T, Big>, std::conditional_t<PL == 1, Half, Mid>, T>;
-    return product<U, PL, false, false>(dz, x, n, p.Kp, a.M, rows, 1, HeadEpi<U, true>{g}, s);
+    return product<U, PL, false, false>(dz, x, n, p.Kp, R, rows, 1, HeadEpi<U, true>{g}, s);
   }
 
   hipError_t fwd() const {
@@ -1163,7 +1225,8 @@ struct Tiles {
     float* scale = at<float>(p.scale);
     if (prepared()) {
       hipLaunchKernelGGL(vocab_prepared_kernel<PL>, dim3((unsigned)a.M), dim3(256), 0, s, a, rows_at, place, n, scale,
-                         at<float>(p.flag), at<RowCoef>(p.rows), at<float2>(p.weight), at<uint16_t>(p.x), p.Kp, p.px);
+                         at<float>(p.flag), at<RowCoef>(p.rows), at<float2>(p.weight), at<uint16_t>(p.x), p.Kp, p.px,
+                         p.two ? 1 : 0);
       TRY(hipGetLastError());
     } else {
       if (a.teacher) {
@@ -1184,11 +1247,18 @@ struct Tiles {
         case BIG: TRY(grads<Big>(w, v0, nv)); break;
         case MID: TRY(grads<Mid>(w, v0, nv)); break;
         default:
-          if constexpr (PL == 1) TRY(grads<FewQ>(w, v0, nv));
+          if constexpr (PL == 1) {
+            if (p.two) TRY((grads<FewQ, true>(w, v0, nv)));
+            else TRY(grads<FewQ>(w, v0, nv));
+          }
       }
       if (a.teacher) {
-        hipLaunchKernelGGL(vocab_entry_kernel<PL>, dim3((unsigned)per(a.M, 4)), dim3(256), 0, s, a, rows_at, n, at<RowCoef>(p.rows),
-                           at<const float2>(p.weight), v0, nv, at<uint16_t>(p.dz), p.ldz, p.pz);
+        auto entries = [&](auto* kernel) {
+          hipLaunchKernelGGL(kernel, dim3((unsigned)per(a.M, 4)), dim3(256), 0, s, a, rows_at, n, at<const RowCoef>(p.rows),
+                             at<const float2>(p.weight), v0, nv, at<uint16_t>(p.dz), p.ldz, p.pz, rest());
+        };
+        if (p.two) entries(vocab_entry_kernel<2>);
+        else entries(vocab_entry_kernel<PL>);
         TRY(hipGetLastError());
       }
       if (a.dx) {
@@ -1198,6 +1268,11 @@ struct Tiles {
           default:
             if constexpr (PL == 1) TRY(data_grad<FewP>(w, nv, v0 == 0));
         }
+      }
+      if (a.fused && a.dx && rest()) {
+        hipLaunchKernelGGL(vocab_rest_kernel, dim3(grid_of(a.M * a.K)), dim3(256), 0, s, rest(), n, v0, nv, a.W.w_bf16, a.K,
+                           at<uint16_t>(p.kept), p.Kp);
+        TRY(hipGetLastError());
       }
       if (!a.fused && !a.dw) continue;
       HeadGrad g{};
@@ -1220,14 +1295,14 @@ struct Tiles {
       TRY(p.dw.shape == BIG ? head_grad<Big>(g, nv) : head_grad<Mid>(g, nv));
     }
     if (!a.dx) return hipSuccess;
-    const bool vec = a.K % 4 == 0 && a.ldx % 4 == 0 && ((uintptr_t)a.dx) % (a.gbf ? 8 : 16) == 0;
-    const float* part = at<const float>(p.pdx);
-    if (vec)
-      hipLaunchKernelGGL(vocab_dx_kernel<4>, dim3(grid_of(a.M * a.K / 4)), dim3(256), 0, s, part, p.dx.S, a.M, p.Kp, place, scale,
-                         a.K, a.dx, a.ldx, a.gbf ? 1 : 0);
-    else
-      hipLaunchKernelGGL(vocab_dx_kernel<1>, dim3(grid_of(a.M * a.K)), dim3(256), 0, s, part, p.dx.S, a.M, p.Kp, place, scale,
-                         a.K, a.dx, a.ldx, a.gbf ? 1 : 0);
+    const uint16_t* rw = a.fused ? at<uint16_t>(p.kept) : a.W.w_bf16;
+    const bool vec = a.K % 4 == 0 && a.ldx % 4 == 0 && ((uintptr_t)a.dx) % (a.gbf ? 8 : 16) == 0 && (PL == 3 || ((uintptr_t)rw) % 8 == 0);
+    const auto go = [&](auto* kernel, int each) {
+      hipLaunchKernelGGL(kernel, dim3(grid_of(a.M * a.K / each)), dim3(256), 0, s, at<const float>(p.pdx), p.dx.S, a.M, p.Kp, place,
+                         scale, a.K, a.dx, a.ldx, a.gbf ? 1 : 0, rest(), rw, a.fused ? p.Kp : a.K, a.fused ? 1 : 0);
+    };
+    if (vec) go(vocab_dx_kernel<4>, 4);
+    else go(vocab_dx_kernel<1>, 1);
     return hipGetLastError();
   }
 };
