@@ -596,7 +596,10 @@ __global__ __launch_bounds__(256) void vocab_prepared_kernel(VocabArgs a, int* a
 // A row's gradient is mostly its label's, and one rounding of that to bf16 (up to 2^-8) is a common factor of the
 // row's dX, where the others' roundings average out: what it leaves is kept (rest: id, value) and taken with W's
 // row when dX is stored.  dW adds rows up, which averages too unless they are few: up
-// to kFew of them have a second plane, which dW's reduction takes as more rows.
+// to kTwo of them have a second plane, which dW's reduction takes as more rows (backward, one plane / two, us: 64
+// rows over 5003 of width 320 26.5 / 27.2, over 32768 of 1024 61.9 / 65.1, 128 of those 82.3 / 97.9).
+constexpr int kTwo = 64;
+static_assert(kTwo <= kPrepared, "the second plane's rows follow the first's");
 template <class Shape_, int PL, bool TWO>
 struct GradEpi {
   static constexpr int NP = TWO ? 2 : PL;
@@ -1057,7 +1060,7 @@ TilesPlan tiles_plan(const VocabArgs& a, bool bwd) {
   // one size
   const int64_t room = std::max<int64_t>(256, (1LL << 28) / (p.Kp * p.PL) / 256 * 256);
   p.copied = std::min(up(per(a.V, per(a.V, room)), 256), up(a.V, 8));
-  p.two = bwd && a.bf16 && a.M <= kFew;
+  p.two = bwd && a.bf16 && a.M <= kTwo;
   p.px = a.M * p.Kp;
   p.x = take(p.px * (p.two ? 2 : p.PL) * 2);
   if (!bwd) {
@@ -1170,6 +1173,20 @@ struct Tiles {
                            prepared() && !a.dloss ? at<const float>(p.flag) : nullptr, (int)a.M, at<float>(p.scale), a.T, a.teacher ? nullptr : rest()};
     return product<T, PL, true, true>(w, Operand{at<uint16_t>(p.x), p.Kp, p.px}, n, a.M, a.K, at<int>(p.n), 1, e, s);
   }
+  template <bool TWO>
+  hipError_t shaped_grads(const Operand& w, int64_t v0, int64_t nv) const {
+    if constexpr (PL == 3 && TWO) {
+      return hipErrorInvalidValue;
+    } else {
+      switch (p.logits.shape) {
+        case BIG: return grads<Big, TWO>(w, v0, nv);
+        case MID: return grads<Mid, TWO>(w, v0, nv);
+        default:
+          if constexpr (PL == 1) return grads<FewQ, TWO>(w, v0, nv);
+          return hipErrorInvalidValue;
+      }
+    }
+  }
   template <class T>
   hipError_t data_grad(const Operand& w, int64_t n, bool first) const {
     const PartEpi<T, ROWS_P> e{at<float>(p.pdx), a.M, p.Kp, first ? 0 : 1};
@@ -1243,15 +1260,7 @@ struct Tiles {
       const int64_t nv = std::min(piece, a.V - v0);
       Operand w;
       TRY(head(v0, nv, &w));
-      switch (p.logits.shape) {
-        case BIG: TRY(grads<Big>(w, v0, nv)); break;
-        case MID: TRY(grads<Mid>(w, v0, nv)); break;
-        default:
-          if constexpr (PL == 1) {
-            if (p.two) TRY((grads<FewQ, true>(w, v0, nv)));
-            else TRY(grads<FewQ>(w, v0, nv));
-          }
-      }
+      TRY(p.two ? shaped_grads<true>(w, v0, nv) : shaped_grads<false>(w, v0, nv));
       if (a.teacher) {
         auto entries = [&](auto* kernel) {
           hipLaunchKernelGGL(kernel, dim3((unsigned)per(a.M, 4)), dim3(256), 0, s, a, rows_at, n, at<const RowCoef>(p.rows),
