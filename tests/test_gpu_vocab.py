@@ -359,6 +359,41 @@ def test_update_on_large_tiles(gpu, dtype):
     test_update(gpu, dtype, 1024, 16384, 1024, 0, OPTS[2])
 
 
+@pytest.mark.parametrize("M,k", [(3, 0), (64, 0), (65, 0), (200, 0), (500, 0), (3, 1), (64, 1), (500, 1)])
+def test_label_gradient_is_not_rounded(gpu, M, k):
+    """bf16: only one row of W is not zero, and every row's label is it, so that dX is the label's gradient times that
+    row: no rounding of the gradient to bf16 is left in it (u = 0), and up to 64 rows' dW has two planes (2^-16)."""
+    V, K = 300, 64
+    ids = torch.full((M, 1), 171)
+    c = Call(gpu, M, V, K, "bf16", k=k, T=2.0 if k else 1.0, grads="f32", given=True, ids=ids)
+    c.w[:171], c.w[172:] = 0, 0
+    c.dev_w.copy_(c.w)
+    c.fwd()
+    c.bwd()
+    r = c.reference(u=0.0)
+    near("dx", c.dx, r.dx, r.e_dx)
+    if M <= 64:
+        r = c.reference(u=2.0 ** -16)
+        near("dw", c.dw, r.dw, r.e_dw)
+    c.check_bwd()
+
+
+@pytest.mark.parametrize("k", [0, 2])
+def test_update_in_pieces(gpu, k):
+    """More logits than one piece of the gradient holds: dX is that of a stored gradient, from W before its update."""
+    M, V, K = 32768, 16384, 8
+    c = Call(gpu, M, V, K, "bf16", k=k, ids=torch.randint(0, V, (M, max(k, 1)), generator=torch.Generator().manual_seed(8)))
+    w = c.dev_w.float()
+    m, v = torch.zeros_like(w), torch.zeros_like(w)
+    c.fwd()
+    c.bwd()
+    dx = c.dx.clone()
+    c.param = L.OfParam(w.data_ptr(), m.data_ptr(), v.data_ptr(), c.dev_w.data_ptr(), V * K)
+    c.bwd_fused(L.make_opt(dict(OPTS[2], lr=0.1), 1))
+    assert torch.equal(c.dx, dx)
+    assert not torch.equal(c.dev_w.cpu(), c.w)
+
+
 @pytest.mark.parametrize("dtype,k", [("f32", 0), ("bf16", 0), ("f32", 5), ("bf16", 5)])
 def test_differences(gpu, dtype, k):
     """dX and dW against differences of the mean loss.
