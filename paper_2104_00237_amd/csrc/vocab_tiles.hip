@@ -1003,8 +1003,10 @@ struct Choice {
 // epilogue; parts are written and read again.  us, fitted to products of 512 to 32768 rows and columns.
 // few_p, few_q: the 32-wide tiles' rows and columns where they may be taken (bf16): they read operands more often, and
 // are the only ones to fill the chip with a few hundred rows over a small vocabulary (backward of 579 rows over
-// 338 of width 4160: 77 -> 52 us).
-Choice choose(int64_t P, int64_t Q, int64_t R, int planes, bool split, int few_p = 0, int few_q = 0) {
+// 338 of width 4160: 77 -> 52 us).  grads: the gradient's epilogue, whose code a large tile runs through once
+// (29 KB with 128 x 128, 11 with 128 x 32; whole backward, 128 x 128 / 128 x 32, us: 301 rows over 12345 of width
+// 257 70.2 / 60.9, 300 over 8192 of 512 47.6 / 38.1; 512 over 32768 of 1024, 256 x 256 / 128 x 32: 148 / 169).
+Choice choose(int64_t P, int64_t Q, int64_t R, int planes, bool split, int few_p = 0, int few_q = 0, bool grads = false) {
   Choice best{MID, 1};
   double least = 1e300;
   for (const Shape s : {BIG, MID, FEW}) {
@@ -1015,9 +1017,9 @@ Choice choose(int64_t P, int64_t Q, int64_t R, int planes, bool split, int few_p
       if (S > 1 && R / S < 128) break;
       const int64_t wg = tiles * S;
       const double stages = (double)up(per(per(R, 32), S) * (planes == 3 ? 6 : 1), s == FEW ? 8 : 4);
-      const double one = s == BIG   ? stages * 0.85 + 8
-                         : s == MID ? stages * (wg > 256 ? 0.58 : 0.36) + 4
-                                    : stages * (wg > 256 ? 0.3 : 0.18) + 4;
+      const double one = s == BIG   ? stages * 0.85 + (grads ? 30 : 8)
+                         : s == MID ? stages * (wg > 256 ? 0.58 : 0.36) + (grads ? 16 : 4)
+                                    : stages * (wg > 256 ? 0.3 : 0.18) + (grads ? 3 : 4);
       const double time = per(wg, s == BIG ? 256 : 512) * one + (S > 1 ? 2 + (double)P * Q * S * 8 / 4e6 : 0);
       if (time < least) least = time, best = Choice{s, S};
     }
@@ -1052,7 +1054,7 @@ TilesPlan tiles_plan(const VocabArgs& a, bool bwd) {
     here += (size_t)up(bytes, 256);
     return at;
   };
-  p.logits = a.M <= kFew && a.bf16 ? Choice{FEW, 1} : choose(a.V, a.M, a.K, p.PL, false, FewQ::BP, FewQ::BQ);
+  p.logits = a.M <= kFew && a.bf16 ? Choice{FEW, 1} : choose(a.V, a.M, a.K, p.PL, false, FewQ::BP, FewQ::BQ, bwd && a.bf16);
   p.BP = p.logits.shape == BIG ? 256 : 128;
   p.group = 32 * (p.logits.shape == BIG ? Big::IQ : p.logits.shape == MID ? Mid::IQ : FewQ::IQ);
   p.vtiles = per(a.V, p.BP), p.groups = per(a.M, p.group);
