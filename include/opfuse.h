@@ -823,7 +823,9 @@ of_status of_attn_bwd(const of_attn_desc* d, const void* q, const void* k, const
  *
  * A row that does not count has loss 0 and gives and gets no gradient, whatever its X holds; its lse is
  * that of its X.  A label or id >= V makes the row's loss NaN (and the mean); the row counts and gets no
- * gradient.  A logit of +infinity or NaN makes the row's lse NaN.
+ * gradient.  A logit of +infinity or NaN makes the row's lse NaN (fp32 operands on the matrix cores: an
+ * infinite element of X or W counts as 3.39e38 of its sign).  An infinite dloss makes its row's gradient
+ * infinite or NaN.
  *
  * dtype is the type in memory of X and of the head that is read (OF_F32: W->w; OF_BF16: W->w_bf16,
  * uint16 bit patterns) and of the matrix-core operands; logits, statistics and sums are fp32 or wider.
@@ -835,7 +837,9 @@ typedef struct of_vocab_desc {
   int64_t ldx;            /* row stride of X and dX; 0 means K; <= 2^21 */
   int32_t dtype;          /* of_dtype of X and W */
   int32_t grad_dtype;     /* backward: of_dtype of dX and dW (OF_BF16 only with dtype OF_BF16).  bf16 operands:
-                             the logits' gradient is rounded to bf16 as an operand, also for fp32 gradients */
+                             the logits' gradient is rounded to bf16 as an operand, also for fp32 gradients (but
+                             not the label's, or a row's largest such rounding, in dX; up to 64 rows: twice as
+                             many bits in dW) */
   int32_t topk;           /* distillation: entries of a row, 1 .. 1024; cross-entropy: 0 or 1 */
   int32_t teacher_dtype;  /* distillation: of_dtype of the teacher's logits */
   float softcap;          /* 0: none */
@@ -852,7 +856,7 @@ size_t of_vocab_workspace_size(const of_vocab_desc* d, int32_t op);
 /*
  * Forward.  loss, lse: fp32 [M]; zt: fp32 [M] (distillation [M, topk]): z of the label (of the entries), 0
  * where there is none; mean: fp32 [1] or NULL: the sum of the losses over the number of rows that
- * count (0 if none does).  lse and zt are kept for the backward.
+ * count (0 if none does).  The backward takes lse and zt as they are here.
  */
 of_status of_vocab_xent_fwd(const of_vocab_desc* d, const void* x, const of_param* W, const int64_t* labels,
                             float* loss, float* lse, float* zt, float* mean, void* ws, size_t ws_bytes, void* stream);

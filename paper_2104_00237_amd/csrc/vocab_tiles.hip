@@ -8,7 +8,8 @@
 // work); then per piece of the vocabulary the logits' product again, stored as their gradient in bf16,
 // dX summed over the pieces in fp32, dW (or the update) of the piece's rows; at the end dX rounded and
 // put back to its rows.  A common factor (T over the rows that count) is left out of the stored gradient
-// and applied to the sums: p - 1 near -1 then rounds to itself.
+// and applied to the sums: p - 1 near -1 then rounds to itself, and what rounding the label's still leaves is
+// added to dX's sums in fp32.
 // Six products' worth of flops for M V K instead of the four that stored logits would need.
 //
 // fp32 operands take the same way as three bf16 planes each (vocab_tile.h), made beforehand: X once, W
@@ -433,7 +434,10 @@ struct RowCoef {
   float zt;
 };
 __device__ __forceinline__ RowCoef row_coef(const VocabArgs& a, int64_t row, float lse, float ct, int label) {
-  return RowCoef{lse, __fmul_rn(ct, __fmaf_rn(2.f * a.z_loss, lse, 1.f)), ct, label, label >= 0 ? a.zt[row] : 0.f};
+  // (an infinite factor makes the row's gradient NaN: planes hold no infinity, and a loss scale's overflow must show)
+  float cp = __fmul_rn(ct, __fmaf_rn(2.f * a.z_loss, lse, 1.f));
+  if (fabsf(cp) == INFINITY || fabsf(ct) == INFINITY) cp = ct = NAN;
+  return RowCoef{lse, cp, ct, label, label >= 0 ? a.zt[row] : 0.f};
 }
 __global__ __launch_bounds__(1024) void vocab_index_kernel(VocabArgs a, const uint8_t* flag, int* at, int* place, int* n,
                                                            float* scale, RowCoef* rows) {
@@ -841,12 +845,24 @@ struct HeadEpi {
   HeadGrad g;
   template <class Acc>
   __device__ __forceinline__ void operator()(const TilePlace& t, Acc& acc, const Ring&, int lane, int, int wp, int wq) const {
+    if constexpr (UPDATE) {
+      // (the optimizer tested once, not at each element: update of 32768 x 1024 over 1024 fp32 rows 1184 -> 1166 us)
+      OptK o = g.opt;
+      opt_prepare(o);
+      if (o.kind == OF_OPT_ADAMW) run<OF_OPT_ADAMW>(t, acc, o, lane, wp, wq);
+      else if (o.kind == OF_OPT_ADAM) run<OF_OPT_ADAM>(t, acc, o, lane, wp, wq);
+      else run<-1>(t, acc, o, lane, wp, wq);
+    } else {
+      run<-1>(t, acc, g.opt, lane, wp, wq);
+    }
+  }
+  template <int KIND, class Acc>
+  __device__ __forceinline__ void run(const TilePlace& t, Acc& acc, OptK o, int lane, int wp, int wq) const {
+    if constexpr (KIND >= 0) o.kind = KIND;
     const int np = t.np - wp * T::IP * 32, nq = (int)min((int64_t)t.nq, g.K - t.q0) - wq * T::IQ * 32;
     const int h4 = (lane >> 5) * 4, l32 = lane & 31;
     const int64_t org = (int64_t)(t.p0 + wp * T::IP * 32) * g.K + t.q0 + wq * T::IQ * 32;
     const float scale = *g.scale;
-    OptK o = g.opt;
-    if constexpr (UPDATE) opt_prepare(o);
     // bf16: lanes 2l and 2l + 1 trade a value so that each stores two columns of a row
     const bool pair = !UPDATE && g.gbf && !g.accumulate && g.K % 2 == 0 && ((uintptr_t)g.dw & 3u) == 0;
     auto at = [&](int r) { return 8 * (r >> 2) + h4 + (r & 3); };

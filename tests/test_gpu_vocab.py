@@ -279,6 +279,26 @@ def test_infinite_and_nan_logits(gpu, dtype):
     near("lse", c.lse[keep.to(gpu)], r.lse[keep], r.e_lse[keep])
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,V,k", [(20, 300, 0), (90, 300, 0), (500, 300, 0), (20, 300, 3), (512, 5000, 0), (512, 5000, 3)])
+def test_infinite_gradients(gpu, dtype, M, V, k):
+    """A loss scale that overflowed shows: rows with an infinite gradient are infinite or NaN, the others are right."""
+    c = Call(gpu, M, V, 48, dtype, k=k, given=True)
+    c.fwd()
+    counts = c.reference().counts
+    rows = torch.nonzero(counts)[:, 0][::7]
+    c.dloss[rows] = math.inf
+    c.dev_dloss.copy_(c.dloss)
+    c.bwd()
+    c.dloss[rows] = 0.0
+    r = c.reference()
+    keep = torch.ones(M, dtype=torch.bool)
+    keep[rows] = False
+    assert not torch.isfinite(c.dx.cpu()[rows].float()).any()
+    assert not torch.isfinite(c.dw.float()).any()
+    near("dx", c.dx.cpu()[keep], r.dx[keep], r.e_dx[keep], TYPES[dtype][2])
+
+
 @pytest.mark.parametrize("dtype,grads", [("f32", "f32"), ("bf16", "bf16"), ("bf16", "f32")])
 @pytest.mark.parametrize("M,V,K", [(50, 200, 48), (260, 300, 129)])
 def test_parts_of_the_backward(gpu, M, V, K, dtype, grads):
