@@ -25,21 +25,8 @@ __device__ __forceinline__ float wave_max(float v) {
   return v;
 }
 
-// tanh(x) as x P(x^2) / Q(x^2), fitted in float64 for the least relative error on (0, 9] (2.1e-8; with fp32
-// rounding at most 3.2e-7, rms 5.3e-8, near 0 too, where 1 - 2 / (e^2x + 1) has nothing left); beyond 9 it
-// is 1 within half a step.  A third of tanhf's instructions: a capped tile of logits takes 65536 of them.
-__device__ __forceinline__ float vocab_tanh(float x) {
-  x = fabsf(x) > 9.f ? copysignf(9.f, x) : x;   // (a NaN stays)
-  const float u = __fmul_rn(x, x);
-  float p = 1.33548417e-08f, q = 7.77663388e-07f;
-  p = __fmaf_rn(p, u, 2.06092191e-05f), q = __fmaf_rn(q, u, 3.28564871e-04f);
-  p = __fmaf_rn(p, u, 3.49559658e-03f), q = __fmaf_rn(q, u, 2.58770157e-02f);
-  p = __fmaf_rn(p, u, 1.33810326e-01f), q = __fmaf_rn(q, u, 4.67143476e-01f);
-  p = __fmaf_rn(p, u, 1.f), q = __fmaf_rn(q, u, 1.f);
-  return __fmul_rn(__fmul_rn(x, p), __builtin_amdgcn_rcpf(q));
-}
-// The same for |x| <= 0.75 as x + x^3 R(x^2), fitted likewise (3.2e-8; with rounding at most 9.7e-8): half the
-// instructions again.
+// tanh(x) for |x| <= 0.75 as x + x^3 R(x^2), fitted in float64 for the least relative error (3.2e-8; with fp32
+// rounding at most 9.7e-8).
 constexpr float kTanhNear = 0.75f;
 __device__ __forceinline__ float vocab_tanh_near(float x) {
   const float u = __fmul_rn(x, x);
@@ -50,9 +37,30 @@ __device__ __forceinline__ float vocab_tanh_near(float x) {
   r = __fmaf_rn(r, u, -3.33330691e-01f);
   return __fmaf_rn(__fmul_rn(x, u), r, x);
 }
+// Anywhere: beyond 0.75 as 1 - 2 e / (1 + e) with e = exp(-2 |x|), which never exceeds 1 (at most 1.9e-7 of it off,
+// an ulp of the exponential and of the reciprocal counted; half a step of fp32 from |x| = 3 on).
+__device__ __forceinline__ float tanh_exp(float x) { return __builtin_amdgcn_exp2f(__fmul_rn(fabsf(x), -2.88539008f)); }
+__device__ __forceinline__ float vocab_tanh(float x) {
+  const float e = tanh_exp(x), far = __fmaf_rn(__fmul_rn(-2.f, e), __builtin_amdgcn_rcpf(__fadd_rn(1.f, e)), 1.f);
+  float near = vocab_tanh_near(x);
+  asm("" : "+v"(near));   // (both and a choice: the compiler makes a branch for every element of it)
+  return fabsf(x) <= kTanhNear ? near : copysignf(far, x);   // (a NaN stays: e is one)
+}
+// 1 - tanh(x)^2 with t = tanh(x), never negative.  Beyond 0.75 from x as 4 e / (1 + e)^2 (1.8e-6 of it off): what
+// a saturated t has left of 1 - t^2 is its rounding (2 % of it at x = 7, all of it from 9 on).
+__device__ __forceinline__ float tanh_slope(float x, float t) {
+  const float e = tanh_exp(x), r = __builtin_amdgcn_rcpf(__fadd_rn(1.f, e));
+  return fabsf(x) <= kTanhNear ? __fmaf_rn(-t, t, 1.f) : __fmul_rn(__fmul_rn(4.f * e, r), r);
+}
 // In full precision, for fp32 operands: a relative error of 1e-7 in a logit of 10 is one of 1e-6 in its
-// probability.
-__device__ __forceinline__ float vocab_cap_exact(float s, float cap) { return cap > 0.f ? __fmul_rn(cap, tanhf(__fdiv_rn(s, cap))) : s; }
+// probability.  slope: the cap's derivative there.
+__device__ __forceinline__ float vocab_cap_exact(float s, float cap, float* slope = nullptr) {
+  if (slope) *slope = 1.f;
+  if (cap <= 0.f) return s;
+  const float x = __fdiv_rn(s, cap), t = tanhf(x);
+  if (slope) *slope = tanh_slope(x, t);
+  return __fmul_rn(cap, t);
+}
 
 // A row's target as a wavefront sees it: entry j has weight exp(t_j / T - top) / total.
 // Entries with a negative id are left out whatever their logit; a row none of whose entries has a
@@ -151,13 +159,15 @@ __device__ __forceinline__ float row_loss(const VocabArgs& a, int64_t row, float
   return a.T * a.T * wave_sum(loss);
 }
 
-// The gradient at a place with logit z (capped): cp p - ct q, through the cap.
-__device__ __forceinline__ float place_grad(float T, float cap, float z, float lse, float cp, float ct, float q) {
+// The gradient at a place with logit z (capped): cp p - ct q, times the cap's slope there; that of an entry from its
+// capped logit, which is all that the forward keeps.
+__device__ __forceinline__ float place_grad(float T, float z, float slope, float lse, float cp, float ct, float q) {
   const float p = expf(__fsub_rn(__fdiv_rn(z, T), lse));
-  const float d = __fmaf_rn(cp, p, -__fmul_rn(ct, q));
-  if (cap <= 0.f) return d;
-  const float r = __fdiv_rn(z, cap);
-  return __fmul_rn(d, __fmaf_rn(-r, r, 1.f));
+  return __fmul_rn(__fmaf_rn(cp, p, -__fmul_rn(ct, q)), slope);
+}
+__device__ __forceinline__ float entry_grad(float T, float cap, float z, float lse, float cp, float ct, float q) {
+  const float r = cap > 0.f ? __fdiv_rn(z, cap) : 0.f;
+  return place_grad(T, z, __fmaf_rn(-r, r, 1.f), lse, cp, ct, q);
 }
 // An entry's logit for it: the forward's own where the one computed again agrees with it up to rounding.  Where an
 // entry has most of the probability, a rounding of its logit is in lse too and leaves p - q alone; another

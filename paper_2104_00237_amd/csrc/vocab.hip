@@ -121,9 +121,13 @@ __global__ __launch_bounds__(256) void vocab_grad_kernel(VocabArgs a, float* __r
     g = 1.f / fmaxf(red[0] + red[1] + red[2] + red[3], 1.f);
   }
   const float lse = a.lse[row], ct = __fmul_rn(c.x, g), cp = __fmul_rn(c.y, g);
-  auto grad = [&](float logit) { return place_grad(a.T, a.cap, vocab_cap_exact(logit, a.cap), lse, cp, 0.f, 0.f); };
+  auto grad = [&](float logit) {
+    float slope;
+    const float z = vocab_cap_exact(logit, a.cap, &slope);
+    return place_grad(a.T, z, slope, lse, cp, 0.f, 0.f);
+  };
   auto entry = [&](int64_t i, int place, float q) {
-    return place_grad(a.T, a.cap, entry_logit(vocab_cap_exact(s[place], a.cap), a.zt[i]), lse, cp, ct, q);
+    return entry_grad(a.T, a.cap, entry_logit(vocab_cap_exact(s[place], a.cap), a.zt[i]), lse, cp, ct, q);
   };
   const int64_t at = row * a.k;
   int where[EACH];

@@ -149,18 +149,26 @@ __device__ __forceinline__ float2 stat2_join(float2 x, float2 y, float c) {
                                   __fmul_rn(y.y, __builtin_amdgcn_exp2f(__fmul_rn(y.x - s, c)))));
 }
 
-// tanh of a block's logits over their cap.  Trained logits stay well inside it: a wavefront whose 1024 all
-// lie within 0.75 of it takes the short form.
-__device__ __forceinline__ void tanh_block(vacc_t& v, float rcap) {
+// tanh of a block's logits over their cap, and its slope there if asked for.  Trained logits stay well inside it: a
+// wavefront whose 1024 all lie within 0.75 of it takes the short form.
+__device__ __forceinline__ void tanh_block(vacc_t& v, float rcap, float* slope = nullptr) {
   float m = 0.f;
 #pragma unroll
   for (int r = 0; r < 16; ++r) m = fmaxf(m, fabsf(v[r]));
   if (__all(m * rcap <= kTanhNear)) {
 #pragma unroll
-    for (int r = 0; r < 16; ++r) v[r] = vocab_tanh_near(__fmul_rn(v[r], rcap));
+    for (int r = 0; r < 16; ++r) {
+      v[r] = vocab_tanh_near(__fmul_rn(v[r], rcap));
+      if (slope) slope[r] = __fmaf_rn(-v[r], v[r], 1.f);
+    }
   } else {
 #pragma unroll
-    for (int r = 0; r < 16; ++r) v[r] = vocab_tanh(__fmul_rn(v[r], rcap));
+    for (int r = 0; r < 16; ++r) {
+      const float x = __fmul_rn(v[r], rcap);
+      v[r] = vocab_tanh(x);
+      if (slope) slope[r] = tanh_slope(x, v[r]);
+      if (r % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // (no more of them at a time than there are registers for)
+    }
   }
 }
 // A block's logits capped.
@@ -646,28 +654,28 @@ struct GradEpi {
         constexpr bool capped = decltype(Capped)::value;
         // bf16 operands: what is left of the logit is tanh alone, and lse is taken off in units of log2 (its
         // rounding there, 1e-6 of a probability, is nothing beside bf16's)
-        if constexpr (capped && PL == 1) tanh_block(acc[i][j], rcap);
+        float slope[16];
+        if constexpr (capped && PL == 1) tanh_block(acc[i][j], rcap, slope);
         float at_label = 0.f;
         const float c2 = rT * kLog2E * (capped ? cap : 1.f), lse2 = rc[j].lse * kLog2E;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          float d, z, x = 0.f;   // x: the logit over its cap
+          float d, z;
           if constexpr (PL == 1) {
-            x = acc[i][j][r];
+            const float x = acc[i][j][r];   // the logit over its cap
             z = capped ? __fmul_rn(cap, x) : x;
             d = __builtin_amdgcn_exp2f(__fmaf_rn(x, c2, -lse2));
           } else {
-            z = vocab_cap_exact(acc[i][j][r], capped ? cap : 0.f);
-            x = __fmul_rn(z, rcap);
+            z = vocab_cap_exact(acc[i][j][r], capped ? cap : 0.f, &slope[r]);
             d = __builtin_amdgcn_exp2f(__fmul_rn(kLog2E, __fmaf_rn(z, rT, -rc[j].lse)));
           }
           d = __fmul_rn(d, rc[j].cp);
-          d = capped ? __fmul_rn(d, __fmaf_rn(-x, x, 1.f)) : d;
+          d = capped ? __fmul_rn(d, slope[r]) : d;
           acc[i][j][r] = d;
           if (here) at_label = 8 * (r >> 2) + (r & 3) == label ? z : at_label;
         }
         if (here) {
-          const float d = place_grad(T, cap, entry_logit(at_label, rc[j].zt), rc[j].lse, rc[j].cp, rc[j].ct, 1.f);
+          const float d = entry_grad(T, cap, entry_logit(at_label, rc[j].zt), rc[j].lse, rc[j].cp, rc[j].ct, 1.f);
 #pragma unroll
           for (int r = 0; r < 16; ++r) acc[i][j][r] = 8 * (r >> 2) + (r & 3) == label ? d : acc[i][j][r];
           if (rest && label >= 0 && label < 32 && !(label & 4)) {
@@ -769,7 +777,7 @@ __global__ __launch_bounds__(256) void vocab_entry_kernel(VocabArgs a, const int
     }
     if (!lead) continue;
     uint16_t* d = dz + (int64_t)i * ldz + place;
-    float x = place_grad(a.T, a.cap, a.zt[first + j], rc.lse, rc.cp, rc.ct, q), y = 0.f;
+    float x = entry_grad(a.T, a.cap, a.zt[first + j], rc.lse, rc.cp, rc.ct, q), y = 0.f;
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
       d[p * plane] = (uint16_t)take_part(x, y);

@@ -1,0 +1,57 @@
+"""of_vocab_xent_* and of_vocab_distill_* where values or batches leave the ordinary: logits at their cap, operands and
+gradients that are not finite, batches whose rows are gathered, other logits than the backward's own."""
+import math
+
+import pytest
+import torch
+
+from paper_2104_00237_amd import _lib as L
+from tests.test_gpu_vocab import TYPES, Call
+
+pytestmark = pytest.mark.gpu
+E = 2.0 ** -24
+
+
+@pytest.mark.parametrize("dtype,grads", [("f32", "f32"), ("bf16", "bf16"), ("bf16", "f32")])
+@pytest.mark.parametrize("M,V,k", [(40, 300, 0), (40, 300, 3), (300, 700, 0), (512, 5000, 0), (512, 5000, 2), (2048, 8192, 0)])
+def test_logits_at_their_cap(gpu, M, V, k, dtype, grads):
+    """All logits between 4 and 9.5 caps: none leaves the cap, and a gradient keeps its sign and most of its bits where
+    1 - tanh^2 has none left.
+
+    Column 0 of X is 1 and the only one of W that is not zero, so that dW there is the sum of the rows' ds.  Relative
+    to it: the slope 2^-18 and 2 |x| roundings of its argument (2^-17 in all), a probability's z and lse (the largest
+    exponent's 4 E cap twice, 277 E of the sums, 8 E (1 + |z| + |lse|)), the sum's M E, roundings u to the type.  An entry's slope
+    comes from its stored z, which is 6 E of the cap off."""
+    cap = 2.0
+    c = Call(gpu, M, V, 8, dtype, k=k, cap=cap, given=True, grads=grads, ids=torch.arange(max(k, 1)).repeat(M, 1))
+    s = cap * torch.linspace(4.0, 9.5, V)
+    s[1::2] *= -1
+    s[:max(k, 1)] = 4.5 * cap + torch.arange(max(k, 1))
+    c.w.zero_(), c.x.zero_()
+    c.w[:, 0], c.x[:, 0] = s.to(c.w.dtype), 1
+    c.dev_w.copy_(c.w), c.dev_x.copy_(c.x)
+    c.dev_dloss.fill_(2.0 ** -11)
+    c.fwd()
+    c.bwd()
+    s = c.w[:, 0].double()
+    z = cap * torch.tanh(s / cap)
+    e = torch.exp(-2 * s.abs() / cap)
+    slope = 4 * e / (1 + e) ** 2
+    p = torch.softmax(z, 0)
+    q = torch.zeros(M, V).double()
+    if k:
+        q.scatter_(1, c.ids, torch.softmax(c.teacher.double(), 1))
+    else:
+        q[:, 0] = 1
+    d = 2.0 ** -11 * (M * p - q.sum(0)) * slope
+    got = c.dw[:, 0].double().cpu()
+    u, half = TYPES[dtype][2], TYPES[grads][2]
+    rel = u + half + (2 * 4 * cap + 277 + V / 64 + 8 * 12 + M) * E + 2.0 ** -17
+    bound = 1.01 * rel * d.abs()
+    n = max(k, 1)
+    bound[:n] += 1.01 * 2.0 ** -11 * M * 16 * E
+    assert (c.zt.abs() <= cap).all()
+    assert (got[n:] >= 0).all(), got[n:].min()
+    assert (got[:n] <= 0).all()
+    over = (got - d).abs() - bound - 1e-38
+    assert (over <= 0).all(), (float(over.max()), int(over.argmax()), float(got[over.argmax()]), float(d[over.argmax()]))
