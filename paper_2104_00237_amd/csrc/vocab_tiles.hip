@@ -646,6 +646,8 @@ struct GradEpi {
     }
     auto fill = [&](auto J_, auto Capped) __attribute__((always_inline)) {
       constexpr int j = decltype(J_)::value;
+      // a row without a gradient (a prepared one that does not count, of zeros) keeps nothing of an infinite W
+      const bool none = rc[j].cp == 0.f && rc[j].ct == 0.f, some_none = __any(none);
       each(std::make_integer_sequence<int, IP>{}, [&](auto I_) __attribute__((always_inline)) {
         constexpr int i = decltype(I_)::value;
         // the label among this block's entries
@@ -674,8 +676,12 @@ struct GradEpi {
           acc[i][j][r] = d;
           if (here) at_label = 8 * (r >> 2) + (r & 3) == label ? z : at_label;
         }
+        if (some_none) {
+#pragma unroll
+          for (int r = 0; r < 16; ++r) acc[i][j][r] = none ? 0.f : acc[i][j][r];
+        }
         if (here) {
-          const float d = entry_grad(T, cap, entry_logit(at_label, rc[j].zt), rc[j].lse, rc[j].cp, rc[j].ct, 1.f);
+          const float d = none ? 0.f : entry_grad(T, cap, entry_logit(at_label, rc[j].zt), rc[j].lse, rc[j].cp, rc[j].ct, 1.f);
 #pragma unroll
           for (int r = 0; r < 16; ++r) acc[i][j][r] = 8 * (r >> 2) + (r & 3) == label ? d : acc[i][j][r];
           if (rest && label >= 0 && label < 32 && !(label & 4)) {

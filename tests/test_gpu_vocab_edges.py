@@ -7,6 +7,7 @@ import torch
 
 from paper_2104_00237_amd import _lib as L
 from tests.test_gpu_vocab import TYPES, Call
+from tests.vocab_reference import near
 
 pytestmark = pytest.mark.gpu
 E = 2.0 ** -24
@@ -55,3 +56,30 @@ def test_logits_at_their_cap(gpu, M, V, k, dtype, grads):
     assert (got[:n] <= 0).all()
     over = (got - d).abs() - bound - 1e-38
     assert (over <= 0).all(), (float(over.max()), int(over.argmax()), float(got[over.argmax()]), float(d[over.argmax()]))
+
+
+@pytest.mark.parametrize("M,V", [(9, 100), (50, 300), (300, 1000), (300, 8000), (500, 700), (512, 5000)])
+@pytest.mark.parametrize("dtype,k", [("bf16", 0), ("bf16", 2)])
+def test_rows_that_do_not_count_beside_an_infinite_head(gpu, M, V, dtype, k):
+    """An entry that a head rules out (W of -infinity where every X is 1: probability 0) gets a gradient of exactly 0, with
+    rows that do not count among the others, with gradients of 0, and where no row counts."""
+    c = Call(gpu, M, V, 16, dtype, k=k, given=True)
+    c.ids[::3] = -1
+    c.ids[c.ids >= V - 3] = 0
+    c.x[:, 0] = 1
+    c.w[:, 0] = 0
+    c.w[V - 2, 0] = -math.inf
+    c.dloss[1::6] = 0.0
+    for a, b in ((c.t[0], c.ids), (c.dev_x, c.x), (c.dev_w, c.w), (c.dev_dloss, c.dloss)):
+        a.copy_(b)
+    c.fwd()
+    c.bwd(dx=False)
+    c.w[V - 2, 0] = -3e4
+    r = c.reference()
+    near("dw", c.dw, r.dw, r.e_dw, TYPES[dtype][2])
+    assert (c.dw[V - 2] == 0).all()
+    c.ids[:] = -1
+    c.t[0].copy_(c.ids)
+    c.fwd()
+    c.bwd()
+    assert (c.dw == 0).all() and (c.dx == 0).all()
