@@ -821,7 +821,7 @@ of_status of_attn_bwd(const of_attn_desc* d, const void* q, const void* k, const
  * A row without an entry, or with logits of -infinity only, does not count.  An id that stands more than
  * once has the weights of all its entries in the gradient, and a term for each in the loss.
  *
- * A row that does not count has loss 0 and gives and gets no gradient, whatever its X holds; its lse is
+ * A row that does not count has loss 0 and gives and gets no gradient, whatever its X or W holds; its lse is
  * that of its X.  A label or id >= V makes the row's loss NaN (and the mean); the row counts and gets no
  * gradient.  A logit of +infinity or NaN makes the row's lse NaN (fp32 operands on the matrix cores: an
  * infinite element of X or W counts as 3.39e38 of its sign).  An infinite dloss makes its row's gradient

@@ -89,12 +89,20 @@ __global__ __launch_bounds__(256) void vocab_prepare_kernel(VocabArgs a, float2*
       const float g = live ? (a.dloss ? a.dloss[row] : 1.f) * a.T : 0.f;
       coef[row] = make_float2(g, live ? __fmul_rn(g, __fmaf_rn(2.f * a.z_loss, a.lse[row], 1.f)) : 0.f);
       counts[row] = r.counts ? 1.f : 0.f;
+      counts[a.M + row] = live ? 1.f : 0.f;
       on = live;
     }
   }
   __syncthreads();
   const float* src = (const float*)a.x + row * a.ldx;
   for (int64_t c = t; c < a.K; c += 256) x[row * a.K + c] = on ? src[c] : 0.f;
+}
+
+// dX of rows that get no gradient: zeros, where the products' zeros times an infinite or NaN W are NaN.
+__global__ __launch_bounds__(64) void vocab_clear_kernel(VocabArgs a, const float* live) {
+  const int64_t row = blockIdx.x;
+  if (live[row] != 0.f) return;
+  for (int64_t i = threadIdx.x; i < a.K; i += 64) ((float*)a.dx)[row * a.ldx + i] = 0.f;
 }
 
 // The gradient of a chunk of a row's logits, in place of them.  An entry's place is written by its first
@@ -212,7 +220,7 @@ Plan plan_of(const VocabArgs& a, bool bwd) {
   }
   p.gemm = take(g);
   if (bwd) {
-    p.counts = take((size_t)a.M * 4);
+    p.counts = take((size_t)a.M * 8);   // rows that count, and those with a gradient
     p.coef = take((size_t)a.M * 8);
     p.x = take((size_t)a.M * a.K * 4);
   } else {
@@ -323,7 +331,8 @@ hipError_t vocab_bwd_launch(const VocabArgs& a, void* ws, hipStream_t s) {
       TRY(g.product(EPI_WGRAD, pr, ea));
     }
   }
-  return hipSuccess;
+  if (a.dx) hipLaunchKernelGGL(vocab_clear_kernel, dim3((unsigned)a.M), dim3(64), 0, s, a, counts + a.M);
+  return hipGetLastError();
 }
 
 }  // namespace opfuse

@@ -59,7 +59,7 @@ def test_logits_at_their_cap(gpu, M, V, k, dtype, grads):
 
 
 @pytest.mark.parametrize("M,V", [(9, 100), (50, 300), (300, 1000), (300, 8000), (500, 700), (512, 5000)])
-@pytest.mark.parametrize("dtype,k", [("bf16", 0), ("bf16", 2)])
+@pytest.mark.parametrize("dtype,k", [("f32", 0), ("bf16", 0), ("f32", 2), ("bf16", 2)])
 def test_rows_that_do_not_count_beside_an_infinite_head(gpu, M, V, dtype, k):
     """An entry that a head rules out (W of -infinity where every X is 1: probability 0) gets a gradient of exactly 0, with
     rows that do not count among the others, with gradients of 0, and where no row counts."""
