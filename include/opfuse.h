@@ -823,8 +823,8 @@ of_status of_attn_bwd(const of_attn_desc* d, const void* q, const void* k, const
  *
  * A row that does not count has loss 0 and gives and gets no gradient, whatever its X or W holds; its lse is
  * that of its X.  A label or id >= V makes the row's loss NaN (and the mean); the row counts and gets no
- * gradient.  A logit of +infinity or NaN makes the row's lse NaN (fp32 operands on the matrix cores: an
- * infinite element of X or W counts as 3.39e38 of its sign).  An infinite dloss makes its row's gradient
+ * gradient.  A logit of +infinity or NaN makes the row's lse NaN, one of -infinity has probability 0 (fp32
+ * operands: the product of two infinite elements may be NaN).  An infinite dloss makes its row's gradient
  * infinite or NaN.
  *
  * dtype is the type in memory of X and of the head that is read (OF_F32: W->w; OF_BF16: W->w_bf16,

@@ -19,7 +19,8 @@
 // nearest bf16 to what the ones before leave (the splitting of Henry, Tang and Heinecke, Leveraging the
 // bfloat16 Artificial Intelligence Datatype For Higher-Precision Computations, ARITH 2019).  Parts shrink
 // by 2^-9, so three hold all 24 bits, and of the nine partial products the three below 2^-26 of the
-// whole are left out: six are summed in one accumulator.
+// whole are left out: six are summed in one accumulator.  An infinite x is (0, 0, x): its low part meets the
+// other operand's high part alone.
 #pragma once
 
 #include <type_traits>

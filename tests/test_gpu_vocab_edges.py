@@ -83,3 +83,51 @@ def test_rows_that_do_not_count_beside_an_infinite_head(gpu, M, V, dtype, k):
     c.fwd()
     c.bwd()
     assert (c.dw == 0).all() and (c.dx == 0).all()
+
+
+@pytest.mark.parametrize("dtype,M,V,k", [("f32", 12, 90, 0), ("f32", 512, 9000, 0), ("f32", 1030, 16384, 2), ("bf16", 12, 90, 0),
+                                         ("bf16", 512, 5000, 2)])
+def test_infinite_operands(gpu, dtype, M, V, k):
+    """At every size the same: an infinite X or W that gives a row a logit of +infinity (or a NaN) makes its lse, loss and
+    gradient NaN; one that gives -infinity leaves a probability of 0; other rows are as without it."""
+    K, row = 16, 7
+    c = Call(gpu, M, V, K, dtype, k=k, given=True, ids=None if k else torch.arange(M)[:, None] % (V - 40))
+    c.ids[c.ids >= V - 40] = 1
+    c.w[:, 0], c.x[:, 0] = 0, 1
+    c.w[V - 20, 0] = -math.inf          # probability 0, but for X of 0 there: NaN
+    nan = torch.zeros(M, dtype=torch.bool)
+    nan[[2, 5, row, M - 1]] = True
+    c.x[2, 0] = 0                       # 0 * -infinity
+    c.x[5, 0] = -1                      # +infinity
+    c.x[row, 3] = math.inf             # with W of both signs there
+    c.x[M - 1, 4] = -math.inf
+    c.ids[[2, 5, row, M - 1], 0] = 3
+    for a, b in ((c.t[0], c.ids), (c.dev_x, c.x), (c.dev_w, c.w)):
+        a.copy_(b)
+    c.fwd()
+    assert (c.lse.isnan().cpu() == nan).all()
+    assert (c.loss.isnan().cpu() == nan).all() and c.mean.isnan().all()
+    c.bwd()
+    assert not torch.isfinite(c.dx.cpu()[nan].float()).any() and not torch.isfinite(c.dw.float()).any()
+    clean_x, keep = c.x.clone(), ~nan
+    clean_x[nan] = 0
+    c.w[V - 20, 0] = -3e4
+    r = c.reference(x=clean_x)
+    near("lse", c.lse[keep.to(gpu)], r.lse[keep], r.e_lse[keep])
+    near("loss", c.loss[keep.to(gpu)], r.loss[keep], r.e_loss[keep])
+    near("dx", c.dx.cpu()[keep, 1:], r.dx[keep, 1:], r.e_dx[keep, 1:], TYPES[dtype][2])
+    counts = keep & r.counts
+    assert c.dx.cpu()[counts, 0].isnan().all()    # 0 * -infinity, as the product has it
+    assert (c.dx.cpu()[~r.counts] == 0).all()
+
+
+@pytest.mark.parametrize("M,V", [(12, 90), (512, 9000), (1030, 16384)])
+def test_largest_operands(gpu, M, V):
+    """fp32 operands up to the largest fp32 value keep all their bits."""
+    c = Call(gpu, M, V, 16, "f32", ids=torch.arange(M)[:, None] % V)
+    c.x[:, 0] = torch.linspace(3.3e38, 3.4028234e38, M)
+    c.w[:, 0] = 0
+    c.w[1::2, 0] = 2.0 ** -126 * 1.5
+    c.dev_x.copy_(c.x), c.dev_w.copy_(c.w)
+    c.fwd()
+    c.check_fwd()
