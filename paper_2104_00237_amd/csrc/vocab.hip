@@ -106,7 +106,7 @@ __global__ __launch_bounds__(64) void vocab_clear_kernel(VocabArgs a, const floa
 }
 
 // The gradient of a chunk of a row's logits, in place of them.  An entry's place is written by its first
-// entry with the weights of all that name it; its logit is read before the row is overwritten.
+// entry with the weights of all that name it.
 __global__ __launch_bounds__(256) void vocab_grad_kernel(VocabArgs a, float* __restrict__ z, int64_t ldz, int64_t v0, int n,
                                                          const float2* coef, const float* counts) {
   constexpr int EACH = kTopMax / 256;
@@ -134,9 +134,7 @@ __global__ __launch_bounds__(256) void vocab_grad_kernel(VocabArgs a, float* __r
     const float z = vocab_cap_exact(logit, a.cap, &slope);
     return place_grad(a.T, z, slope, lse, cp, 0.f, 0.f);
   };
-  auto entry = [&](int64_t i, int place, float q) {
-    return entry_grad(a.T, a.cap, entry_logit(vocab_cap_exact(s[place], a.cap), a.zt[i]), lse, cp, ct, q);
-  };
+  auto entry = [&](int64_t i, float q) { return entry_grad(a.T, a.cap, a.zt[i], lse, cp, ct, q); };
   const int64_t at = row * a.k;
   int where[EACH];
   float d[EACH];
@@ -144,7 +142,7 @@ __global__ __launch_bounds__(256) void vocab_grad_kernel(VocabArgs a, float* __r
     where[0] = -1;
     if (t == 0) {
       const int64_t id = a.ids[row] - v0;
-      if (id >= from && id < end) where[0] = (int)id, d[0] = entry(row, (int)id, 1.f);
+      if (id >= from && id < end) where[0] = (int)id, d[0] = entry(row, 1.f);
     }
 #pragma unroll
     for (int u = 1; u < EACH; ++u) where[u] = -1;
@@ -166,7 +164,7 @@ __global__ __launch_bounds__(256) void vocab_grad_kernel(VocabArgs a, float* __r
       }
       if (!first) continue;
       where[u] = (int)(id - v0);
-      d[u] = entry(at + j, (int)(id - v0), q);
+      d[u] = entry(at + j, q);
     }
   }
   Chunk k;
