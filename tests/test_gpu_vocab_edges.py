@@ -158,3 +158,32 @@ def test_backward_takes_the_forwards_lse_and_logits(gpu, dtype, k, M, V, K):
     e = e * f + (TYPES[dtype][2] + 8 * E) * d.abs() + 1e-38
     near("dx", c.dx, d @ w, e @ w.abs() + (V + 8) * E * (d.abs() @ w.abs()))
     near("dw", c.dw, d.t() @ x, e.t() @ x.abs() + (M + 8) * E * (d.abs().t() @ x.abs()))
+
+
+@pytest.mark.parametrize("M,V,k", [(2048, 90, 0), (2049, 90, 0), (3000, 90, 3), (20000, 40, 0)])
+def test_many_rows_over_few_entries(gpu, M, V, k):
+    """fp32, the mean's gradient: how many rows count is the same for all of them."""
+    c = Call(gpu, M, V, 24, "f32", k=k)
+    c.fwd()
+    c.bwd()
+    c.check_fwd()
+    c.check_bwd()
+
+
+def test_time_grows_with_the_rows(gpu):
+    """16 times the rows in less than 40 times the time (a workgroup a row that looks at all rows: 150 times)."""
+    best = []
+    for M in (1 << 14, 1 << 18):
+        c = Call(gpu, M, 4, 32, "f32", ids=torch.randint(-1, 4, (M, 1), generator=torch.Generator().manual_seed(1)))
+        c.fwd()
+        c.bwd()
+        times = []
+        for _ in range(5):
+            start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            start.record()
+            c.bwd()
+            end.record()
+            end.synchronize()
+            times.append(start.elapsed_time(end))
+        best.append(min(times))
+    assert best[1] < 40 * best[0], best
