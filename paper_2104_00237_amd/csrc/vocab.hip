@@ -134,6 +134,7 @@ __global__ __launch_bounds__(256) void vocab_grad_kernel(VocabArgs a, float* __r
                                                          const float2* coef, const float* counts, const float* total) {
   constexpr int EACH = kTopMax / 256;
   __shared__ float red[4];
+  __shared__ __attribute__((aligned(16))) int places[kTopMax];   // of the entries in this chunk, or -1
   const int64_t row = blockIdx.x;
   const int t = threadIdx.x, from = blockIdx.y * kChunk, end = min(n, from + kChunk);
   float* s = z + row * ldz;
@@ -173,23 +174,32 @@ __global__ __launch_bounds__(256) void vocab_grad_kernel(VocabArgs a, float* __r
     for (int u = 1; u < EACH; ++u) where[u] = -1;
   } else {
     const RowTarget r = row_target(a, row, t & 63);
+    const int k4 = (a.k + 3) & ~3;
+    for (int j = t; j < k4; j += 256) {
+      const int64_t id = j < a.k ? a.ids[at + j] - v0 : -1;
+      places[j] = id >= from && id < end ? (int)id : -1;
+    }
+    __syncthreads();
 #pragma unroll
     for (int u = 0; u < EACH; ++u) {
-      where[u] = -1;
       const int j = t + u * 256;
-      if (j >= a.k) continue;
-      const int64_t id = a.ids[at + j];
-      if (id < v0 + from || id >= v0 + end) continue;
-      float q = 0.f;
+      where[u] = j < a.k ? places[j] : -1;
+      if (where[u] < 0) continue;
+      // (entries that name one place twice are rare: four compares an LDS read, weights only where one matches)
+      float q = r.weight(teacher_logit(a, at + j));
       bool first = true;
-      for (int i = 0; i < a.k; ++i) {
-        if (a.ids[at + i] != id) continue;
-        first &= i >= j;
-        q = __fadd_rn(q, r.weight(teacher_logit(a, at + i)));
+      for (int i = 0; i < k4; i += 4) {
+        const int4 p = *reinterpret_cast<const int4*>(&places[i]);
+        const int x[4] = {p.x, p.y, p.z, p.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          if (x[e] != where[u] || i + e == j) continue;
+          first &= i + e > j;
+          q = __fadd_rn(q, r.weight(teacher_logit(a, at + i + e)));
+        }
       }
-      if (!first) continue;
-      where[u] = (int)(id - v0);
-      d[u] = entry(at + j, q);
+      if (first) d[u] = entry(at + j, q);
+      else where[u] = -1;
     }
   }
   Chunk k;

@@ -187,3 +187,15 @@ def test_time_grows_with_the_rows(gpu):
             times.append(start.elapsed_time(end))
         best.append(min(times))
     assert best[1] < 40 * best[0], best
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("M,V,k", [(20, 700, 1024), (20, 9000, 1023), (33, 5000, 257), (450, 600, 301)])
+def test_many_entries(gpu, dtype, M, V, k):
+    """More entries than a workgroup has lanes, some named twice, over one and over several chunks of logits."""
+    ids = torch.randint(-1, V, (M, k), generator=torch.Generator().manual_seed(k))
+    c = Call(gpu, M, V, 40, dtype, k=k, ids=ids, T=1.5)
+    c.fwd()
+    c.bwd()
+    c.check_fwd()
+    c.check_bwd()
