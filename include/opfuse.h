@@ -829,7 +829,8 @@ of_status of_attn_bwd(const of_attn_desc* d, const void* q, const void* k, const
  *
  * dtype is the type in memory of X and of the head that is read (OF_F32: W->w; OF_BF16: W->w_bf16,
  * uint16 bit patterns) and of the matrix-core operands; logits, statistics and sums are fp32 or wider.
- * Any alignment to the elements' size is accepted; rows of 16-byte pieces save a copy.  M * V < 2^37,
+ * Any alignment to the elements' size is accepted; bf16 rows of 16-byte pieces (K and ldx multiples of 8) save a
+ * copy, and its workspace with `aligned`.  M * V < 2^37,
  * V * K <= 2^36, M * K < 2^29, X < 2 GiB.
  */
 typedef struct of_vocab_desc {
@@ -845,6 +846,8 @@ typedef struct of_vocab_desc {
   float softcap;          /* 0: none */
   float z_loss;           /* cross-entropy: >= 0; distillation: 0 */
   float temperature;      /* distillation: > 0, 0 means 1; cross-entropy: 0 or 1 */
+  int32_t aligned;        /* 1: X and the W that is read are 16-byte aligned (a call with others is refused), so that the
+                             workspace has no room for copies of bf16 ones whose rows are 16-byte pieces; 0: either */
 } of_vocab_desc;
 
 typedef enum of_vocab_op { OF_VOCAB_FWD = 0, OF_VOCAB_BWD = 1 /* bwd and bwd_fused */ } of_vocab_op;

@@ -101,7 +101,7 @@ OF_VOCAB_FWD, OF_VOCAB_BWD = 0, 1
 class OfVocabDesc(ctypes.Structure):
     _fields_ = [("M", c_int64), ("V", c_int64), ("K", c_int64), ("ldx", c_int64), ("dtype", c_int32),
                 ("grad_dtype", c_int32), ("topk", c_int32), ("teacher_dtype", c_int32), ("softcap", c_float),
-                ("z_loss", c_float), ("temperature", c_float)]
+                ("z_loss", c_float), ("temperature", c_float), ("aligned", c_int32)]
 
 
 class OpfuseError(RuntimeError):

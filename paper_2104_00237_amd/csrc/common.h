@@ -495,6 +495,7 @@ struct VocabArgs {
   bool tbf;                        // the teacher's logits are bf16
   int k;
   float cap, rcap, z_loss, T;      // cap 0: none; rcap = 1 / cap
+  bool aligned, entries;           // X and W are 16-byte aligned; the descriptor has entries (distillation may be meant)
   float *loss, *lse, *zt, *mean;   // forward: [M], [M], [M, k], [1] or NULL
   // backward
   const float* dloss;              // [M] or NULL: the mean's

@@ -1409,6 +1409,7 @@ of_status check_vocab(const of_vocab_desc* d, bool bwd, VocabArgs* a) {
             "softcap and temperature must be 0 or in [2^-40, 2^40]");
   }
   REQUIRE(std::isfinite(d->z_loss) && d->z_loss >= 0.f, OF_EINVAL, "z_loss must be finite and >= 0");
+  REQUIRE(d->aligned == 0 || d->aligned == 1, OF_EINVAL, "aligned must be 0 or 1");
   memset(a, 0, sizeof(*a));
   a->M = d->M, a->V = d->V, a->K = d->K;
   a->ldx = d->ldx ? d->ldx : d->K;
@@ -1427,6 +1428,8 @@ of_status check_vocab(const of_vocab_desc* d, bool bwd, VocabArgs* a) {
   a->gbf = d->grad_dtype == OF_BF16;
   a->tbf = d->teacher_dtype == OF_BF16;
   a->k = std::max<int32_t>(d->topk, 1);
+  a->entries = d->topk > 0;
+  a->aligned = d->aligned != 0;
   a->cap = d->softcap;
   a->rcap = a->cap ? 1.f / a->cap : 0.f;
   a->z_loss = d->z_loss;
@@ -1452,6 +1455,8 @@ of_status check_vocab_call(const of_vocab_desc* d, bool bwd, bool distill, const
   REQUIRE(W->numel == a->V * a->K, OF_EINVAL, "W->numel is %lld, expected V * K = %lld", (long long)W->numel,
           (long long)(a->V * a->K));
   REQUIRE(aligned_to(x, es) && aligned_to(w, es), OF_EALIGN, "x and W must be %d-byte aligned", (int)es);
+  REQUIRE(!a->aligned || (aligned_to(x, 16) && aligned_to(w, 16)), OF_EALIGN,
+          "x and W must be 16-byte aligned, as the descriptor says");
   REQUIRE(aligned_to(ids, 8), OF_EALIGN, "labels and ids must be 8-byte aligned");
   REQUIRE(!distill || aligned_to(teacher, a->tbf ? 2 : 4), OF_EALIGN, "teacher must be %d-byte aligned", a->tbf ? 2 : 4);
   REQUIRE(al4(lse) && al4(zt), OF_EALIGN, "lse and zt must be 4-byte aligned");

@@ -1093,12 +1093,13 @@ TilesPlan tiles_plan(const VocabArgs& a, bool bwd) {
   p.copied = std::min(up(per(a.V, per(a.V, room)), 256), up(a.V, 8));
   p.two = bwd && a.bf16 && a.M <= kTwo;
   p.px = a.M * p.Kp;
-  p.x = take(p.px * (p.two ? 2 : p.PL) * 2);
+  const bool whole = a.bf16 && a.aligned && a.K % 8 == 0;   // W's rows need no copy
   if (!bwd) {
+    p.x = take(whole && a.ldx % 8 == 0 ? 0 : p.px * p.PL * 2);
     p.pw = p.copied * p.Kp;
-    p.w = take(p.pw * p.PL * 2);
-    p.off = take(p.groups * (p.vtiles + 1) * 4);
-    p.list = take(p.groups * p.group * a.k * 4);
+    p.w = take(whole ? 0 : p.pw * p.PL * 2);
+    p.off = take(a.entries ? p.groups * (p.vtiles + 1) * 4 : 0);
+    p.list = take(a.entries ? p.groups * p.group * a.k * 4 : 0);
     p.part = take(p.vtiles * a.M * 8);
     p.sums = take((int64_t)vocab_join_bytes(a));
     p.done = take(4);
@@ -1110,7 +1111,8 @@ TilesPlan tiles_plan(const VocabArgs& a, bool bwd) {
   p.piece = std::min(up(per(a.V, per(a.V, most)), 256), up(a.V, 8));
   p.copied = std::min(p.copied, p.piece);
   p.pw = p.copied * p.Kp;
-  p.w = take(p.pw * p.PL * 2);
+  p.x = take(p.px * (p.two ? 2 : p.PL) * 2);
+  p.w = take(whole ? 0 : p.pw * p.PL * 2);
   p.ldz = p.piece;
   p.pz = a.M * p.ldz;
   p.dx = a.M <= kFew && a.bf16 ? Choice{FEW, few_parts(a.K, p.piece)} : choose(a.M, a.K, p.piece, p.PL, true, FewP::BP, FewP::BQ);

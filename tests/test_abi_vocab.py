@@ -144,3 +144,43 @@ def test_calls(kind):
         assert refused(kind, dw=6 * FAKE) == L.OF_EINVAL
         assert refused(kind, accumulate=2) == L.OF_EINVAL
         assert refused(kind, dw=FAKE + 1) == L.OF_EALIGN
+
+
+def size(op, **kw):
+    return L.of_vocab_workspace_size(desc(**kw), op)
+
+
+def test_workspace_of_aligned_operands():
+    """bf16 operands of 16-byte pieces that are promised to be aligned: no room for copies of W, nor of a forward's X, and
+    none for entries where there are none."""
+    M, V, K = 4, 32768, 1024
+    kw = dict(M=M, V=V, K=K)
+    copy_w, copy_x = V * K * 2, M * K * 2
+    for op in (L.OF_VOCAB_FWD, L.OF_VOCAB_BWD):
+        assert size(op, **kw) - size(op, aligned=1, **kw) == copy_w + (copy_x if op == L.OF_VOCAB_FWD else 0)
+        # not for rows that are no whole pieces, or fp32 (whose planes are made)
+        for more in (dict(K=1023), dict(dtype=L.OF_F32, grad_dtype=L.OF_F32)):
+            assert size(op, **{**kw, **more}) == size(op, aligned=1, **{**kw, **more})
+    odd = dict(kw, ldx=1028, aligned=1)
+    assert size(L.OF_VOCAB_FWD, **odd) - size(L.OF_VOCAB_FWD, **kw, aligned=1) == copy_x
+    # a few statistics a row and tile
+    assert size(L.OF_VOCAB_FWD, aligned=1, **kw) <= 8 * M * V // 128 + (1 << 13)
+    # logits in bf16 would be 2 MB, 256 MB, 1 GB (a backward keeps 512 MB of their gradient: half of W at a time)
+    assert size(L.OF_VOCAB_FWD, M=32, V=32768, K=1024, aligned=1) < 1 << 17
+    assert size(L.OF_VOCAB_FWD, M=4096, V=32768, K=1024, topk=0, aligned=1) < 8 << 20
+    big = dict(M=8192, V=65536, K=4096)
+    assert size(L.OF_VOCAB_BWD, **big) - size(L.OF_VOCAB_BWD, aligned=1, **big) == 65536 // 2 * 4096 * 2
+    assert size(L.OF_VOCAB_FWD, topk=64, **big) > size(L.OF_VOCAB_FWD, **big)
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_aligned_operands_are_checked(kind):
+    more = {"topk": 4} if kind.startswith("distill") else {}
+    assert refused(kind, desc(aligned=2, **more)) == L.OF_EINVAL
+    assert refused(kind, desc(aligned=-1, **more)) == L.OF_EINVAL
+    d = desc(aligned=1, **more)
+    assert refused(kind, d, x=FAKE + 2) == L.OF_EALIGN
+    assert refused(kind, d, x=FAKE + 8) == L.OF_EALIGN
+    assert refused(kind, d, param(d, w_bf16=FAKE + 8)) == L.OF_EALIGN
+    f = desc(aligned=1, dtype=L.OF_F32, grad_dtype=L.OF_F32, **more)
+    assert refused(kind, f, param(f, w=FAKE + 4, w_bf16=None)) == L.OF_EALIGN

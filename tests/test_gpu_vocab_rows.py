@@ -111,3 +111,31 @@ def test_update_of_either_loss(gpu, dtype, M, V, k, hyper):
         assert torch.equal(a, b), (name, float((a - b).abs().max()))
     if dtype == "bf16":
         assert torch.equal(shadow, ref_shadow)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("M,V,K,k,gap", [(4, 3000, 64, 0, 0), (40, 300, 64, 0, 8), (70, 900, 257, 5, 0), (300, 2000, 128, 3, 3),
+                                         (600, 5000, 320, 0, 16), (600, 5000, 320, 7, 0)])
+def test_aligned_operands(gpu, dtype, M, V, K, k, gap):
+    """What the smaller workspace of aligned operands gives is the same, and nothing behind it is touched."""
+    c = Call(gpu, M, V, K, dtype, k=k, gap=gap)
+    c.fwd()
+    c.bwd()
+    want = [t.clone() for t in (c.loss, c.lse, c.zt, c.mean, c.dx, c.dw)]
+    c.d.aligned = 1
+    for op in c.ws:
+        c.ws[op] = torch.full((L.of_vocab_workspace_size(c.d, op) + 256,), 0xff, dtype=torch.uint8, device=gpu)
+    for t in (c.loss, c.lse, c.zt, c.mean, c.dx, c.dw):
+        t.fill_(7.0)
+    c.fwd()
+    c.bwd()
+    for a, b in zip((c.loss, c.lse, c.zt, c.mean, c.dx, c.dw), want):
+        assert torch.equal(a, b)
+    w, m, v = (torch.zeros(V, K, device=gpu) for _ in range(3))
+    if dtype == "f32":
+        w = c.dev_w
+    c.param = L.OfParam(w.data_ptr(), m.data_ptr(), v.data_ptr(), c.dev_w.data_ptr() if dtype == "bf16" else None, V * K)
+    c.dx.fill_(7.0)
+    c.bwd_fused(L.make_opt(OPTS[1], 1))
+    assert torch.equal(c.dx, want[4])
+    c.untouched()
