@@ -40,15 +40,22 @@ int64_t up(int64_t n, int64_t to) { return (n + to - 1) / to * to; }
 int64_t per(int64_t n, int64_t each) { return (n + each - 1) / each; }
 bool odd_rows(const void* p, int64_t ld, int64_t K) { return !aligned16(p) || ld % 8 != 0 || K % 8 != 0; }
 
-// The nearest bf16s of two values, which keep what that leaves (at most the largest bf16: the largest fp32 values keep
-// the rest).  An infinite value is all in its last part, the others are 0: that part meets only the other operand's
-// first, whose sign and whether it is 0 are its own, so that the products are those of fp32 (with an infinite first
-// part, the other operand's zeros and lower parts would make NaNs of them).  Two infinite factors meet nowhere: NaN.
-__device__ __forceinline__ uint32_t take_part(float& x, float& y, bool last = false) {
+// The nearest bf16s of two values, which keep what that leaves.  What rounds to infinity leaves infinity or NaN: such a
+// gradient shows.
+__device__ __forceinline__ uint32_t take_part(float& x, float& y) {
+  const uint32_t w = pack2(x, y);
+  x = __fsub_rn(x, __uint_as_float(w << 16));
+  y = __fsub_rn(y, __uint_as_float(w & 0xffff0000u));
+  return w;
+}
+// An operand's, at most the largest bf16 (the largest fp32 values keep the rest).  An infinite value is all in its last
+// part, the others are 0: that part meets only the other operand's first, whose sign and whether it is 0 are its own,
+// so that the products are those of fp32 (with an infinite first part, the other operand's zeros and lower parts would
+// make NaNs of them).  Two infinite factors meet nowhere: NaN.
+__device__ __forceinline__ uint32_t take_operand_part(float& x, float& y, bool last) {
+  if (last) return pack2(x, y);
   constexpr float most = 3.38953139e38f;
-  auto part = [&](float v) {   // (a NaN stays)
-    return last ? v : fabsf(v) == INFINITY ? 0.f : fabsf(v) > most ? copysignf(most, v) : v;
-  };
+  auto part = [&](float v) { return fabsf(v) == INFINITY ? 0.f : fabsf(v) > most ? copysignf(most, v) : v; };   // (a NaN stays)
   const uint32_t w = pack2(part(x), part(y));
   x = __fsub_rn(x, __uint_as_float(w << 16));
   y = __fsub_rn(y, __uint_as_float(w & 0xffff0000u));
@@ -445,7 +452,7 @@ struct RowCoef {
   float zt;
 };
 __device__ __forceinline__ RowCoef row_coef(const VocabArgs& a, int64_t row, float lse, float ct, int label) {
-  // (an infinite factor makes the row's gradient NaN: a loss scale's overflow must show, also where dX takes one plane of two)
+  // (an infinite factor makes the row's gradient NaN: a loss scale's overflow must show)
   float cp = __fmul_rn(ct, __fmaf_rn(2.f * a.z_loss, lse, 1.f));
   if (fabsf(cp) == INFINITY || fabsf(ct) == INFINITY) cp = ct = NAN;
   return RowCoef{lse, cp, ct, label, label >= 0 ? a.zt[row] : 0.f};
@@ -547,7 +554,7 @@ __global__ __launch_bounds__(256) void vocab_gather_kernel(const void* srcp, int
       for (int p = 0; p < 3; ++p) {
         uint32_t w[4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) w[e] = take_part(x[2 * e], x[2 * e + 1], p == 2);
+        for (int e = 0; e < 4; ++e) w[e] = take_operand_part(x[2 * e], x[2 * e + 1], p == 2);
         *reinterpret_cast<uint4*>(d + p * plane) = make_uint4(w[0], w[1], w[2], w[3]);
       }
     }
@@ -601,7 +608,7 @@ __global__ __launch_bounds__(256) void vocab_prepared_kernel(VocabArgs a, int* a
       if (twice) *reinterpret_cast<uint32_t*>(d + plane) = two;
     } else {
 #pragma unroll
-      for (int p = 0; p < 3; ++p) *reinterpret_cast<uint32_t*>(d + p * plane) = take_part(v[0], v[1], p == 2);
+      for (int p = 0; p < 3; ++p) *reinterpret_cast<uint32_t*>(d + p * plane) = take_operand_part(v[0], v[1], p == 2);
     }
   }
 }
@@ -718,8 +725,8 @@ struct GradEpi {
               float x[4];
 #pragma unroll
               for (int e = 0; e < 4; ++e) x[e] = acc[i][j][4 * g + e];
-              w.x = take_part(x[0], x[1], p == NP - 1);
-              w.y = take_part(x[2], x[3], p == NP - 1);
+              w.x = take_part(x[0], x[1]);
+              w.y = take_part(x[2], x[3]);
 #pragma unroll
               for (int e = 0; e < 4; ++e) acc[i][j][4 * g + e] = x[e];
             }
@@ -785,7 +792,7 @@ __global__ __launch_bounds__(256) void vocab_entry_kernel(VocabArgs a, const int
     float x = entry_grad(a.T, a.cap, a.zt[first + j], rc.lse, rc.cp, rc.ct, q), y = 0.f;
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
-      d[p * plane] = (uint16_t)take_part(x, y, p == NP - 1);
+      d[p * plane] = (uint16_t)take_part(x, y);
       if (p == 0 && fabsf(x) > fabsf(__int_as_float(most.y))) most = make_int2((int)v0 + place, __float_as_int(x));
     }
   }
