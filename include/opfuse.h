@@ -859,7 +859,7 @@ size_t of_vocab_workspace_size(const of_vocab_desc* d, int32_t op);
 /*
  * Forward.  loss, lse: fp32 [M]; zt: fp32 [M] (distillation [M, topk]): z of the label (of the entries), 0
  * where there is none; mean: fp32 [1] or NULL: the sum of the losses over the number of rows that
- * count (0 if none does).  The backward takes lse and zt as they are here, and the same X and W.
+ * count (0 if none does).  The backward takes lse and zt as they are here.
  */
 of_status of_vocab_xent_fwd(const of_vocab_desc* d, const void* x, const of_param* W, const int64_t* labels,
                             float* loss, float* lse, float* zt, float* mean, void* ws, size_t ws_bytes, void* stream);
@@ -868,8 +868,7 @@ of_status of_vocab_distill_fwd(const of_vocab_desc* d, const void* x, const of_p
                                size_t ws_bytes, void* stream);
 
 /*
- * Backward of sum_m dloss_m loss_m (dloss: fp32 [M]; NULL: of the mean).  With p = exp(z / T - lse), z of the
- * label and of entries from zt:
+ * Backward of sum_m dloss_m loss_m (dloss: fp32 [M]; NULL: of the mean).  With p = exp(z / T - lse):
  *   cross-entropy  dz_v = dloss (p_v (1 + 2 z_loss lse) - [v = label])
  *   distillation   dz_v = dloss T (p_v - sum of the q_j with id_j = v)
  *   ds = dz (1 - (z / softcap)^2),  dX = ds W,  dW = ds^T X

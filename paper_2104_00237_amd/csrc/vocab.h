@@ -159,17 +159,22 @@ __device__ __forceinline__ float row_loss(const VocabArgs& a, int64_t row, float
   return a.T * a.T * wave_sum(loss);
 }
 
-// The gradient at a place with logit z (capped): cp p - ct q, times the cap's slope there.
+// The gradient at a place with logit z (capped): cp p - ct q, times the cap's slope there; that of an entry from its
+// capped logit, which is all that the forward keeps.
 __device__ __forceinline__ float place_grad(float T, float z, float slope, float lse, float cp, float ct, float q) {
   const float p = expf(__fsub_rn(__fdiv_rn(z, T), lse));
   return __fmul_rn(__fmaf_rn(cp, p, -__fmul_rn(ct, q)), slope);
 }
-// An entry's, from the logit that the forward kept: where an entry has most of the probability, a rounding of its logit
-// is in lse too and leaves p - q alone; another product's rounding would not (fp32 forwards and backwards change
-// kernels at different sizes: 7701 rows over 190 of width 3904 were 8.5e-6 from float64 instead of 2.4e-6).
 __device__ __forceinline__ float entry_grad(float T, float cap, float z, float lse, float cp, float ct, float q) {
   const float r = cap > 0.f ? __fdiv_rn(z, cap) : 0.f;
   return place_grad(T, z, __fmaf_rn(-r, r, 1.f), lse, cp, ct, q);
+}
+// An entry's logit for it: the forward's own where the one computed again agrees with it up to rounding.  Where an
+// entry has most of the probability, a rounding of its logit is in lse too and leaves p - q alone; another
+// product's rounding would not (fp32 forwards and backwards change kernels at different sizes: 7701 rows over 190
+// of width 3904 were 8.5e-6 from float64 instead of 2.4e-6).  A W that has moved on from the forward's has its own.
+__device__ __forceinline__ float entry_logit(float z, float forward) {
+  return fabsf(z - forward) <= 0x1p-16f * (1.f + fabsf(forward)) ? forward : z;
 }
 
 // Statistics [parts][M] joined: lse, losses, their mean (vocab_tiles.hip).  sums: vocab_join_bytes; done: 0.

@@ -668,26 +668,30 @@ struct GradEpi {
         // rounding there, 1e-6 of a probability, is nothing beside bf16's)
         float slope[16];
         if constexpr (capped && PL == 1) tanh_block(acc[i][j], rcap, slope);
+        float at_label = 0.f;
         const float c2 = rT * kLog2E * (capped ? cap : 1.f), lse2 = rc[j].lse * kLog2E;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          float d;
+          float d, z;
           if constexpr (PL == 1) {
-            d = __builtin_amdgcn_exp2f(__fmaf_rn(acc[i][j][r], c2, -lse2));
+            const float x = acc[i][j][r];   // the logit over its cap
+            z = capped ? __fmul_rn(cap, x) : x;
+            d = __builtin_amdgcn_exp2f(__fmaf_rn(x, c2, -lse2));
           } else {
-            const float z = vocab_cap_exact(acc[i][j][r], capped ? cap : 0.f, &slope[r]);
+            z = vocab_cap_exact(acc[i][j][r], capped ? cap : 0.f, &slope[r]);
             d = __builtin_amdgcn_exp2f(__fmul_rn(kLog2E, __fmaf_rn(z, rT, -rc[j].lse)));
           }
           d = __fmul_rn(d, rc[j].cp);
           d = capped ? __fmul_rn(d, slope[r]) : d;
           acc[i][j][r] = d;
+          if (here) at_label = 8 * (r >> 2) + (r & 3) == label ? z : at_label;
         }
         if (some_none) {
 #pragma unroll
           for (int r = 0; r < 16; ++r) acc[i][j][r] = none ? 0.f : acc[i][j][r];
         }
         if (here) {
-          const float d = none ? 0.f : entry_grad(T, cap, rc[j].zt, rc[j].lse, rc[j].cp, rc[j].ct, 1.f);
+          const float d = none ? 0.f : entry_grad(T, cap, entry_logit(at_label, rc[j].zt), rc[j].lse, rc[j].cp, rc[j].ct, 1.f);
 #pragma unroll
           for (int r = 0; r < 16; ++r) acc[i][j][r] = 8 * (r >> 2) + (r & 3) == label ? d : acc[i][j][r];
           if (rest && label >= 0 && label < 32 && !(label & 4)) {
