@@ -859,7 +859,8 @@ size_t of_vocab_workspace_size(const of_vocab_desc* d, int32_t op);
 /*
  * Forward.  loss, lse: fp32 [M]; zt: fp32 [M] (distillation [M, topk]): z of the label (of the entries), 0
  * where there is none; mean: fp32 [1] or NULL: the sum of the losses over the number of rows that
- * count (0 if none does).  The backward takes lse and zt as they are here.
+ * count (0 if none does).  The backward takes lse and zt as they are here, of the same X and W: z of
+ * distillation's entries is zt's.
  */
 of_status of_vocab_xent_fwd(const of_vocab_desc* d, const void* x, const of_param* W, const int64_t* labels,
                             float* loss, float* lse, float* zt, float* mean, void* ws, size_t ws_bytes, void* stream);

@@ -169,10 +169,11 @@ __device__ __forceinline__ float entry_grad(float T, float cap, float z, float l
   const float r = cap > 0.f ? __fdiv_rn(z, cap) : 0.f;
   return place_grad(T, z, __fmaf_rn(-r, r, 1.f), lse, cp, ct, q);
 }
-// An entry's logit for it: the forward's own where the one computed again agrees with it up to rounding.  Where an
-// entry has most of the probability, a rounding of its logit is in lse too and leaves p - q alone; another
+// A label's logit for it: the forward's own where the one computed again agrees with it up to rounding.  Where a
+// label has most of the probability, a rounding of its logit is in lse too and leaves p - q alone; another
 // product's rounding would not (fp32 forwards and backwards change kernels at different sizes: 7701 rows over 190
 // of width 3904 were 8.5e-6 from float64 instead of 2.4e-6).  A W that has moved on from the forward's has its own.
+// (Distillation's entries have the forward's at every size: tiles store no logits to look at.)
 __device__ __forceinline__ float entry_logit(float z, float forward) {
   return fabsf(z - forward) <= 0x1p-16f * (1.f + fabsf(forward)) ? forward : z;
 }

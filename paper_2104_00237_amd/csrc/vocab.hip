@@ -129,7 +129,7 @@ __global__ __launch_bounds__(64) void vocab_clear_kernel(VocabArgs a, const floa
 }
 
 // The gradient of a chunk of a row's logits, in place of them.  An entry's place is written by its first
-// entry with the weights of all that name it; its logit is read before the row is overwritten.
+// entry with the weights of all that name it; a label's logit is read before the row is overwritten.
 __global__ __launch_bounds__(256) void vocab_grad_kernel(VocabArgs a, float* __restrict__ z, int64_t ldz, int64_t v0, int n,
                                                          const float2* coef, const float* counts, const float* total) {
   constexpr int EACH = kTopMax / 256;
@@ -160,9 +160,7 @@ __global__ __launch_bounds__(256) void vocab_grad_kernel(VocabArgs a, float* __r
     const float z = vocab_cap_exact(logit, a.cap, &slope);
     return place_grad(a.T, z, slope, lse, cp, 0.f, 0.f);
   };
-  auto entry = [&](int64_t i, int place, float q) {
-    return entry_grad(a.T, a.cap, entry_logit(vocab_cap_exact(s[place], a.cap), a.zt[i]), lse, cp, ct, q);
-  };
+  auto entry = [&](float z, float q) { return entry_grad(a.T, a.cap, z, lse, cp, ct, q); };
   const int64_t at = row * a.k;
   int where[EACH];
   float d[EACH];
@@ -170,7 +168,7 @@ __global__ __launch_bounds__(256) void vocab_grad_kernel(VocabArgs a, float* __r
     where[0] = -1;
     if (t == 0) {
       const int64_t id = a.ids[row] - v0;
-      if (id >= from && id < end) where[0] = (int)id, d[0] = entry(row, (int)id, 1.f);
+      if (id >= from && id < end) where[0] = (int)id, d[0] = entry(entry_logit(vocab_cap_exact(s[id], a.cap), a.zt[row]), 1.f);
     }
 #pragma unroll
     for (int u = 1; u < EACH; ++u) where[u] = -1;
@@ -200,7 +198,7 @@ __global__ __launch_bounds__(256) void vocab_grad_kernel(VocabArgs a, float* __r
           q = __fadd_rn(q, r.weight(teacher_logit(a, at + i + e)));
         }
       }
-      if (first) d[u] = entry(at + j, where[u], q);
+      if (first) d[u] = entry(a.zt[at + j], q);
       else where[u] = -1;
     }
   }

@@ -7,7 +7,7 @@ import torch
 
 from paper_2104_00237_amd import _lib as L
 from tests.test_gpu_vocab import TYPES, Call
-from tests.vocab_reference import near
+from tests.vocab_reference import near, target
 
 pytestmark = pytest.mark.gpu
 E = 2.0 ** -24
@@ -172,3 +172,47 @@ def test_many_entries(gpu, dtype, M, V, k):
     c.bwd()
     c.check_fwd()
     c.check_bwd()
+
+
+@pytest.mark.parametrize("step", [0.5, 0.02])
+@pytest.mark.parametrize("M,V,K", [(40, 300, 40), (300, 1031, 64), (512, 5000, 64), (1030, 16384, 32)])
+@pytest.mark.parametrize("dtype,k,cap", [("f32", 0, 0.0), ("bf16", 0, 0.0), ("f32", 0, 6.0), ("bf16", 0, 6.0), ("f32", 3, 0.0),
+                                         ("bf16", 3, 0.0), ("f32", 70, 6.0), ("bf16", 70, 6.0)])
+def test_a_head_that_moved_on(gpu, dtype, k, cap, M, V, K, step):
+    """W other than the forward's: p = exp(z / T - lse) of the forward's lse and W's own z, at every size; but that
+    distillation's entries have the forward's z.
+
+    Bounds as in tests/vocab_reference.py with lse (and entries' z) given; a label's logit may be the forward's where it
+    differs by 2^-16 (1 + |z|)."""
+    T = 2.0 if k else 1.0
+    c = Call(gpu, M, V, K, dtype, k=k, T=T, cap=cap, given=True, grads="f32")
+    c.fwd()
+    w = (c.w.float() * (1 + step * torch.randn(V, K, generator=torch.Generator().manual_seed(3)))).to(c.w.dtype)
+    c.dev_w.copy_(w)
+    c.bwd()
+    x, w, lse = c.dev_x.double(), w.double().to(gpu), c.lse.double()[:, None]
+    ids = c.t[0]
+    place = torch.where(ids >= 0, ids, V)   # (what is no entry goes to a column behind)
+    at = torch.zeros(M, V + 1, device=gpu, dtype=torch.bool).scatter_(1, place, True)[:, :V]
+    q, counts = target(ids, c.t[1] if k else None, T, V)
+    s = x @ w.t()
+    z = cap * torch.tanh(s / cap) if cap else s
+    dz = (K + 8) * E * (x.abs() @ w.abs().t()) + 4 * E * cap
+    if k:
+        z = torch.where(at, torch.zeros(M, V + 1, device=gpu).double().scatter_(1, place, c.zt.double())[:, :V], z)
+        dz = torch.where(at, 0.0, dz)
+    else:
+        dz = dz + at * 2.0 ** -16 * (1 + z.abs())
+    U, du, p = z / T, dz / T, torch.exp(z / T - lse)
+    u = TYPES[dtype][2]
+    Q = torch.zeros_like(p).scatter_add_(1, ids.clamp_min(0), q)
+    f = torch.where(counts, c.dev_dloss.double() * T, 0.0)[:, None]
+    d = p - Q
+    e = 1.01 * p * (du + 8 * E * (1 + U.abs() + lse.abs())) + 8 * E * p + (2 * c.k + 16) * E * Q
+    if cap:
+        slope = 1 - (z / cap) ** 2
+        e = e * slope + d.abs() * (2 * dz / cap + 8 * E)
+        d = d * slope
+    d, e = d * f, e * f + (u + 8 * E) * (d * f).abs() + 1e-38
+    near("dx", c.dx, d @ w, e @ w.abs() + (V + 8) * E * (d.abs() @ w.abs()))
+    near("dw", c.dw, d.t() @ x, e.t() @ x.abs() + (M + 8) * E * (d.abs().t() @ x.abs()))
