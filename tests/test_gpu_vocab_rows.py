@@ -139,3 +139,74 @@ def test_aligned_operands(gpu, dtype, M, V, K, k, gap):
     c.bwd_fused(L.make_opt(OPTS[1], 1))
     assert torch.equal(c.dx, want[4])
     c.untouched()
+
+
+@pytest.mark.parametrize("dtype,M,V,k", [("bf16", 500, 700, 0), ("bf16", 500, 700, 5), ("f32", 512, 5000, 3), ("f32", 300, 8000, 0),
+                                         ("f32", 2500, 90, 0), ("bf16", 60, 300, 2)])
+def test_replays_of_other_targets(gpu, dtype, M, V, k):
+    """Forward, backward and update captured once and replayed with other targets: as many rows with a gradient as there are
+    (all, some, one, none), and every other result as the eager calls give it."""
+    c = Call(gpu, M, V, 64, dtype, k=k, ids=torch.randint(0, V, (M, max(k, 1)), generator=torch.Generator().manual_seed(4)))
+    w = c.dev_w.float() if dtype == "bf16" else c.dev_w
+    shadow = c.dev_w if dtype == "bf16" else torch.zeros(1, device=gpu)
+    m, v = torch.zeros_like(w), torch.zeros_like(w)
+    c.param = L.OfParam(w.data_ptr(), m.data_ptr(), v.data_ptr(), shadow.data_ptr() if dtype == "bf16" else None, c.V * c.K)
+    step = torch.zeros(1, dtype=torch.int64, device=gpu)
+    opt = L.make_opt(OPTS[1], 0, step.data_ptr())
+    out, state = (c.loss, c.lse, c.zt, c.mean, c.dx, c.dw), (w, m, v, shadow, step)
+
+    def all_calls():
+        c.fwd()
+        c.bwd()
+        step.add_(1)
+        c.bwd_fused(opt)
+
+    start = [t.clone() for t in state]
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        all_calls()
+    s.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        all_calls()
+    g = torch.Generator().manual_seed(2)
+    for out_of in (0.0, 0.3, 1.0, 0.9, 2.0, 0.0):
+        ids = c.ids.clone()
+        ids[torch.rand(M, generator=g) < out_of] = -1
+        if out_of == 1.0:
+            ids[M // 2] = 1
+        c.t[0].copy_(ids)
+        results = []
+        for call in (all_calls, graph.replay):
+            for t, a in zip(state, start):
+                t.copy_(a)
+            for t in out:
+                t.fill_(7.0)
+            torch.cuda.synchronize()
+            call()
+            torch.cuda.synchronize()
+            results.append([t.clone() for t in out + state])
+        for a, b in zip(*results):
+            assert torch.equal(a, b), out_of
+
+
+@pytest.mark.parametrize("dtype,M,V,k", [("bf16", 500, 700, 0), ("bf16", 40, 300, 3), ("f32", 512, 5000, 0), ("f32", 40, 300, 2)])
+def test_update_with_a_clipping_factor(gpu, dtype, M, V, k):
+    """The factor of a clipped gradient applies to dW and the earlier gradient alike, as in the element-wise update."""
+    K = 48
+    c = Call(gpu, M, V, K, dtype, k=k, grads="f32")
+    w = c.dev_w.float() if dtype == "bf16" else c.dev_w
+    m, v = torch.zeros_like(w), torch.zeros_like(w)
+    extra = torch.randn(V, K, generator=torch.Generator().manual_seed(6)).mul_(1e-4).to(gpu)
+    factor = torch.tensor([0.37], device=gpu)
+    opt = L.make_opt(OPTS[0], 3)
+    opt.grad_scale = factor.data_ptr()
+    c.fwd()
+    c.bwd()
+    ref = [t.clone() for t in (w, m, v)]
+    total = c.dw + extra
+    L.of_elementwise_fused_update(L.param_of(*ref), total.data_ptr(), 1, 0, opt, c._stream())
+    c.param = L.OfParam(w.data_ptr(), m.data_ptr(), v.data_ptr(), c.dev_w.data_ptr() if dtype == "bf16" else None, V * K)
+    c.bwd_fused(opt, extra)
+    for a, b in zip((w, m, v), ref):
+        assert torch.equal(a, b)
