@@ -829,6 +829,8 @@ of_status of_attn_bwd(const of_attn_desc* d, const void* q, const void* k, const
  *
  * dtype is the type in memory of X and of the head that is read (OF_F32: W->w; OF_BF16: W->w_bf16,
  * uint16 bit patterns) and of the matrix-core operands; logits, statistics and sums are fp32 or wider.
+ * A probability is as exact as the fp32 lse that it is taken from: |lse| 2^-23 of it.  Gradients of bf16 operands with
+ * all of fp32's bits: give fp32 operands.
  * Any alignment to the elements' size is accepted; bf16 rows of 16-byte pieces (K and ldx multiples of 8) save a
  * copy, and its workspace with `aligned`.  M * V < 2^37,
  * V * K <= 2^36, M * K < 2^29, X < 2 GiB.

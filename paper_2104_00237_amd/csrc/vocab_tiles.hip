@@ -28,7 +28,7 @@ namespace {
 // wavefronts a SIMD, 128x128 where those would not fill the chip, 32 wide for few rows.
 using Big = TileShape<4, 2, 2, 4, 32, 4, 2>;
 using Mid = TileShape<2, 2, 2, 2, 32, 4, 2>;
-using Half = TileShape<4, 2, 2, 2, 32, 3, 2>;   // 256x128, two workgroups a CU: one's epilogue beside the other's MFMAs
+using Half = TileShape<4, 2, 2, 2, 32, 3, 2>;   // 256x128, two workgroups a CU
 using FewQ = TileShape<1, 1, 4, 1, 64, 4, 2>;   // 128 x 32
 using FewP = TileShape<1, 1, 1, 4, 64, 4, 2>;   // 32 x 128
 
@@ -665,7 +665,7 @@ struct GradEpi {
         const bool here = __any(label >= 0 && label < 32);
         constexpr bool capped = decltype(Capped)::value;
         // bf16 operands: what is left of the logit is tanh alone, and lse is taken off in units of log2 (its
-        // rounding there, 1e-6 of a probability, is nothing beside bf16's)
+        // rounding there is one of lse's own size, |lse| 2^-24 of a probability: 1e-6 at 16)
         float slope[16];
         if constexpr (capped && PL == 1) tanh_block(acc[i][j], rcap, slope);
         float at_label = 0.f;
@@ -1248,7 +1248,10 @@ struct Tiles {
       return hipGetLastError();
     }
     if (g.dw) return product<T, PL, false, false>(dz, x, n, p.Kp, R, rows, 1, HeadEpi<T, false>{g}, s);
-    // an update's memory traffic beside another workgroup's MFMAs: two workgroups a CU
+    // An update's tiles are smaller, two workgroups a CU.  Whole calls in us, 256x256 / these: fp32 1024 rows over 32768
+    // of width 1024 1290 / 1250, 4096 over 16384 1962 / 2000; bf16 (fp32 dX) 512 rows over 32768 482 / 495, 4096
+    // 1109 / 1111, of width 4096 4007 / 3942.  Both workgroups of a CU reach their updates together: the products
+    // do not hide them (MFMAs 37 % busy in fp32).
     using U = std::conditional_t<std::is_same_v<T, Big>, std::conditional_t<PL == 1, Half, Mid>, T>;
     return product<U, PL, false, false>(dz, x, n, p.Kp, R, rows, 1, HeadEpi<U, true>{g}, s);
   }
